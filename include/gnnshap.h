@@ -42,7 +42,9 @@
  *     GNNSHAP_EINVAL or GNNSHAP_ECAPACITY nothing is written except the sizes
  *     a call reports.  gnnshap_last_error() gives a thread-local message about
  *     the last failure.
- *   - All floating-point device data is fp32, row-major.
+ *   - All floating-point device data is fp32, row-major, except the token
+ *     operators' (gnnshap_cache_*, gnnshap_token_*), which name their element
+ *     type and strides.
  */
 #ifndef GNNSHAP_H
 #define GNNSHAP_H
@@ -508,6 +510,162 @@ int gnnshap_gat_explain_batch(const gnnshap_subgraph* sgs, const gnnshap_sample_
                               const gnnshap_class* classes, int64_t n, const gnnshap_gat* m, int32_t target_class,
                               uint64_t* masks, float* weights, float* y, float* f_empty_full, int32_t* class_out,
                               float* phi, int32_t* info, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Answers of token models: the players are prompt tokens.                  */
+/* ------------------------------------------------------------------------ */
+/* The plan, the sampler and the least squares above do not ask what a player
+ * is.  When the players are tokens of a prompt, a coalition's value is the
+ * log probability of the model's answer computed from the keys and values of
+ * its tokens alone: every coalition's new token attends over ONE cached
+ * prompt, seeing the positions whose mask bit is set, and over tokens of its
+ * own.  The calls below are the steps of such a model that touch the cache
+ * or the answer; the products with its weights stay with the caller.
+ *
+ * Strides are in elements and need no alignment; the innermost axis
+ * (head_dim elements, or the vocabulary) is contiguous.  `info` [dev, one
+ * int32, may be NULL] is set to 1 where a call meets a page, row, position,
+ * length or token id out of its range, and left as it is otherwise; the call
+ * then reads and writes nothing out of its buffers, and what it returns for
+ * that token or row is unspecified. */
+
+enum gnnshap_dtype { GNNSHAP_F32 = 0, GNNSHAP_F16 = 1, GNNSHAP_BF16 = 2 };
+
+#define GNNSHAP_MAX_HEAD_DIM 256
+#define GNNSHAP_MAX_TOP 64
+
+/* A paged cache of keys and values: element d of head h of the token in slot
+ * s of page p is k[p page_stride + s slot_stride + h head_stride + d], the
+ * value v[...] likewise.  head_dim: a multiple of 8 up to
+ * GNNSHAP_MAX_HEAD_DIM.  A page table holds the pages of one sequence per
+ * row: its token i is in slot i % page_size of page table[row][i / page_size]. */
+typedef struct {
+  int32_t dtype;      /* gnnshap_dtype of keys, values, queries and outputs */
+  int32_t kv_heads;
+  int32_t head_dim;
+  int32_t page_size;  /* tokens per page, any number >= 1 */
+  int64_t num_pages;
+  int64_t page_stride, slot_stride, head_stride;
+  void* k;            /* [dev] */
+  void* v;            /* [dev] */
+} gnnshap_cache;
+
+/* New tokens on their way into a cache. */
+typedef struct {
+  int64_t num_tokens;
+  const void* k;             /* [dev] key of token t, head h: k + t k_token_stride + h k_head_stride */
+  int64_t k_token_stride, k_head_stride;
+  const void* v;             /* [dev] values, likewise */
+  int64_t v_token_stride, v_head_stride;
+  const int32_t* rows;       /* [dev] row of the page table of each token; NULL: token t is of row t */
+  const int32_t* index;      /* [dev] place of each token in its sequence; negative: not stored */
+  const int32_t* positions;  /* [dev] position of each token for the rotation; NULL: index.  Negative: not rotated */
+  const int32_t* table;      /* [dev] num_rows x table_width, row-major */
+  int64_t num_rows, table_width;
+  const float* cos;          /* [dev] num_positions x rot_dim / 2; NULL: no rotation */
+  const float* sin;          /* [dev] likewise */
+  int64_t num_positions;
+  int32_t rot_dim;           /* even, at most head_dim; the elements from rot_dim on are copied */
+  int32_t interleaved;       /* pair i of the rotation: elements 2 i and 2 i + 1; if 0, i and i + rot_dim / 2 */
+  int32_t heads;             /* heads of the queries */
+  int32_t reserved;
+  const void* q;             /* [dev] queries of the same tokens, rotated into q_out; NULL: none */
+  int64_t q_token_stride, q_head_stride;
+  void* q_out;               /* [dev] may be q itself, with the same strides */
+  int64_t q_out_token_stride, q_out_head_stride;
+} gnnshap_new_tokens;
+
+/* Appends keys and values of new tokens to the cache, rotating the keys (and
+ * the tokens' queries, if given) by their positions on the way: the pair
+ * (x, y) becomes (x cos - y sin, y cos + x sin), in fp32, rounded once.
+ * Tokens may be of any sequences in any order (a prompt's, one of every
+ * row's); two tokens of one slot leave either one's vectors there.  The
+ * cache must not overlap the inputs.  EINVAL: sizes, NULL arrays;
+ * EUNSUPPORTED: head_dim, dtype. */
+int gnnshap_cache_append(const gnnshap_cache* cache, const gnnshap_new_tokens* tokens, int32_t* info, void* stream);
+
+/* One new token's queries per row, and what each row sees.  The context of
+ * row b is the shared part of its group, the max_shared or fewer tokens of
+ * row b / rows_per_group of shared_table, followed by its own part, the
+ * lengths[b] tokens of row b of table.  Either part may be missing (a NULL
+ * table).  Position j of the context is player j - first_player; row b sees
+ * it if it is no player (outside 0 .. num_players - 1) or that bit of row b
+ * of `masks` is set (the sampler's layout). */
+typedef struct {
+  int64_t num_rows;
+  int32_t heads;                 /* a multiple of the cache's kv_heads: head h reads head h / (heads / kv_heads) */
+  int32_t reserved;
+  const void* q;                 /* [dev] */
+  int64_t q_row_stride, q_head_stride;
+  void* out;                     /* [dev] must not overlap q */
+  int64_t out_row_stride, out_head_stride;
+  float* lse;                    /* [dev] num_rows x heads, or NULL */
+  const int32_t* table;          /* [dev] num_rows x table_width, or NULL */
+  const int32_t* lengths;        /* [dev] num_rows */
+  int64_t table_width, max_length;       /* max_length: no length is larger; at most table_width pages' tokens */
+  const int32_t* shared_table;   /* [dev] groups x shared_width, or NULL */
+  const int32_t* shared_lengths; /* [dev] groups */
+  int64_t shared_width, max_shared;
+  int64_t rows_per_group;        /* divides num_rows; read with shared_table only */
+  const uint64_t* masks;         /* [dev] num_rows x mask_words, or NULL (num_players is then 0) */
+  int64_t mask_words, num_players, first_player;
+  double scale;                  /* scores are scale q.k; not 0 */
+} gnnshap_queries;
+
+/* Bytes of device workspace for gnnshap_cache_attend (it holds the parts of
+ * contexts that are split over their length). */
+int gnnshap_cache_attend_workspace(const gnnshap_cache* cache, const gnnshap_queries* queries, size_t* bytes);
+
+/* Attention of one new token per row: with s_j = scale q.k_j over the visible
+ * positions j, out = sum_j exp(s_j) v_j / sum_j exp(s_j) and lse =
+ * log sum_j exp(s_j), per head, with the statistics and sums in fp32 (the
+ * weights exp(s_j - max) enter the product with the values in the values'
+ * type).  A row that sees nothing, or whose every score is -inf, has out 0
+ * and lse -inf.  Keys and values of positions that a row does not see do not
+ * reach it, whatever they hold (NaN and infinities too).  EINVAL: sizes,
+ * NULL arrays; EUNSUPPORTED: head_dim, dtype, more than 2^31 - 1 positions;
+ * ECAPACITY: workspace. */
+int gnnshap_cache_attend(const gnnshap_cache* cache, const gnnshap_queries* queries, int32_t* info, void* ws,
+                         size_t ws_bytes, void* stream);
+
+/* Rows of logits and what is read off them.  Outputs may be NULL, each. */
+typedef struct {
+  int32_t dtype;            /* gnnshap_dtype of the logits */
+  int32_t top;              /* alternatives per row, 0 .. min(vocab, GNNSHAP_MAX_TOP) */
+  int64_t num_rows, vocab;
+  const void* logits;       /* [dev] row b at logits + b row_stride */
+  int64_t row_stride;
+  const int64_t* targets;   /* [dev] given token of each row; NULL, or negative: none (logprob 0, rank -1) */
+  float* logprob;           /* [dev] num_rows: log probability of the given token */
+  float* entropy;           /* [dev] num_rows: -sum p log p (natural logarithm) */
+  float* lse;               /* [dev] num_rows: log sum exp of the logits */
+  int32_t* rank;            /* [dev] num_rows: how many logits are larger than the given token's */
+  float* top_logprob;       /* [dev] num_rows x top: log probabilities in falling order */
+  int32_t* top_id;          /* [dev] num_rows x top: their tokens; of equal logits the lowest token first */
+} gnnshap_logits;
+
+int gnnshap_token_logprobs_workspace(const gnnshap_logits* logits, size_t* bytes);
+
+/* One pass over the logits.  A logit of -inf is a token of probability 0 (log
+ * probability -inf); a row of nothing else has lse, logprob and top_logprob
+ * -inf and entropy 0.  A row with a NaN or +inf has lse, logprob, entropy and
+ * top_logprob NaN, and its rank and top_id are unspecified (tokens of the
+ * vocabulary).  EINVAL: sizes, NULL logits; EUNSUPPORTED: dtype, a vocabulary
+ * over 2^30; ECAPACITY: workspace. */
+int gnnshap_token_logprobs(const gnnshap_logits* logits, int32_t* info, void* ws, size_t ws_bytes, void* stream);
+
+/* Gradient by the logits of sum_b g_logprob[b] logprob[b] + g_entropy[b]
+ * entropy[b]: with p = exp(x - lse),
+ *     d x_j = g_logprob (1[j = target] - p_j) - g_entropy p_j (log p_j + entropy),
+ * written in the logits' type to grad + b grad_stride (which may be the
+ * logits themselves, with their stride).  Reads num_rows, vocab, dtype,
+ * logits, row_stride, targets, and lse and entropy as
+ * gnnshap_token_logprobs wrote them; g_logprob and g_entropy [dev, num_rows]
+ * may be NULL (0); entropy is read with g_entropy only.  A row without a
+ * target has no g_logprob.  A row of lse -inf has gradient 0.  EINVAL,
+ * EUNSUPPORTED as above. */
+int gnnshap_token_logprobs_backward(const gnnshap_logits* logits, const float* g_logprob, const float* g_entropy,
+                                    void* grad, int64_t grad_stride, int32_t* info, void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Diagnostics: HIP-event timing of one kernel.                             */

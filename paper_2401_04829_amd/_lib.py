@@ -51,6 +51,35 @@ class gnnshap_gat(ctypes.Structure):
                 ("att_src2", c_vp), ("att_dst2", c_vp), ("b2", c_vp), ("negative_slope", c_dbl)]
 
 
+class gnnshap_cache(ctypes.Structure):
+    _fields_ = [("dtype", c_i32), ("kv_heads", c_i32), ("head_dim", c_i32), ("page_size", c_i32), ("num_pages", c_i64),
+                ("page_stride", c_i64), ("slot_stride", c_i64), ("head_stride", c_i64), ("k", c_vp), ("v", c_vp)]
+
+
+class gnnshap_new_tokens(ctypes.Structure):
+    _fields_ = [("num_tokens", c_i64), ("k", c_vp), ("k_token_stride", c_i64), ("k_head_stride", c_i64), ("v", c_vp),
+                ("v_token_stride", c_i64), ("v_head_stride", c_i64), ("rows", c_vp), ("index", c_vp),
+                ("positions", c_vp), ("table", c_vp), ("num_rows", c_i64), ("table_width", c_i64), ("cos", c_vp),
+                ("sin", c_vp), ("num_positions", c_i64), ("rot_dim", c_i32), ("interleaved", c_i32), ("heads", c_i32),
+                ("reserved", c_i32), ("q", c_vp), ("q_token_stride", c_i64), ("q_head_stride", c_i64),
+                ("q_out", c_vp), ("q_out_token_stride", c_i64), ("q_out_head_stride", c_i64)]
+
+
+class gnnshap_queries(ctypes.Structure):
+    _fields_ = [("num_rows", c_i64), ("heads", c_i32), ("reserved", c_i32), ("q", c_vp), ("q_row_stride", c_i64),
+                ("q_head_stride", c_i64), ("out", c_vp), ("out_row_stride", c_i64), ("out_head_stride", c_i64),
+                ("lse", c_vp), ("table", c_vp), ("lengths", c_vp), ("table_width", c_i64), ("max_length", c_i64),
+                ("shared_table", c_vp), ("shared_lengths", c_vp), ("shared_width", c_i64), ("max_shared", c_i64),
+                ("rows_per_group", c_i64), ("masks", c_vp), ("mask_words", c_i64), ("num_players", c_i64),
+                ("first_player", c_i64), ("scale", c_dbl)]
+
+
+class gnnshap_logits(ctypes.Structure):
+    _fields_ = [("dtype", c_i32), ("top", c_i32), ("num_rows", c_i64), ("vocab", c_i64), ("logits", c_vp),
+                ("row_stride", c_i64), ("targets", c_vp), ("logprob", c_vp), ("entropy", c_vp), ("lse", c_vp),
+                ("rank", c_vp), ("top_logprob", c_vp), ("top_id", c_vp)]
+
+
 _P = ctypes.POINTER
 _SIGNATURES = {
     "gnnshap_status_str": (ctypes.c_char_p, [ctypes.c_int]),
@@ -111,6 +140,13 @@ _SIGNATURES = {
                                                   _P(ctypes.c_size_t)]),
     "gnnshap_gat_eval_coalitions": (ctypes.c_int, [_P(gnnshap_subgraph), _P(gnnshap_gat), c_i32, c_vp, c_i64, c_i64,
                                                    c_vp, c_vp, c_vp, c_vp, ctypes.c_size_t, c_vp]),
+    "gnnshap_cache_append": (ctypes.c_int, [_P(gnnshap_cache), _P(gnnshap_new_tokens), c_vp, c_vp]),
+    "gnnshap_cache_attend_workspace": (ctypes.c_int, [_P(gnnshap_cache), _P(gnnshap_queries), _P(ctypes.c_size_t)]),
+    "gnnshap_cache_attend": (ctypes.c_int, [_P(gnnshap_cache), _P(gnnshap_queries), c_vp, c_vp, ctypes.c_size_t,
+                                            c_vp]),
+    "gnnshap_token_logprobs_workspace": (ctypes.c_int, [_P(gnnshap_logits), _P(ctypes.c_size_t)]),
+    "gnnshap_token_logprobs": (ctypes.c_int, [_P(gnnshap_logits), c_vp, c_vp, ctypes.c_size_t, c_vp]),
+    "gnnshap_token_logprobs_backward": (ctypes.c_int, [_P(gnnshap_logits), c_vp, c_vp, c_vp, c_i64, c_vp, c_vp]),
     "gnnshap_timing_begin": (ctypes.c_int, [ctypes.c_char_p]),
     "gnnshap_timing_end": (ctypes.c_int, [_P(ctypes.c_double), _P(c_i64)]),
     "gnnshap_timing_solves": (ctypes.c_int, [_P(c_i64), c_i64, _P(c_i64)]),
@@ -397,3 +433,32 @@ def gnnshap_fidelity_masks(phi_ptr, M, sparsity, top_k, masks_ptr, stream):
 
 def gnnshap_fidelity_average(terms_ptr, n, stride, avg_ptr, stream):
     check(load().gnnshap_fidelity_average(terms_ptr, int(n), int(stride), avg_ptr, stream), "fidelity_average")
+
+
+def gnnshap_cache_append(cache, tokens, info_ptr, stream):
+    check(load().gnnshap_cache_append(cache, tokens, info_ptr, stream), "cache_append")
+
+
+def gnnshap_cache_attend_workspace(cache, queries):
+    n = ctypes.c_size_t()
+    check(load().gnnshap_cache_attend_workspace(cache, queries, n), "cache_attend_workspace")
+    return n.value
+
+
+def gnnshap_cache_attend(cache, queries, info_ptr, ws_ptr, ws_bytes, stream):
+    check(load().gnnshap_cache_attend(cache, queries, info_ptr, ws_ptr, ws_bytes, stream), "cache_attend")
+
+
+def gnnshap_token_logprobs_workspace(logits):
+    n = ctypes.c_size_t()
+    check(load().gnnshap_token_logprobs_workspace(logits, n), "token_logprobs_workspace")
+    return n.value
+
+
+def gnnshap_token_logprobs(logits, info_ptr, ws_ptr, ws_bytes, stream):
+    check(load().gnnshap_token_logprobs(logits, info_ptr, ws_ptr, ws_bytes, stream), "token_logprobs")
+
+
+def gnnshap_token_logprobs_backward(logits, g_logprob_ptr, g_entropy_ptr, grad_ptr, grad_stride, info_ptr, stream):
+    check(load().gnnshap_token_logprobs_backward(logits, g_logprob_ptr, g_entropy_ptr, grad_ptr, grad_stride,
+                                                 info_ptr, stream), "token_logprobs_backward")

@@ -1,0 +1,228 @@
+"""Torch-facing calls that explain a token model's answer.
+
+The players are tokens of a prompt.  Their keys and values are cached once
+(`append_tokens` into a `PagedCache`); under a coalition, the new token
+attends over the cached prompt, seeing the positions its mask keeps, and over
+tokens of its own (`attend`); the answer's log probability is the coalition's
+value (`token_logprobs`), from which `AnswerExplainer` takes the Shapley
+values with the library's sampler and least squares.
+
+Torch provides device memory and streams; the work runs in libgnnshap.so on
+the current stream.  Every tensor must be on the cache's (the logits') device.
+"""
+import math
+from typing import NamedTuple
+
+import torch
+
+from . import _lib as L
+
+_DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _stream(device):
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def _vector(t, name, dtype, size, device):
+    """The address of an optional contiguous tensor of `dtype` and `size` (None: any shape)."""
+    if t is None:
+        return None
+    _need(t.dtype == dtype and t.device == device and t.is_contiguous() and (size is None or tuple(t.shape) == size),
+          f"{name}: a contiguous {dtype} tensor of shape {size} on {device} is needed, got {t.dtype} {tuple(t.shape)} "
+          f"on {t.device}")
+    return t.data_ptr()
+
+
+def _heads(t, name, heads, dim, dtype, device):
+    """Checks a [rows, heads, dim] tensor whose last axis is contiguous; its address and two strides."""
+    _need(t.dim() == 3 and t.dtype == dtype and t.device == device and t.shape[2] == dim
+          and (heads is None or t.shape[1] == heads) and (t.stride(2) == 1 or t.numel() == 0),
+          f"{name}: a [rows, {heads or 'heads'}, {dim}] {dtype} tensor on {device} with a contiguous last axis is "
+          f"needed, got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+class PagedCache:
+    """Keys and values in pages: `k` and `v` are [pages, page size, kv heads,
+    head dim] tensors (or views, such as of [pages, kv heads, page size, head
+    dim]) of one type and one set of strides, the head dim contiguous.  A page
+    table, int32 [rows, pages of a row], names the pages of each sequence."""
+
+    def __init__(self, k, v):
+        _need(k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype
+              and k.device == v.device, "keys and values: two [pages, page size, kv heads, head dim] tensors of one "
+              "type, device and set of strides are needed")
+        _need(k.dtype in _DTYPES, f"cache type {k.dtype} is not one of float32, float16, bfloat16")
+        _need(k.is_cuda and k.stride(3) == 1, "the cache must be on a GPU, its head dim contiguous")
+        self.k, self.v = k, v
+        pages, page, heads, dim = k.shape
+        self.kv_heads, self.head_dim, self.page_size = heads, dim, page
+        self.dtype, self.device = k.dtype, k.device
+        self._c = L.gnnshap_cache(_DTYPES[k.dtype], heads, dim, page, pages, k.stride(0), k.stride(1), k.stride(2),
+                                  k.data_ptr(), v.data_ptr())
+
+    @classmethod
+    def empty(cls, pages, page_size, kv_heads, head_dim, dtype=torch.bfloat16, device="cuda"):
+        kv = torch.zeros((2, pages, page_size, kv_heads, head_dim), dtype=dtype, device=device)
+        return cls(kv[0], kv[1])
+
+
+def append_tokens(cache, k, v, table, index, rows=None, positions=None, q=None, cos=None, sin=None, interleaved=False,
+                  q_out=None, info=None):
+    """gnnshap_cache_append: writes keys and values [tokens, kv heads, head
+    dim] of new tokens into the cache, token t at place index[t] (int32;
+    negative: not stored) of the sequence in row rows[t] (int32; None: t) of
+    `table`.  With cos and sin (float32 [positions, rot dim / 2]) keys are
+    rotated by positions[t] (int32; None: index), and so are the queries q
+    [tokens, heads, head dim] of the same tokens, which are returned (in
+    q_out, which may be q).  info: int32 [1], set to 1 on an index out of
+    range."""
+    dtype, dev, dim = cache.dtype, cache.device, cache.head_dim
+    n = k.shape[0]
+    kp = _heads(k, "k", cache.kv_heads, dim, dtype, dev)
+    vp = _heads(v, "v", cache.kv_heads, dim, dtype, dev)
+    _need(v.shape[0] == n, f"{n} keys and {v.shape[0]} values")
+    _need(table.dim() == 2, "table: [rows, pages of a row]")
+    heads, qp, op = 0, (None, 0, 0), (None, 0, 0)
+    if q is not None:
+        heads = q.shape[1]
+        qp = _heads(q, "q", heads, dim, dtype, dev)
+        q_out = torch.empty((n, heads, dim), dtype=dtype, device=dev) if q_out is None else q_out
+        op = _heads(q_out, "q_out", heads, dim, dtype, dev)
+        _need(q.shape[0] == n and q_out.shape[0] == n, f"{q.shape[0]} queries of {n} tokens")
+    angles = (0, 0)
+    if cos is not None:
+        _need(sin is not None and cos.dim() == 2, "cos and sin: two [positions, rot dim / 2] tensors")
+        angles = tuple(cos.shape)
+    t = L.gnnshap_new_tokens(
+        n, *kp, *vp, _vector(rows, "rows", torch.int32, (n,), dev), _vector(index, "index", torch.int32, (n,), dev),
+        _vector(positions, "positions", torch.int32, (n,), dev), _vector(table, "table", torch.int32, None, dev),
+        table.shape[0], table.shape[1], _vector(cos, "cos", torch.float32, angles, dev),
+        _vector(sin, "sin", torch.float32, angles, dev), angles[0], 2 * angles[1], int(interleaved), heads, 0, *qp, *op)
+    with torch.cuda.device(dev):
+        L.gnnshap_cache_append(cache._c, t, _vector(info, "info", torch.int32, (1,), dev), _stream(dev))
+    return q_out
+
+
+def attend(cache, q, table=None, lengths=None, max_length=None, shared_table=None, shared_lengths=None,
+           max_shared=None, masks=None, num_players=None, first_player=0, scale=None, out=None, return_lse=False,
+           info=None):
+    """gnnshap_cache_attend: attention of one new token per row, q [rows,
+    heads, head dim].  Row b sees lengths[b] tokens of row b of `table` and,
+    before them, the shared part of its group: shared_lengths[g] tokens of row
+    g of shared_table, whose rows are the groups of rows / groups consecutive
+    rows.  max_length and max_shared bound the lengths (None: what the table's
+    pages hold).  masks (int64 [rows, words], the sampler's bits): position
+    first_player + j of the context is player j of num_players, seen where bit
+    j is set; other positions are always seen.  scale:
+    None for 1 / sqrt(head dim).  Returns out, or (out, lse) with the log of
+    the sum of exponentials, float32 [rows, heads]; a row that sees nothing
+    has out 0 and lse -inf."""
+    dtype, dev, dim = cache.dtype, cache.device, cache.head_dim
+    qp = _heads(q, "q", None, dim, dtype, dev)
+    rows, heads = q.shape[0], q.shape[1]
+    out = torch.empty((rows, heads, dim), dtype=dtype, device=dev) if out is None else out
+    op = _heads(out, "out", heads, dim, dtype, dev)
+    _need(out.shape[0] == rows, f"out of {out.shape[0]} rows for {rows}")
+    lse = torch.empty((rows, heads), dtype=torch.float32, device=dev) if return_lse else None
+    width = shared_width = per = 0
+    if table is not None:
+        _need(table.dim() == 2 and table.shape[0] == rows and lengths is not None, "table: [rows, pages], with lengths")
+        width = table.shape[1]
+        max_length = width * cache.page_size if max_length is None else max_length
+    if shared_table is not None:
+        _need(shared_table.dim() == 2 and shared_lengths is not None, "shared_table: [groups, pages], with lengths")
+        groups, shared_width = shared_table.shape
+        _need(groups > 0 and rows % groups == 0, f"{groups} groups of {rows} rows")
+        per = rows // groups
+        max_shared = shared_width * cache.page_size if max_shared is None else max_shared
+    words = 0
+    if masks is not None:
+        _need(num_players is not None, "masks without num_players")
+        words = masks.shape[-1]
+    else:
+        _need(not num_players, "players without masks")
+        num_players = first_player = 0
+    a = L.gnnshap_queries(
+        rows, heads, 0, *qp, *op, _ptr(lse), _vector(table, "table", torch.int32, None, dev),
+        _vector(lengths, "lengths", torch.int32, (rows,), dev), width, max_length or 0,
+        _vector(shared_table, "shared_table", torch.int32, None, dev),
+        _vector(shared_lengths, "shared_lengths", torch.int32, None if per == 0 else (rows // per,), dev), shared_width,
+        max_shared or 0, max(per, 1) if shared_table is not None else 0,
+        _vector(masks, "masks", torch.int64, (rows, words), dev), words, num_players, first_player,
+        1.0 / math.sqrt(dim) if scale is None else scale)
+    with torch.cuda.device(dev):
+        nbytes = L.gnnshap_cache_attend_workspace(cache._c, a)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+        L.gnnshap_cache_attend(cache._c, a, _vector(info, "info", torch.int32, (1,), dev), _ptr(ws), nbytes,
+                               _stream(dev))
+    return (out, lse) if return_lse else out
+
+
+class TokenLogprobs(NamedTuple):
+    logprob: torch.Tensor       # float32 [rows]: log probability of the given token
+    entropy: torch.Tensor       # float32 [rows]
+    lse: torch.Tensor           # float32 [rows]: log of the sum of exponentials
+    rank: torch.Tensor          # int32 [rows]: logits larger than the given token's
+    top_logprob: torch.Tensor   # float32 [rows, top], falling
+    top_id: torch.Tensor        # int32 [rows, top]
+
+
+def _logits(x, targets, top, **outputs):
+    _need(x.dim() == 2 and x.is_cuda and x.dtype in _DTYPES and (x.stride(1) == 1 or x.shape[1] < 2),
+          f"logits: a [rows, vocabulary] float32, float16 or bfloat16 tensor on a GPU with a contiguous last axis is "
+          f"needed, got {x.dtype} {tuple(x.shape)} with strides {x.stride()} on {x.device}")
+    rows = x.shape[0]
+    return L.gnnshap_logits(dtype=_DTYPES[x.dtype], top=top, num_rows=rows, vocab=x.shape[1], logits=x.data_ptr(),
+                            row_stride=x.stride(0),
+                            targets=_vector(targets, "targets", torch.int64, (rows,), x.device), **outputs)
+
+
+def token_logprobs(logits, targets=None, top=0, info=None):
+    """gnnshap_token_logprobs of logits [rows, vocabulary]: log probability and
+    rank of the tokens `targets` (int64 [rows]; negative or None: no token, 0
+    and -1), entropy, and the `top` most likely tokens (at most 64; of equal
+    logits the lowest token first).  Returns a TokenLogprobs."""
+    rows, dev = logits.shape[0], logits.device
+    f = torch.empty((3, rows), dtype=torch.float32, device=dev)
+    r = TokenLogprobs(f[0], f[1], f[2], torch.empty(rows, dtype=torch.int32, device=dev),
+                      torch.empty((rows, top), dtype=torch.float32, device=dev),
+                      torch.empty((rows, top), dtype=torch.int32, device=dev))
+    a = _logits(logits, targets, top, logprob=r.logprob.data_ptr(), entropy=r.entropy.data_ptr(),
+                lse=r.lse.data_ptr(), rank=r.rank.data_ptr(), top_logprob=r.top_logprob.data_ptr(),
+                top_id=r.top_id.data_ptr())
+    with torch.cuda.device(dev):
+        nbytes = L.gnnshap_token_logprobs_workspace(a)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+        L.gnnshap_token_logprobs(a, _vector(info, "info", torch.int32, (1,), dev), _ptr(ws), nbytes, _stream(dev))
+    return r
+
+
+def token_logprobs_backward(logits, targets, lse, entropy=None, grad_logprob=None, grad_entropy=None, out=None,
+                            info=None):
+    """gnnshap_token_logprobs_backward: the gradient by the logits of
+    sum(grad_logprob * logprob) + sum(grad_entropy * entropy), in the logits'
+    type.  lse and entropy as token_logprobs gave them; out may be the logits
+    themselves."""
+    rows, dev = logits.shape[0], logits.device
+    a = _logits(logits, targets, 0, lse=_vector(lse, "lse", torch.float32, (rows,), dev),
+                entropy=_vector(entropy, "entropy", torch.float32, (rows,), dev))
+    out = torch.empty(logits.shape, dtype=logits.dtype, device=dev) if out is None else out
+    _need(out.shape == logits.shape and out.dtype == logits.dtype and out.device == dev
+          and (out.stride(1) == 1 or out.shape[1] < 2), "out: a tensor like the logits is needed")
+    with torch.cuda.device(dev):
+        L.gnnshap_token_logprobs_backward(a, _vector(grad_logprob, "grad_logprob", torch.float32, (rows,), dev),
+                                          _vector(grad_entropy, "grad_entropy", torch.float32, (rows,), dev),
+                                          out.data_ptr(), out.stride(0),
+                                          _vector(info, "info", torch.int32, (1,), dev), _stream(dev))
+    return out
