@@ -19,7 +19,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libgnnshap.so")
 
 HIP_SOURCES = ["extract.hip", "sample.hip", "eval.hip", "eval_wide.hip", "solve.hip", "cg.hip", "fidelity.hip", "gat.hip", "batch.hip", "append.hip",
-               "attend.hip", "logprob.hip", "timing.hip"]
+               "attend.hip", "attend_wide.hip", "logprob.hip", "timing.hip"]
 HOST_SOURCES = ["plan.cpp", "status.cpp"]
 ARCH = "gfx950"
 

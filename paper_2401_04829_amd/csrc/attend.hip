@@ -20,94 +20,11 @@
 // score is replaced by -inf, and 0 times a finite value is 0; where a result
 // comes out non-finite, the workgroup's queries are done again by a slow path
 // that skips the positions each row does not see.
-#include "tokens.h"
+#include "attend.h"
 
 namespace {
 
-using gnnshap::bf16_t;
-using gnnshap::f16_t;
-using gnnshap::load_pack;
-using gnnshap::Pack;
-
-typedef float f4_t __attribute__((ext_vector_type(4)));
-typedef unsigned u4_t __attribute__((ext_vector_type(4)));
-
-constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kWaves = 4;
-constexpr int kChunk = 32;  // keys of a wavefront's step
-
-// One part of the rows' contexts: `r` consecutive rows share each row of its
-// table.  A group's rows times the query heads of a kv head are its queries,
-// in tiles; a workgroup takes a tile over split_keys keys.
-struct Part {
-  const int32_t* table;
-  const int32_t* lengths;
-  int64_t width;
-  int max_len;
-  int r;
-  int tiles;
-  int splits;
-  int split_keys;
-  int slot0;  // first of the part's slots of partial results
-};
-
-struct AttendArgs {
-  gnnshap_cache c;
-  gnnshap_queries q;
-  int share;       // query heads per kv head
-  int page_shift;  // log2 of the page size, or -1
-  float scale2;    // scale log2 e
-  Part shared, own;
-  bool direct;     // one part of one split: results go straight to the caller
-  float* part_o;   // [slot][row][head][head_dim], not divided by l
-  float2* part_ml; // [slot][row][head]: m, l
-  int32_t* info;
-};
-
-__device__ __forceinline__ int page_of(const AttendArgs& a, int key, int& slot) {
-  if (a.page_shift >= 0) {
-    slot = key & ((1 << a.page_shift) - 1);
-    return key >> a.page_shift;
-  }
-  const int p = key / a.c.page_size;
-  slot = key - p * a.c.page_size;
-  return p;
-}
-
-// The length of sequence `g` of a part, at most what its arrays hold.
-__device__ __forceinline__ int length_of(const AttendArgs& a, const Part& part, int64_t g) {
-  const int n = part.lengths[g];
-  if (n < 0 || n > part.max_len) {
-    if (a.info) *a.info = 1;
-    return n < 0 ? 0 : part.max_len;
-  }
-  return n;
-}
-
-// Which of the positions at .. at + 31 a row sees; `at` counts from the first player.
-__device__ __forceinline__ uint32_t seen(const uint64_t* row, int64_t at, int64_t players) {
-  if (at + 32 <= 0 || at >= players) return ~0u;
-  const uint32_t* w = reinterpret_cast<const uint32_t*>(row);
-  const int64_t words = (players + 31) >> 5, i = at >> 5;
-  const int sh = static_cast<int>(at & 31);
-  const uint32_t lo = i >= 0 ? w[i] : 0u, hi = sh && i + 1 < words ? w[i + 1] : 0u;
-  uint32_t bits = sh ? (lo >> sh) | (hi << (32 - sh)) : lo;
-  if (at < 0) bits |= (1u << -at) - 1u;
-  if (at + 32 > players) bits |= ~0u << (players - at);
-  return bits;
-}
-
-// Where a query's results go.
-__device__ __forceinline__ int64_t part_index(const AttendArgs& a, int slot, int64_t row, int head) {
-  return (static_cast<int64_t>(slot) * a.q.num_rows + row) * a.q.heads + head;
-}
-
-template <class T>
-__device__ __forceinline__ T* out_of(const AttendArgs& a, int64_t row, int head) {
-  return static_cast<T*>(a.q.out) + row * a.q.out_row_stride + head * a.q.out_head_stride;
-}
-
-__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : m * kLn2 + logf(l); }
+using namespace gnnshap;
 
 // The matrix instructions and operand layouts of an element type.  DP: the
 // head_dim rounded up; kOwn: consecutive elements of a value row that a lane
@@ -217,258 +134,234 @@ struct Ops<float, DP> {
   }
 };
 
-struct Place {  // what a workgroup works on
-  int64_t group;
-  int kv_head, tile, split;
-  int64_t first;  // context position of the part's position 0, counted from the first player
-  int k0, k1;     // keys of the split
+// One query tile's state: running maximum, sum (this lane's part) and O^T.
+template <class T, int DP>
+struct State {
+  using O = Ops<T, DP>;
+  float m = -INFINITY, l = 0.f;
+  f4_t o[O::kGroups][O::kOwn];
+  __device__ __forceinline__ State() {
+#pragma unroll
+    for (int i = 0; i < O::kGroups; ++i)
+#pragma unroll
+      for (int e = 0; e < O::kOwn; ++e) o[i][e] = f4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  // 32 keys, of which the lane's query sees those whose bit is set.
+  __device__ __forceinline__ void step(const typename O::Row (&key)[2], const typename O::Values& val,
+                                       const typename O::Row& q, uint32_t bits, float scale2) {
+    bits >>= 4 * ((threadIdx.x >> 4) & 3);
+    float s[8], top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const f4_t c = O::scores(key[i], q);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[4 * i + e] = bits >> (16 * i + e) & 1u ? c[e] * scale2 : -INFINITY;
+        top = fmaxf(top, s[4 * i + e]);
+      }
+    }
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    top = fmaxf(top, m);
+    const float use = top == -INFINITY ? 0.f : top, down = __builtin_amdgcn_exp2f(m - use);
+    m = top;
+    l *= down;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      s[j] = __builtin_amdgcn_exp2f(s[j] - use);
+      l += s[j];
+    }
+#pragma unroll
+    for (int i = 0; i < O::kGroups; ++i)
+#pragma unroll
+      for (int e = 0; e < O::kOwn; ++e) o[i][e] *= down;
+    O::add(o, val, s);
+  }
 };
 
-// The slow path: queries one after the other, a thread per key and then per
-// element; a position that the row does not see enters no product.
-template <class T>
-__device__ void attend_slowly(const AttendArgs& a, const Part& part, Place at, int queries, const int* pages,
-                                           float* lds) {
-  const int tid = threadIdx.x, D = a.c.head_dim, wave = tid >> 6, lane = tid & 63;
-  float* weight = lds;       // 256
-  float* red = lds + 256;    // 2 x kWaves
-  const int page0 = at.k0 / a.c.page_size;
-  const int64_t head_at = static_cast<int64_t>(at.kv_head) * a.c.head_stride;
-  for (int i = 0; i < queries; ++i) {
-    const int qi = at.tile * queries + i;
-    if (qi >= part.r * a.share) break;
-    const int64_t row = at.group * part.r + qi / a.share;
-    const int head = at.kv_head * a.share + qi % a.share;
-    const T* q = static_cast<const T*>(a.q.q) + row * a.q.q_row_stride + head * a.q.q_head_stride;
-    float m = -INFINITY, l = 0.f, o = 0.f;
-    for (int c = at.k0; c < at.k1; c += 256) {
-      const int key = c + tid;
-      bool sees = key < at.k1;
-      if (sees && a.q.num_players > 0)
-        sees = seen(a.q.masks + row * a.q.mask_words, at.first + key, a.q.num_players) & 1u;
-      float s = -INFINITY;
-      if (sees) {
-        int slot;
-        const int pg = page_of(a, key, slot);
-        const T* k = static_cast<const T*>(a.c.k) + pages[pg - page0] * a.c.page_stride + slot * a.c.slot_stride + head_at;
-        s = 0.f;
-        for (int d = 0; d < D; ++d) s += static_cast<float>(q[d]) * static_cast<float>(k[d]);
-        s *= a.scale2;
-      }
-      float top = s;
-      for (int off = 1; off < 64; off *= 2) top = fmaxf(top, __shfl_xor(top, off));
-      if (lane == 0) red[wave] = top;
-      __syncthreads();
-      top = m;
-      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, red[w]);
-      const float use = top == -INFINITY ? 0.f : top;
-      const float p = sees ? __builtin_amdgcn_exp2f(s - use) : -1.f;
-      weight[tid] = p;
-      float sum = sees ? p : 0.f;
-      for (int off = 1; off < 64; off *= 2) sum += __shfl_xor(sum, off);
-      if (lane == 0) red[kWaves + wave] = sum;
-      __syncthreads();
-      const float down = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - use);
-      l *= down;
-      for (int w = 0; w < kWaves; ++w) l += red[kWaves + w];
-      m = top;
-      if (tid < D) {
-        o = m == -INFINITY ? 0.f : o * down;
-        const int n = at.k1 - c < 256 ? at.k1 - c : 256;
-        for (int j = 0; j < n; ++j) {
-          const float pj = weight[j];
-          if (pj < 0.f) continue;
-          int slot;
-          const int pg = page_of(a, c + j, slot);
-          o += pj * static_cast<float>(static_cast<const T*>(a.c.v)[pages[pg - page0] * a.c.page_stride +
-                                                                    slot * a.c.slot_stride + head_at + tid]);
-        }
-      }
-      __syncthreads();
-    }
-    if (l == 0.f) o = 0.f;
-    if (a.direct) {
-      if (tid < D) out_of<T>(a, row, head)[tid] = static_cast<T>(l == 0.f ? 0.f : o / l);
-      if (tid == 0 && a.q.lse) a.q.lse[row * a.q.heads + head] = lse_of(m, l);
-    } else {
-      const int64_t p = part_index(a, part.slot0 + at.split, row, head);
-      if (tid < D) a.part_o[p * D + tid] = o;
-      if (tid == 0) a.part_ml[p] = make_float2(m, l);
-    }
-  }
-}
+enum { kOwnPart, kShared, kSharedByQuery };
 
-// A workgroup: 16 RT queries over one split of keys.  Its four wavefronts
-// take the split's chunks of 32 keys in turn and are joined through LDS.
-template <class T, int DP, int RT>
-__global__ __launch_bounds__(64 * kWaves) void k_cache_attend(AttendArgs a, Part part, bool is_own) {
+// A workgroup: one split of keys against RT tiles of 16 queries, its four
+// wavefronts taking chunks of 32 keys in turn and joined through LDS
+// (kSharedByQuery: against RT tiles of each wavefront, every wavefront taking all
+// chunks, nothing to join).
+template <class T, int DP, int RT, int MODE>
+__global__ __launch_bounds__(64 * kWaves) void k_cache_attend(AttendArgs a, Part part) {
   using O = Ops<T, DP>;
-  constexpr int kStride = DP + 4;
+  constexpr bool BY_QUERY = MODE == kSharedByQuery, IS_OWN = MODE == kOwnPart;
+  constexpr int kStride = DP + 4, kQueries = 16 * RT * (BY_QUERY ? kWaves : 1);
   extern __shared__ int lds[];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, r = lane & 15, g = lane >> 4;
   const int D = a.c.head_dim;
-  Place at;
-  int64_t b = blockIdx.x;
-  at.kv_head = b % a.c.kv_heads;
-  b /= a.c.kv_heads;
-  at.split = b % part.splits;
-  b /= part.splits;
-  at.tile = b % part.tiles;
-  at.group = b / part.tiles;
-  const int len = length_of(a, part, at.group);
-  at.k0 = at.split * part.split_keys;
-  at.k1 = len - at.k0 < part.split_keys ? len : at.k0 + part.split_keys;
-  if (at.k0 >= at.k1) {
-    if (!a.direct) return;
-    at.k1 = at.k0;
-  }
-  at.first = -a.q.first_player;
-  if (is_own && a.shared.table) at.first += length_of(a, a.shared, at.group / a.shared.r);
-
-  // the pages of the split
+  const Place at = place_of(a, part, IS_OWN);
+  if (at.k0 >= at.k1 && !a.direct && !at.with_own) return;
   const int page0 = at.k0 / a.c.page_size;
   int* pages = lds;
-  const int n_pages = at.k1 > at.k0 ? (at.k1 - 1) / a.c.page_size - page0 + 1 : 0;
-  for (int i = tid; i < n_pages; i += 64 * kWaves) {
-    int p = part.table[at.group * part.width + page0 + i];
-    if (p < 0 || p >= a.c.num_pages) {
-      if (a.info) *a.info = 1;
-      p = 0;
-    }
-    pages[i] = p;
-  }
+  stage_pages(a, part, at, pages);
   float* merge = reinterpret_cast<float*>(lds + ((part.split_keys / a.c.page_size + 2 + 3) & ~3));
 
   typename O::Row q[RT];
   int64_t row[RT];
-  int head[RT];
-  bool valid[RT];
-  float m[RT], l[RT];
-  f4_t o[RT][O::kGroups][O::kOwn];
+  State<T, DP> st[RT];
+  const int q0 = at.tile * kQueries + (BY_QUERY ? wave * RT * 16 : 0), n_queries = part.r * a.share;
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
-    const int qi = (at.tile * RT + t) * 16 + r;
-    valid[t] = qi < part.r * a.share;
-    const int qs = valid[t] ? qi : 0;
+    const int qi = q0 + t * 16 + r, qs = qi < n_queries ? qi : 0;
     row[t] = at.group * part.r + qs / a.share;
-    head[t] = at.kv_head * a.share + qs % a.share;
-    q[t].load(static_cast<const T*>(a.q.q) + row[t] * a.q.q_row_stride + head[t] * a.q.q_head_stride, D);
-    m[t] = -INFINITY;
-    l[t] = 0.f;
-#pragma unroll
-    for (int i = 0; i < O::kGroups; ++i)
-#pragma unroll
-      for (int e = 0; e < O::kOwn; ++e) o[t][i][e] = f4_t{0.f, 0.f, 0.f, 0.f};
+    const int head = at.kv_head * a.share + qs % a.share;
+    q[t].load(static_cast<const T*>(a.q.q) + row[t] * a.q.q_row_stride + head * a.q.q_head_stride, D);
   }
   __syncthreads();
 
   const int64_t head_at = static_cast<int64_t>(at.kv_head) * a.c.head_stride;
+  const T* const kbase = static_cast<const T*>(a.c.k);
+  const T* const vbase = static_cast<const T*>(a.c.v);
   const auto offset = [&](int key) {
     key = key < at.k1 ? key : at.k1 - 1;
     int slot;
     const int pg = page_of(a, key, slot);
     return pages[pg - page0] * a.c.page_stride + slot * a.c.slot_stride + head_at;
   };
-  for (int k = at.k0 + wave * kChunk; k < at.k1; k += kWaves * kChunk) {
-    typename O::Row key[2];
-    typename O::Values val;
+  typename O::Row key[2];
+  typename O::Values val;
+  constexpr int kTurn = BY_QUERY ? kChunk : kWaves * kChunk;
+  for (int k = at.k0 + (BY_QUERY ? 0 : wave * kChunk); k < at.k1; k += kTurn) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) key[i].load(static_cast<const T*>(a.c.k) + offset(k + 16 * i + r), D);
+    for (int i = 0; i < 2; ++i) key[i].load(kbase + offset(k + 16 * i + r), D);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) val.load(j, static_cast<const T*>(a.c.v) + offset(k + 16 * (j >> 2) + 4 * g + (j & 3)), D);
+    for (int j = 0; j < 8; ++j) val.load(j, vbase + offset(k + 16 * (j >> 2) + 4 * g + (j & 3)), D);
     const uint32_t there = at.k1 - k >= 32 ? ~0u : (1u << (at.k1 - k)) - 1u;
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       uint32_t bits = there;
       if (a.q.num_players > 0) bits &= seen(a.q.masks + row[t] * a.q.mask_words, at.first + k, a.q.num_players);
-      bits >>= 4 * g;
-      float s[8], top = -INFINITY;
+      st[t].step(key, val, q[t], bits, a.scale2);
+    }
+  }
+
+  if (!IS_OWN && at.with_own) {
+    const int64_t first = length_of(a, part, at.group) - a.q.first_player;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const f4_t c = O::scores(key[i], q[t]);
+    for (int t = 0; t < RT; ++t) {
+      if (!BY_QUERY && t % kWaves != wave) continue;
+      const int len = length_of(a, a.own, row[t]);
+      const OwnTile own(a, part, at, q0 + t * 16, 16, len);
+      for (int p = 0; p < own.passes; ++p) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          s[4 * i + e] = bits >> (16 * i + e) & 1u ? c[e] * a.scale2 : -INFINITY;
-          top = fmaxf(top, s[4 * i + e]);
+        for (int i = 0; i < 2; ++i) {
+          const int64_t x = own.at(a, p, 16 * i + r, at.kv_head);
+          key[i].load(kbase + (x < 0 ? 0 : x), x < 0 ? 0 : D);
         }
-      }
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      top = fmaxf(top, m[t]);
-      const float use = top == -INFINITY ? 0.f : top, down = __builtin_amdgcn_exp2f(m[t] - use);
-      m[t] = top;
-      l[t] *= down;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        s[j] = __builtin_amdgcn_exp2f(s[j] - use);
-        l[t] += s[j];
+        for (int j = 0; j < 8; ++j) {
+          const int64_t x = own.at(a, p, 16 * (j >> 2) + 4 * g + (j & 3), at.kv_head);
+          val.load(j, vbase + (x < 0 ? 0 : x), x < 0 ? 0 : D);
+        }
+        st[t].step(key, val, q[t], own.bits(a, p, row[t], len, first), a.scale2);
       }
+    }
+  }
+
+  bool bad = false;
+  if constexpr (BY_QUERY) {
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      float l = st[t].l;
+      l += __shfl_xor(l, 16);
+      l += __shfl_xor(l, 32);
+      const int qi = q0 + t * 16 + r;
+      if (qi >= n_queries) continue;
+      const int head = at.kv_head * a.share + qi % a.share;
+      const int64_t p = part_index(a, part.slot0 + at.split, row[t], head);
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      bad |= !isfinite(l);
 #pragma unroll
       for (int i = 0; i < O::kGroups; ++i)
 #pragma unroll
-        for (int e = 0; e < O::kOwn; ++e) o[t][i][e] *= down;
-      O::add(o[t], val, s);
-    }
-  }
-
-  // join the wavefronts
-  bool bad = false;
-  float* ml = merge + kWaves * 16 * kStride;  // [wave][query]: m, then l
+        for (int x = 0; x < 4; ++x) {
+          const int d = (16 * i + 4 * g + x) * O::kOwn;
+          if (d >= D) continue;
+          Pack<T, O::kOwn> done;
+          Pack<float, O::kOwn> part_done;
 #pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    l[t] += __shfl_xor(l[t], 16);
-    l[t] += __shfl_xor(l[t], 32);
-    if (t > 0) __syncthreads();
-    float* mine = merge + (wave * 16 + r) * kStride;
-#pragma unroll
-    for (int i = 0; i < O::kGroups; ++i)
-#pragma unroll
-      for (int x = 0; x < 4; ++x)
-#pragma unroll
-        for (int e = 0; e < O::kOwn; ++e) mine[(16 * i + 4 * g + x) * O::kOwn + e] = o[t][i][e][x];
-    if (g == 0) {
-      ml[wave * 16 + r] = m[t];
-      ml[kWaves * 16 + wave * 16 + r] = l[t];
-    }
-    __syncthreads();
-    const int qi = (at.tile * RT + t) * 16 + (tid >> 4), d0 = (tid & 15) * (DP / 16);
-    if (qi < part.r * a.share) {
-      float top = -INFINITY, sum = 0.f, f[kWaves];
-      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[w * 16 + (tid >> 4)]);
-      const float use = top == -INFINITY ? 0.f : top;
-      for (int w = 0; w < kWaves; ++w) {
-        f[w] = __builtin_amdgcn_exp2f(ml[w * 16 + (tid >> 4)] - use);
-        sum += f[w] * ml[kWaves * 16 + w * 16 + (tid >> 4)];
-      }
-      const int64_t row_t = at.group * part.r + qi / a.share;
-      const int head_t = at.kv_head * a.share + qi % a.share;
-      const int64_t p = part_index(a, part.slot0 + at.split, row_t, head_t);
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      bad |= !isfinite(sum);
-#pragma unroll
-      for (int e = 0; e < DP / 16; ++e) {
-        const int d = d0 + e;
-        float x = 0.f;
-        for (int w = 0; w < kWaves; ++w) x += f[w] * merge[(w * 16 + (tid >> 4)) * kStride + d];
-        if (d >= D) continue;
-        bad |= !isfinite(x);
-        if (a.direct)
-          out_of<T>(a, row_t, head_t)[d] = static_cast<T>(x * inv);
-        else
-          a.part_o[p * D + d] = x;
-      }
-      if ((tid & 15) == 0) {
+          for (int e = 0; e < O::kOwn; ++e) {
+            bad |= !isfinite(st[t].o[i][e][x]);
+            done.v[e] = static_cast<T>(st[t].o[i][e][x] * inv);
+            part_done.v[e] = st[t].o[i][e][x];
+          }
+          if (a.direct)
+            store_pack(out_of<T>(a, row[t], head) + d, done);
+          else
+            store_pack(a.part_o + p * D + d, part_done);
+        }
+      if (g == 0) {
         if (!a.direct)
-          a.part_ml[p] = make_float2(top, sum);
+          a.part_ml[p] = make_float2(st[t].m, l);
         else if (a.q.lse)
-          a.q.lse[row_t * a.q.heads + head_t] = lse_of(top, sum);
+          a.q.lse[row[t] * a.q.heads + head] = lse_of(st[t].m, l);
+      }
+    }
+  } else {
+    // join the wavefronts
+    float* ml = merge + kWaves * 16 * kStride;  // [wave][query]: m, then l
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      float l = st[t].l;
+      l += __shfl_xor(l, 16);
+      l += __shfl_xor(l, 32);
+      if (t > 0) __syncthreads();
+      float* mine = merge + (wave * 16 + r) * kStride;
+#pragma unroll
+      for (int i = 0; i < O::kGroups; ++i)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+          for (int e = 0; e < O::kOwn; ++e) mine[(16 * i + 4 * g + x) * O::kOwn + e] = st[t].o[i][e][x];
+      if (g == 0) {
+        ml[wave * 16 + r] = st[t].m;
+        ml[kWaves * 16 + wave * 16 + r] = l;
+      }
+      __syncthreads();
+      const int ql = tid >> 4, qi = q0 + t * 16 + ql, d0 = (tid & 15) * (DP / 16);
+      if (qi < n_queries) {
+        float top = -INFINITY, sum = 0.f, f[kWaves];
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[w * 16 + ql]);
+        const float use = top == -INFINITY ? 0.f : top;
+        for (int w = 0; w < kWaves; ++w) {
+          f[w] = __builtin_amdgcn_exp2f(ml[w * 16 + ql] - use);
+          sum += f[w] * ml[kWaves * 16 + w * 16 + ql];
+        }
+        const int64_t row_t = at.group * part.r + qi / a.share;
+        const int head = at.kv_head * a.share + qi % a.share;
+        const int64_t p = part_index(a, part.slot0 + at.split, row_t, head);
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        bad |= !isfinite(sum);
+#pragma unroll
+        for (int e = 0; e < DP / 16; ++e) {
+          const int d = d0 + e;
+          float x = 0.f;
+          for (int w = 0; w < kWaves; ++w) x += f[w] * merge[(w * 16 + ql) * kStride + d];
+          if (d >= D) continue;
+          bad |= !isfinite(x);
+          if (a.direct)
+            out_of<T>(a, row_t, head)[d] = static_cast<T>(x * inv);
+          else
+            a.part_o[p * D + d] = x;
+        }
+        if ((tid & 15) == 0) {
+          if (!a.direct)
+            a.part_ml[p] = make_float2(top, sum);
+          else if (a.q.lse)
+            a.q.lse[row_t * a.q.heads + head] = lse_of(top, sum);
+        }
       }
     }
   }
-  if (__syncthreads_or(bad)) attend_slowly<T>(a, part, at, 16 * RT, pages, merge);
+  if (__syncthreads_or(bad)) attend_slowly<T>(a, part, at, kQueries, merge);
 }
 
-// Joins the parts of each query, a wavefront per row and head.
+// Joins the parts of each query, a wavefront per row and head: the lanes weigh
+// 64 parts at a time, then add up the parts' elements, eight loads in flight.
 template <class T>
 __global__ __launch_bounds__(256) void k_cache_attend_join(AttendArgs a) {
   const int lane = threadIdx.x & 63, D = a.c.head_dim;
@@ -478,25 +371,49 @@ __global__ __launch_bounds__(256) void k_cache_attend_join(AttendArgs a) {
   const int head = static_cast<int>(i % a.q.heads);
   int ns = 0, no = 0;
   if (a.shared.table) ns = (length_of(a, a.shared, row / a.shared.r) + a.shared.split_keys - 1) / a.shared.split_keys;
-  if (a.own.table) no = (length_of(a, a.own, row) + a.own.split_keys - 1) / a.own.split_keys;
+  if (a.fused) ns = max(ns, 1);
+  if (a.own.table && !a.fused) no = (length_of(a, a.own, row) + a.own.split_keys - 1) / a.own.split_keys;
+  const auto slot_of = [&](int n) { return n < ns ? a.shared.slot0 + n : a.own.slot0 + n - ns; };
   float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int n = 0; n < ns + no; ++n) {
-    const int slot = n < ns ? a.shared.slot0 + n : a.own.slot0 + n - ns;
-    const int64_t p = part_index(a, slot, row, head);
-    const float2 ml = a.part_ml[p];
-    if (ml.y == 0.f) continue;
-    const float top = fmaxf(m, ml.x), use = top == -INFINITY ? 0.f : top;
-    const float down = __builtin_amdgcn_exp2f(m - use), up = __builtin_amdgcn_exp2f(ml.x - use);
-    m = top;
-    l = l * down + ml.y * up;
+  for (int n0 = 0; n0 < ns + no; n0 += 64) {
+    const int n = min(64, ns + no - n0);
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (lane < n) ml = a.part_ml[part_index(a, slot_of(n0 + lane), row, head)];
+    float top = fmaxf(m, ml.x);
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (4 * lane + e < D) o[e] = o[e] * down + a.part_o[p * D + 4 * lane + e] * up;
+    for (int off = 1; off < 64; off *= 2) top = fmaxf(top, __shfl_xor(top, off));
+    const float use = top == -INFINITY ? 0.f : top, down = __builtin_amdgcn_exp2f(m - use);
+    const float up = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - use);
+    float sum = ml.y == 0.f ? 0.f : ml.y * up;
+#pragma unroll
+    for (int off = 1; off < 64; off *= 2) sum += __shfl_xor(sum, off);
+    m = top;
+    l = l * down + sum;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] *= down;
+    if (4 * lane < D) {
+      for (int j0 = 0; j0 < n; j0 += 8) {
+        Pack<float, 4> x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          x[j] = load_pack<float, 4>(a.part_o + part_index(a, slot_of(n0 + min(j0 + j, n - 1)), row, head) * D + 4 * lane);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float w = j0 + j < n ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(up), j0 + j)) : 0.f;
+          if (w != 0.f)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += x[j].v[e] * w;
+        }
+      }
+    }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
+  if (4 * lane < D) {
+    Pack<T, 4> done;
 #pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (4 * lane + e < D) out_of<T>(a, row, head)[4 * lane + e] = static_cast<T>(o[e] * inv);
+    for (int e = 0; e < 4; ++e) done.v[e] = static_cast<T>(o[e] * inv);
+    store_pack(out_of<T>(a, row, head) + 4 * lane, done);
+  }
   if (lane == 0 && a.q.lse) a.q.lse[row * a.q.heads + head] = lse_of(m, l);
 }
 
@@ -556,6 +473,8 @@ int lay_out(AttendArgs& a, const gnnshap_cache* c, const gnnshap_queries* q) {
   a.page_shift = -1;
   for (int i = 0; i < 31; ++i)
     if (c->page_size == 1 << i) a.page_shift = i;
+  // own parts of few tokens ride along with the shared part
+  a.fused = q->shared_table && q->table && q->max_length <= 64;
   Part* parts[2] = {&a.shared, &a.own};
   int slots = 0;
   for (int i = 0; i < 2; ++i) {
@@ -567,13 +486,18 @@ int lay_out(AttendArgs& a, const gnnshap_cache* c, const gnnshap_queries* q) {
     p.width = i ? q->table_width : q->shared_width;
     p.max_len = static_cast<int>(i ? q->max_length : q->max_shared);
     p.r = static_cast<int>(i ? 1 : q->rows_per_group);
+    if (i && a.fused) continue;
     const int64_t queries = static_cast<int64_t>(p.r) * a.share;
-    if (queries > INT32_MAX) return gnnshap::fail(GNNSHAP_EUNSUPPORTED, "%lld queries of a group", static_cast<long long>(queries));
-    p.tiles = static_cast<int>(ceil_div(queries, 16 * tile_of(queries, c->head_dim)));
+    if (queries > INT32_MAX - 1024)
+      return gnnshap::fail(GNNSHAP_EUNSUPPORTED, "%lld queries of a group", static_cast<long long>(queries));
+    p.wide = !i && queries >= 64 && c->dtype != GNNSHAP_F32;
+    p.by_query = !i && queries >= 64 && !p.wide;
+    p.tile = p.wide ? 128 : p.by_query ? 64 : 16 * tile_of(queries, c->head_dim);
+    p.tiles = static_cast<int>(ceil_div(queries, p.tile));
     // enough workgroups for the chip, at least 256 keys each, at most 4096
     const int64_t base = q->num_rows / p.r * c->kv_heads * p.tiles;
     int64_t keys = ceil_div(std::max(p.max_len, 1), std::max<int64_t>(1, 1024 / std::max<int64_t>(base, 1)));
-    keys = std::min<int64_t>(std::max<int64_t>(ceil_div(keys, 128) * 128, 256), i ? 1024 : 4096);
+    keys = std::min<int64_t>(std::max<int64_t>(ceil_div(keys, 128) * 128, 256), i ? 512 : 4096);
     p.split_keys = static_cast<int>(keys);
     p.splits = static_cast<int>(std::max<int64_t>(1, ceil_div(p.max_len, keys)));
     p.slot0 = slots;
@@ -593,36 +517,41 @@ size_t carve(AttendArgs& a, void* ws) {
   return c.bytes();
 }
 
-template <class T, int DP, int RT>
-int launch_part(const AttendArgs& a, const Part& p, bool is_own, hipStream_t s) {
+template <class T, int DP, int RT, int MODE>
+int launch_part(const AttendArgs& a, const Part& p, hipStream_t s) {
   const int pages = p.split_keys / a.c.page_size + 2;
   const size_t bytes = sizeof(int) * ((pages + 3) & ~3) + sizeof(float) * (kWaves * 16 * (DP + 4) + 2 * kWaves * 16);
   const unsigned grid = static_cast<unsigned>(a.q.num_rows / p.r * a.c.kv_heads * p.tiles * p.splits);
   if (bytes > 65536)
-    GS_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&k_cache_attend<T, DP, RT>),
+    GS_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&k_cache_attend<T, DP, RT, MODE>),
                                hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)));
   {
     GS_TIMED("k_cache_attend", s);
-    k_cache_attend<T, DP, RT><<<grid, 64 * kWaves, bytes, s>>>(a, p, is_own);
+    k_cache_attend<T, DP, RT, MODE><<<grid, 64 * kWaves, bytes, s>>>(a, p);
   }
   GS_LAUNCHED();
   return GNNSHAP_OK;
 }
 
+template <class T, int DP, int MODE>
+int launch_tiles(const AttendArgs& a, const Part& p, hipStream_t s) {
+  if (p.tile == 16) return launch_part<T, DP, 1, MODE>(a, p, s);
+  if constexpr (DP <= 128)
+    if (p.tile == 32) return launch_part<T, DP, 2, MODE>(a, p, s);
+  if constexpr (DP <= 64)
+    if (p.tile == 64) return launch_part<T, DP, 4, MODE>(a, p, s);
+  return fail(GNNSHAP_EHIP, "no kernel for tiles of %d", p.tile);
+}
+
 template <class T, int DP>
 int launch_all(const AttendArgs& a, hipStream_t s) {
-  for (int i = 0; i < 2; ++i) {
-    const Part& p = i ? a.own : a.shared;
-    if (!p.table) continue;
-    const int tiles = tile_of(static_cast<int64_t>(p.r) * a.share, a.c.head_dim);
-    int st = GNNSHAP_OK;
-    if constexpr (DP <= 64)
-      if (tiles == 4) st = launch_part<T, DP, 4>(a, p, i, s);
-    if constexpr (DP <= 128)
-      if (tiles == 2) st = launch_part<T, DP, 2>(a, p, i, s);
-    if (tiles == 1) st = launch_part<T, DP, 1>(a, p, i, s);
-    if (st) return st;
-  }
+  int st = GNNSHAP_OK;
+  if (a.shared.table)
+    st = a.shared.wide ? launch_attend_wide(a, s)
+         : a.shared.by_query ? launch_part<T, DP, 1, kSharedByQuery>(a, a.shared, s)
+                             : launch_tiles<T, DP, kShared>(a, a.shared, s);
+  if (!st && a.own.table && !a.fused) st = launch_tiles<T, DP, kOwnPart>(a, a.own, s);
+  if (st) return st;
   if (!a.direct || (!a.shared.table && !a.own.table)) {
     GS_TIMED("k_cache_attend_join", s);
     k_cache_attend_join<T><<<static_cast<unsigned>(gnnshap::ceil_div(a.q.num_rows * a.q.heads, 4)), 256, 0, s>>>(a);

@@ -1,0 +1,351 @@
+// Attention over the shared part for many 16-bit queries of a group: every
+// coalition's new token, times the query heads of a kv head, against the same
+// keys.
+//
+// It is a matrix product with a softmax inside, bound by the matrix
+// instructions and, beside them, by the exponentials (one per query and key).
+// A workgroup takes 128 queries, a wavefront 32 of them, over all keys of a
+// split in tiles of 64, staged in LDS twice: while a tile is multiplied, the
+// next one is on its way from the cache to registers.
+//
+// The layout is the transposed one of the other kernels on 32 x 32 x 16
+// instructions: S^T = K Q^T leaves query = lane % 32 and keys in registers,
+// register i of a lane in the upper half (h = 1) or lower half key
+// 8 (i / 4) + 4 h + i % 4; eight registers on end are the right operand of
+// 16 keys of O^T = V^T P^T.  Values are turned over on the way to LDS: row d
+// holds the elements d of the 64 keys, in the order of those registers.  Row
+// r of the product's tile t is element NT r + t of the NT tiles, so that a
+// lane's results (and the values that it reads for own tokens) are NT
+// elements on end.  LDS rows are whole multiples of 128 bytes, their 16-byte
+// pieces swapped by the row's number, so that neither side meets itself in a
+// bank.
+#include "attend.h"
+
+namespace {
+
+using namespace gnnshap;
+
+typedef float f16v_t __attribute__((ext_vector_type(16)));
+typedef unsigned u2_t __attribute__((ext_vector_type(2)));
+
+constexpr int kTile = 64;      // keys of a step
+constexpr int kQueries = 128;  // queries of a workgroup
+
+template <class T, int DP>
+struct Wide {
+  typedef T vec8 __attribute__((ext_vector_type(8)));
+  static constexpr int NT = DP / 32;          // tiles of O^T, elements on end of a lane
+  static constexpr int KS = DP / 16;          // steps of K Q^T
+  static constexpr int kPieces = DP / 8;      // 16-byte pieces of a key's row
+  static constexpr int kKeyLoads = kPieces / 4;         // of a thread, per tile
+  static constexpr int kValElems = DP >= 128 ? 8 : 4;   // elements on end that a thread turns over, of four keys
+  static constexpr int kValPieces = DP / kValElems;
+  static constexpr int kValLoads = kTile / 4 * kValPieces / 256;  // times four keys
+  static constexpr int kKeyBytes = kTile * DP * 2, kBufBytes = 2 * kKeyBytes;
+
+  static __device__ __forceinline__ f16v_t mfma(u4_t a, u4_t b, f16v_t c) {
+    if constexpr (std::is_same_v<T, bf16_t>)
+      return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(vec8, a), __builtin_bit_cast(vec8, b), c, 0, 0, 0);
+    else
+      return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(vec8, a), __builtin_bit_cast(vec8, b), c, 0, 0, 0);
+  }
+  // Byte of piece p of key row r, and of 16-byte piece p of the values' row d.
+  static __device__ __forceinline__ int key_at(int r, int p) { return r * DP * 2 + ((p ^ (r & 7)) << 4); }
+  static __device__ __forceinline__ int val_at(int d, int p) {
+    return kKeyBytes + d * kTile * 2 + ((p ^ (((d / NT) ^ (d / (8 * NT))) & 7)) << 4);
+  }
+  // 8-byte place of the four keys 4 c on in a values' row: the order of the weights' registers.
+  static __device__ __forceinline__ int quad_place(int c) {
+    const int in = c & 7;  // of 32 keys
+    return (c >> 3) * 8 + (in >> 2) * 4 + (in & 1) * 2 + ((in >> 1) & 1);
+  }
+
+  u4_t key[kKeyLoads];
+  unsigned val[kValLoads][4][kValElems / 2];
+
+  // A tile's keys k .. k + 63 (those behind k1 as the last one) on their way to registers.
+  template <class Offset>
+  __device__ __forceinline__ void load(const AttendArgs& a, Offset offset, int k, int k1) {
+    const int tid = threadIdx.x, D = a.c.head_dim;
+#pragma unroll
+    for (int i = 0; i < kKeyLoads; ++i) {
+      const int r = tid / kPieces + i * (256 / kPieces), p = tid % kPieces;
+      key[i] = u4_t{0u, 0u, 0u, 0u};
+      if (8 * p < D) __builtin_memcpy(&key[i], static_cast<const T*>(a.c.k) + offset(min(k + r, k1 - 1)) + 8 * p, 16);
+    }
+#pragma unroll
+    for (int i = 0; i < kValLoads; ++i) {
+      const int c = tid / kValPieces + i * (256 / kValPieces), d = tid % kValPieces * kValElems;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+#pragma unroll
+        for (int e = 0; e < kValElems / 2; ++e) val[i][j][e] = 0u;
+        if (d < D)
+          __builtin_memcpy(&val[i][j][0], static_cast<const T*>(a.c.v) + offset(min(k + 4 * c + j, k1 - 1)) + d, 2 * kValElems);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(char* buf) const {
+    const int tid = threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < kKeyLoads; ++i) {
+      const int r = tid / kPieces + i * (256 / kPieces), p = tid % kPieces;
+      *reinterpret_cast<u4_t*>(buf + key_at(r, p)) = key[i];
+    }
+#pragma unroll
+    for (int i = 0; i < kValLoads; ++i) {
+      const int c = tid / kValPieces + i * (256 / kValPieces), d = tid % kValPieces * kValElems, at = quad_place(c);
+#pragma unroll
+      for (int e = 0; e < kValElems; ++e) {
+        const unsigned sel = e & 1 ? 0x07060302u : 0x05040100u;
+        const u2_t x = {__builtin_amdgcn_perm(val[i][1][e / 2], val[i][0][e / 2], sel),
+                        __builtin_amdgcn_perm(val[i][3][e / 2], val[i][2][e / 2], sel)};
+        *reinterpret_cast<u2_t*>(buf + val_at(d + e, at >> 1) + (at & 1) * 8) = x;
+      }
+    }
+  }
+};
+
+// Tiles of 32 keys: their scores (the score of an unseen key is -inf).
+template <class T, int DP>
+struct WideState {
+  using W = Wide<T, DP>;
+  float m = -INFINITY, l = 0.f;
+  f16v_t o[W::NT];
+  __device__ __forceinline__ WideState() {
+#pragma unroll
+    for (int t = 0; t < W::NT; ++t) o[t] = f16v_t{};
+  }
+  // The starting value of scores: -inf where the query does not see the key.
+  static __device__ __forceinline__ f16v_t unseen(uint32_t bits) {
+    f16v_t c;
+    const uint32_t off = ~bits >> (4 * (threadIdx.x >> 5 & 1));
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int bit = 8 * (i / 4) + i % 4;
+      c[i] = __uint_as_float(static_cast<uint32_t>(static_cast<int32_t>(off << (31 - bit)) >> 31) & 0xFF800000u);
+    }
+    return c;
+  }
+  // The weights of N tiles' scores, in place, after the running maximum has
+  // risen to theirs (or stays up to 2^8 below: O is scaled down less often).
+  template <int N>
+  __device__ __forceinline__ void weigh(f16v_t (&s)[N], float scale) {
+    float top = s[0][0];
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
+    top = fmaxf(top, __shfl_xor(top, 32)) * scale;
+    if (__ballot(top > m + 8.f)) {
+      const float up = fmaxf(top, m), use = up == -INFINITY ? 0.f : up, down = __builtin_amdgcn_exp2f(m - use);
+      m = up;
+      l *= down;
+#pragma unroll
+      for (int t = 0; t < W::NT; ++t) o[t] *= down;
+    }
+    const float use = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], scale, -use));
+        l += s[n][i];
+      }
+  }
+  // Eight of a tile's weights, rounded to the values' type: an operand of 16 keys.
+  static __device__ __forceinline__ u4_t operand(const f16v_t& s, int u) {
+    typename W::vec8 w;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = static_cast<T>(s[8 * u + j]);
+    return __builtin_bit_cast(u4_t, w);
+  }
+};
+
+template <class T, int DP>
+__global__ __launch_bounds__(64 * kWaves, DP <= 128 ? 2 : 1) void k_cache_attend_wide(AttendArgs a, Part part) {
+  using W = Wide<T, DP>;
+  extern __shared__ char room[];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, r = lane & 31, h = lane >> 5;
+  const int D = a.c.head_dim;
+  const Place at = place_of(a, part, false);
+  if (at.k0 >= at.k1 && !a.direct && !at.with_own) return;
+  int* pages = reinterpret_cast<int*>(room + 2 * W::kBufBytes);
+  const int page0 = at.k0 / a.c.page_size;
+  stage_pages(a, part, at, pages);
+
+  const int n_queries = part.r * a.share, q0 = at.tile * kQueries + wave * 32, qi = q0 + r, qs = qi < n_queries ? qi : 0;
+  const int64_t row = at.group * part.r + qs / a.share;
+  const int head = at.kv_head * a.share + qs % a.share;
+  const float scale = fabsf(a.scale2);
+  u4_t q[W::KS];
+  {
+    const T* p = static_cast<const T*>(a.q.q) + row * a.q.q_row_stride + head * a.q.q_head_stride;
+    const unsigned flip = a.scale2 < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+    for (int i = 0; i < W::KS; ++i) {
+      const int d = 16 * i + 8 * h;
+      q[i] = u4_t{0u, 0u, 0u, 0u};
+      if (d < D) __builtin_memcpy(&q[i], p + d, 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) q[i][e] ^= flip;
+    }
+  }
+  WideState<T, DP> st;
+  __syncthreads();
+
+  const int64_t head_at = static_cast<int64_t>(at.kv_head) * a.c.head_stride;
+  const auto offset = [&](int key) {
+    int slot;
+    const int pg = page_of(a, key, slot);
+    return pages[pg - page0] * a.c.page_stride + slot * a.c.slot_stride + head_at;
+  };
+  const uint64_t* mask = a.q.masks + row * a.q.mask_words;
+  const auto bits_of = [&](int k) {
+    const int left = at.k1 - k;
+    const uint32_t there = left >= 32 ? ~0u : left <= 0 ? 0u : (1u << left) - 1u;
+    return a.q.num_players > 0 && left > 0 ? there & seen(mask, at.first + k, a.q.num_players) : there;
+  };
+
+  if (at.k0 < at.k1) {
+    W next;
+    next.load(a, offset, at.k0, at.k1);
+    uint32_t bits[2] = {bits_of(at.k0), bits_of(at.k0 + 32)};
+    next.store(room);
+    __syncthreads();
+    int turn = 0;
+    for (int k = at.k0; k < at.k1; k += kTile, turn ^= 1) {
+      const char* buf = room + turn * W::kBufBytes;
+      const bool more = k + kTile < at.k1;
+      uint32_t bits_next[2] = {0u, 0u};
+      if (more) {
+        next.load(a, offset, k + kTile, at.k1);
+        bits_next[0] = bits_of(k + kTile);
+        bits_next[1] = bits_of(k + kTile + 32);
+      }
+      f16v_t s[2];
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        s[n] = __ballot(bits[n] != ~0u) ? WideState<T, DP>::unseen(bits[n]) : f16v_t{};
+#pragma unroll
+        for (int i = 0; i < W::KS; ++i)
+          s[n] = W::mfma(*reinterpret_cast<const u4_t*>(buf + W::key_at(32 * n + r, 2 * i + h)), q[i], s[n]);
+      }
+      st.weigh(s, scale);
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const u4_t p = WideState<T, DP>::operand(s[n], u);
+#pragma unroll
+          for (int t = 0; t < W::NT; ++t)
+            st.o[t] = W::mfma(*reinterpret_cast<const u4_t*>(buf + W::val_at(W::NT * r + t, 4 * n + 2 * u + h)), p, st.o[t]);
+        }
+      if (more) next.store(room + (turn ^ 1) * W::kBufBytes);
+      bits[0] = bits_next[0];
+      bits[1] = bits_next[1];
+      __syncthreads();
+    }
+  }
+
+  if (at.with_own) {
+    const int len = length_of(a, a.own, row);
+    const int64_t first = length_of(a, part, at.group) - a.q.first_player;
+    const OwnTile own(a, part, at, q0, 32, len);
+    for (int pass = 0; pass < own.passes; ++pass) {
+      const int64_t mine = own.at(a, pass, r, at.kv_head);
+      f16v_t s[1] = {WideState<T, DP>::unseen(own.bits(a, pass, row, len, first))};
+#pragma unroll
+      for (int i = 0; i < W::KS; ++i) {
+        u4_t k = {0u, 0u, 0u, 0u};
+        if (mine >= 0 && 16 * i + 8 * h < D)
+          __builtin_memcpy(&k, static_cast<const T*>(a.c.k) + mine + 16 * i + 8 * h, 16);
+        s[0] = W::mfma(k, q[i], s[0]);
+      }
+      unsigned v[2][8][W::NT / 2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int64_t x = __shfl(mine, 16 * u + 8 * (j / 4) + 4 * h + j % 4);
+#pragma unroll
+          for (int e = 0; e < W::NT / 2; ++e) v[u][j][e] = 0u;
+          const int d = W::NT * r;
+          if (x >= 0 && d < D) __builtin_memcpy(&v[u][j][0], static_cast<const T*>(a.c.v) + x + d, 2 * W::NT);
+        }
+      st.weigh(s, scale);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const u4_t p = WideState<T, DP>::operand(s[0], u);
+#pragma unroll
+        for (int t = 0; t < W::NT; ++t) {
+          u4_t x;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            x[j] = __builtin_amdgcn_perm(v[u][2 * j + 1][t / 2], v[u][2 * j][t / 2], t & 1 ? 0x07060302u : 0x05040100u);
+          st.o[t] = W::mfma(x, p, st.o[t]);
+        }
+      }
+    }
+  }
+
+  const float l = st.l + __shfl_xor(st.l, 32);
+  bool bad = false;
+  if (qi < n_queries) {
+    const int64_t p = part_index(a, part.slot0 + at.split, row, head);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    bad = !isfinite(l);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int d = W::NT * (8 * (i / 4) + 4 * h + i % 4);
+      if (d >= D) continue;
+      Pack<T, W::NT> done;
+      Pack<float, W::NT> part_done;
+#pragma unroll
+      for (int t = 0; t < W::NT; ++t) {
+        bad |= !isfinite(st.o[t][i]);
+        done.v[t] = static_cast<T>(st.o[t][i] * inv);
+        part_done.v[t] = st.o[t][i];
+      }
+      if (a.direct)
+        store_pack(out_of<T>(a, row, head) + d, done);
+      else
+        store_pack(a.part_o + p * D + d, part_done);
+    }
+    if (h == 0) {
+      if (!a.direct)
+        a.part_ml[p] = make_float2(st.m, l);
+      else if (a.q.lse)
+        a.q.lse[row * a.q.heads + head] = lse_of(st.m, l);
+    }
+  }
+  if (__syncthreads_or(bad)) attend_slowly<T>(a, part, at, kQueries, reinterpret_cast<float*>(room));
+}
+
+template <class T, int DP>
+int launch(const AttendArgs& a, hipStream_t s) {
+  const Part& p = a.shared;
+  const size_t bytes = 2 * Wide<T, DP>::kBufBytes + sizeof(int) * (p.split_keys / a.c.page_size + 2);
+  const unsigned grid = static_cast<unsigned>(a.q.num_rows / p.r * a.c.kv_heads * p.tiles * p.splits);
+  GS_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&k_cache_attend_wide<T, DP>),
+                             hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)));
+  {
+    GS_TIMED("k_cache_attend_wide", s);
+    k_cache_attend_wide<T, DP><<<grid, 64 * kWaves, bytes, s>>>(a, p);
+  }
+  GS_LAUNCHED();
+  return GNNSHAP_OK;
+}
+
+template <class T>
+int launch_type(const AttendArgs& a, hipStream_t s) {
+  if (a.c.head_dim <= 64) return launch<T, 64>(a, s);
+  if (a.c.head_dim <= 128) return launch<T, 128>(a, s);
+  return launch<T, 256>(a, s);
+}
+
+}  // namespace
+
+int gnnshap::launch_attend_wide(const AttendArgs& a, hipStream_t s) {
+  return a.c.dtype == GNNSHAP_BF16 ? launch_type<bf16_t>(a, s) : launch_type<f16_t>(a, s);
+}
