@@ -20,6 +20,9 @@ from . import _lib as L
 _DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
+_raw_stream = torch._C._cuda_getCurrentRawStream   # torch.cuda.current_stream(device).cuda_stream without its object
+
+
 def _need(ok, what):
     if not ok:
         raise ValueError(what)
@@ -29,27 +32,33 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _stream(device):
-    return torch.cuda.current_stream(device).cuda_stream
+def _on(device, call, *args):
+    """call(*args, stream) with `device` current and its current stream."""
+    index = device.index
+    if torch.cuda.current_device() == index:
+        return call(*args, _raw_stream(index))
+    with torch.cuda.device(device):
+        return call(*args, _raw_stream(index))
 
 
 def _vector(t, name, dtype, size, device):
     """The address of an optional contiguous tensor of `dtype` and `size` (None: any shape)."""
     if t is None:
         return None
-    _need(t.dtype == dtype and t.device == device and t.is_contiguous() and (size is None or tuple(t.shape) == size),
-          f"{name}: a contiguous {dtype} tensor of shape {size} on {device} is needed, got {t.dtype} {tuple(t.shape)} "
-          f"on {t.device}")
+    if t.dtype != dtype or t.device != device or not t.is_contiguous() or (size is not None and t.shape != size):
+        raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {size} on {device} is needed, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
 def _heads(t, name, heads, dim, dtype, device):
     """Checks a [rows, heads, dim] tensor whose last axis is contiguous; its address and two strides."""
-    _need(t.dim() == 3 and t.dtype == dtype and t.device == device and t.shape[2] == dim
-          and (heads is None or t.shape[1] == heads) and (t.stride(2) == 1 or t.numel() == 0),
-          f"{name}: a [rows, {heads or 'heads'}, {dim}] {dtype} tensor on {device} with a contiguous last axis is "
-          f"needed, got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
-    return t.data_ptr(), t.stride(0), t.stride(1)
+    shape, stride = t.shape, t.stride()
+    if (len(shape) != 3 or t.dtype != dtype or t.device != device or shape[2] != dim
+            or (heads is not None and shape[1] != heads) or (stride[2] != 1 and t.numel() > 0)):
+        raise ValueError(f"{name}: a [rows, {heads or 'heads'}, {dim}] {dtype} tensor on {device} with a contiguous "
+                         f"last axis is needed, got {t.dtype} {tuple(shape)} with strides {stride} on {t.device}")
+    return t.data_ptr(), stride[0], stride[1]
 
 
 class PagedCache:
@@ -91,7 +100,7 @@ def append_tokens(cache, k, v, table, index, rows=None, positions=None, q=None, 
     n = k.shape[0]
     kp = _heads(k, "k", cache.kv_heads, dim, dtype, dev)
     vp = _heads(v, "v", cache.kv_heads, dim, dtype, dev)
-    _need(v.shape[0] == n, f"{n} keys and {v.shape[0]} values")
+    _need(v.shape[0] == n, "as many values as keys are needed")
     _need(table.dim() == 2, "table: [rows, pages of a row]")
     heads, qp, op = 0, (None, 0, 0), (None, 0, 0)
     if q is not None:
@@ -99,7 +108,7 @@ def append_tokens(cache, k, v, table, index, rows=None, positions=None, q=None, 
         qp = _heads(q, "q", heads, dim, dtype, dev)
         q_out = torch.empty((n, heads, dim), dtype=dtype, device=dev) if q_out is None else q_out
         op = _heads(q_out, "q_out", heads, dim, dtype, dev)
-        _need(q.shape[0] == n and q_out.shape[0] == n, f"{q.shape[0]} queries of {n} tokens")
+        _need(q.shape[0] == n and q_out.shape[0] == n, "as many queries as keys are needed")
     angles = (0, 0)
     if cos is not None:
         _need(sin is not None and cos.dim() == 2, "cos and sin: two [positions, rot dim / 2] tensors")
@@ -109,8 +118,7 @@ def append_tokens(cache, k, v, table, index, rows=None, positions=None, q=None, 
         _vector(positions, "positions", torch.int32, (n,), dev), _vector(table, "table", torch.int32, None, dev),
         table.shape[0], table.shape[1], _vector(cos, "cos", torch.float32, angles, dev),
         _vector(sin, "sin", torch.float32, angles, dev), angles[0], 2 * angles[1], int(interleaved), heads, 0, *qp, *op)
-    with torch.cuda.device(dev):
-        L.gnnshap_cache_append(cache._c, t, _vector(info, "info", torch.int32, (1,), dev), _stream(dev))
+    _on(dev, L.gnnshap_cache_append, cache._c, t, _vector(info, "info", torch.int32, (1,), dev))
     return q_out
 
 
@@ -133,7 +141,7 @@ def attend(cache, q, table=None, lengths=None, max_length=None, shared_table=Non
     rows, heads = q.shape[0], q.shape[1]
     out = torch.empty((rows, heads, dim), dtype=dtype, device=dev) if out is None else out
     op = _heads(out, "out", heads, dim, dtype, dev)
-    _need(out.shape[0] == rows, f"out of {out.shape[0]} rows for {rows}")
+    _need(out.shape[0] == rows, "out of as many rows as q is needed")
     lse = torch.empty((rows, heads), dtype=torch.float32, device=dev) if return_lse else None
     width = shared_width = per = 0
     if table is not None:
@@ -143,7 +151,7 @@ def attend(cache, q, table=None, lengths=None, max_length=None, shared_table=Non
     if shared_table is not None:
         _need(shared_table.dim() == 2 and shared_lengths is not None, "shared_table: [groups, pages], with lengths")
         groups, shared_width = shared_table.shape
-        _need(groups > 0 and rows % groups == 0, f"{groups} groups of {rows} rows")
+        _need(groups > 0 and rows % groups == 0, "rows that the groups divide are needed")
         per = rows // groups
         max_shared = shared_width * cache.page_size if max_shared is None else max_shared
     words = 0
@@ -161,11 +169,9 @@ def attend(cache, q, table=None, lengths=None, max_length=None, shared_table=Non
         max_shared or 0, max(per, 1) if shared_table is not None else 0,
         _vector(masks, "masks", torch.int64, (rows, words), dev), words, num_players, first_player,
         1.0 / math.sqrt(dim) if scale is None else scale)
-    with torch.cuda.device(dev):
-        nbytes = L.gnnshap_cache_attend_workspace(cache._c, a)
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
-        L.gnnshap_cache_attend(cache._c, a, _vector(info, "info", torch.int32, (1,), dev), _ptr(ws), nbytes,
-                               _stream(dev))
+    nbytes = L.gnnshap_cache_attend_workspace(cache._c, a)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+    _on(dev, L.gnnshap_cache_attend, cache._c, a, _vector(info, "info", torch.int32, (1,), dev), _ptr(ws), nbytes)
     return (out, lse) if return_lse else out
 
 
@@ -178,14 +184,11 @@ class TokenLogprobs(NamedTuple):
     top_id: torch.Tensor        # int32 [rows, top]
 
 
-def _logits(x, targets, top, **outputs):
-    _need(x.dim() == 2 and x.is_cuda and x.dtype in _DTYPES and (x.stride(1) == 1 or x.shape[1] < 2),
-          f"logits: a [rows, vocabulary] float32, float16 or bfloat16 tensor on a GPU with a contiguous last axis is "
-          f"needed, got {x.dtype} {tuple(x.shape)} with strides {x.stride()} on {x.device}")
-    rows = x.shape[0]
-    return L.gnnshap_logits(dtype=_DTYPES[x.dtype], top=top, num_rows=rows, vocab=x.shape[1], logits=x.data_ptr(),
-                            row_stride=x.stride(0),
-                            targets=_vector(targets, "targets", torch.int64, (rows,), x.device), **outputs)
+def _check_logits(x):
+    if x.dim() != 2 or not x.is_cuda or x.dtype not in _DTYPES or (x.stride(1) != 1 and x.shape[1] > 1):
+        raise ValueError(f"logits: a [rows, vocabulary] float32, float16 or bfloat16 tensor on a GPU with a contiguous "
+                         f"last axis is needed, got {x.dtype} {tuple(x.shape)} with strides {x.stride()} on {x.device}")
+    return _DTYPES[x.dtype]
 
 
 def token_logprobs(logits, targets=None, top=0, info=None):
@@ -193,18 +196,19 @@ def token_logprobs(logits, targets=None, top=0, info=None):
     rank of the tokens `targets` (int64 [rows]; negative or None: no token, 0
     and -1), entropy, and the `top` most likely tokens (at most 64; of equal
     logits the lowest token first).  Returns a TokenLogprobs."""
-    rows, dev = logits.shape[0], logits.device
-    f = torch.empty((3, rows), dtype=torch.float32, device=dev)
-    r = TokenLogprobs(f[0], f[1], f[2], torch.empty(rows, dtype=torch.int32, device=dev),
-                      torch.empty((rows, top), dtype=torch.float32, device=dev),
-                      torch.empty((rows, top), dtype=torch.int32, device=dev))
-    a = _logits(logits, targets, top, logprob=r.logprob.data_ptr(), entropy=r.entropy.data_ptr(),
-                lse=r.lse.data_ptr(), rank=r.rank.data_ptr(), top_logprob=r.top_logprob.data_ptr(),
-                top_id=r.top_id.data_ptr())
-    with torch.cuda.device(dev):
-        nbytes = L.gnnshap_token_logprobs_workspace(a)
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
-        L.gnnshap_token_logprobs(a, _vector(info, "info", torch.int32, (1,), dev), _ptr(ws), nbytes, _stream(dev))
+    dtype = _check_logits(logits)
+    (rows, vocab), dev = logits.shape, logits.device
+    logprob, entropy, lse = torch.empty((3, rows), dtype=torch.float32, device=dev).unbind(0)
+    rank, top_id = torch.empty(rows * (top + 1), dtype=torch.int32, device=dev).split((rows, rows * top))
+    r = TokenLogprobs(logprob, entropy, lse, rank, torch.empty((rows, top), dtype=torch.float32, device=dev),
+                      top_id.view(rows, top))
+    a = L.gnnshap_logits(dtype, top, rows, vocab, logits.data_ptr(), logits.stride(0),
+                         _vector(targets, "targets", torch.int64, (rows,), dev), logprob.data_ptr(),
+                         entropy.data_ptr(), lse.data_ptr(), rank.data_ptr(), r.top_logprob.data_ptr(),
+                         top_id.data_ptr())
+    nbytes = L.gnnshap_token_logprobs_workspace(a)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+    _on(dev, L.gnnshap_token_logprobs, a, _vector(info, "info", torch.int32, (1,), dev), _ptr(ws), nbytes)
     return r
 
 
@@ -214,15 +218,17 @@ def token_logprobs_backward(logits, targets, lse, entropy=None, grad_logprob=Non
     sum(grad_logprob * logprob) + sum(grad_entropy * entropy), in the logits'
     type.  lse and entropy as token_logprobs gave them; out may be the logits
     themselves."""
-    rows, dev = logits.shape[0], logits.device
-    a = _logits(logits, targets, 0, lse=_vector(lse, "lse", torch.float32, (rows,), dev),
-                entropy=_vector(entropy, "entropy", torch.float32, (rows,), dev))
-    out = torch.empty(logits.shape, dtype=logits.dtype, device=dev) if out is None else out
+    dtype = _check_logits(logits)
+    (rows, vocab), dev = logits.shape, logits.device
+    out = torch.empty((rows, vocab), dtype=logits.dtype, device=dev) if out is None else out
     _need(out.shape == logits.shape and out.dtype == logits.dtype and out.device == dev
-          and (out.stride(1) == 1 or out.shape[1] < 2), "out: a tensor like the logits is needed")
-    with torch.cuda.device(dev):
-        L.gnnshap_token_logprobs_backward(a, _vector(grad_logprob, "grad_logprob", torch.float32, (rows,), dev),
-                                          _vector(grad_entropy, "grad_entropy", torch.float32, (rows,), dev),
-                                          out.data_ptr(), out.stride(0),
-                                          _vector(info, "info", torch.int32, (1,), dev), _stream(dev))
+          and (out.stride(1) == 1 or vocab == 1), "out: a tensor like the logits is needed")
+    a = L.gnnshap_logits(dtype, 0, rows, vocab, logits.data_ptr(), logits.stride(0),
+                         _vector(targets, "targets", torch.int64, (rows,), dev), None,
+                         _vector(entropy, "entropy", torch.float32, (rows,), dev),
+                         _vector(lse, "lse", torch.float32, (rows,), dev))
+    _on(dev, L.gnnshap_token_logprobs_backward, a,
+        _vector(grad_logprob, "grad_logprob", torch.float32, (rows,), dev),
+        _vector(grad_entropy, "grad_entropy", torch.float32, (rows,), dev), out.data_ptr(), out.stride(0),
+        _vector(info, "info", torch.int32, (1,), dev))
     return out

@@ -494,12 +494,16 @@ int lay_out(AttendArgs& a, const gnnshap_cache* c, const gnnshap_queries* q) {
     p.by_query = !i && queries >= 64 && !p.wide;
     p.tile = p.wide ? 128 : p.by_query ? 64 : 16 * tile_of(queries, c->head_dim);
     p.tiles = static_cast<int>(ceil_div(queries, p.tile));
-    // enough workgroups for the chip, at least 256 keys each, at most 4096
+    // Splits: as many as all the workgroups that the chip holds at a time
+    // (two per compute unit of the wide kernel, four of the others), of 256
+    // keys at least; own parts of unlike lengths in pieces of at most 512.
     const int64_t base = q->num_rows / p.r * c->kv_heads * p.tiles;
-    int64_t keys = ceil_div(std::max(p.max_len, 1), std::max<int64_t>(1, 1024 / std::max<int64_t>(base, 1)));
-    keys = std::min<int64_t>(std::max<int64_t>(ceil_div(keys, 128) * 128, 256), i ? 512 : 4096);
-    p.split_keys = static_cast<int>(keys);
-    p.splits = static_cast<int>(std::max<int64_t>(1, ceil_div(p.max_len, keys)));
+    const int64_t want = std::max<int64_t>(1, (p.wide ? 512 : 1024) / std::max<int64_t>(base, 1));
+    int64_t keys = ceil_div(std::max(p.max_len, 1), want);
+    keys = std::max<int64_t>(ceil_div(keys, 128) * 128, 256);
+    if (!p.wide) keys = std::min<int64_t>(keys, i ? 512 : 4096);
+    p.split_keys = static_cast<int>(std::min<int64_t>(keys, INT32_MAX / 2));
+    p.splits = static_cast<int>(std::max<int64_t>(1, ceil_div(p.max_len, p.split_keys)));
     p.slot0 = slots;
     slots += p.splits;
     if (base * p.splits > INT32_MAX) return gnnshap::fail(GNNSHAP_EUNSUPPORTED, "too many workgroups");

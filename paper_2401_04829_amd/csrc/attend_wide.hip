@@ -12,13 +12,16 @@
 // instructions: S^T = K Q^T leaves query = lane % 32 and keys in registers,
 // register i of a lane in the upper half (h = 1) or lower half key
 // 8 (i / 4) + 4 h + i % 4; eight registers on end are the right operand of
-// 16 keys of O^T = V^T P^T.  Values are turned over on the way to LDS: row d
-// holds the elements d of the 64 keys, in the order of those registers.  Row
-// r of the product's tile t is element NT r + t of the NT tiles, so that a
-// lane's results (and the values that it reads for own tokens) are NT
-// elements on end.  LDS rows are whole multiples of 128 bytes, their 16-byte
-// pieces swapped by the row's number, so that neither side meets itself in a
-// bank.
+// 16 keys of O^T = V^T P^T.  Values are turned over on the way to LDS: a row
+// holds one element of the 64 keys, in the order of those registers.  Row r of
+// the product's tile t is element NT r + t of the NT tiles, so that a lane's
+// results (and the values that it reads for own tokens) are NT elements on
+// end.  The 16-byte pieces of an LDS row are swapped by the row's number, so
+// that the 16 lanes that are served at a time meet 16 different columns.
+//
+// Where a tile's keys are is found out two tiles ahead: one wavefront turns
+// 64 page table entries into byte offsets in LDS, having asked for the next
+// tile's entries a step before.
 #include "attend.h"
 
 namespace {
@@ -49,10 +52,12 @@ struct Wide {
     else
       return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(vec8, a), __builtin_bit_cast(vec8, b), c, 0, 0, 0);
   }
-  // Byte of piece p of key row r, and of 16-byte piece p of the values' row d.
-  static __device__ __forceinline__ int key_at(int r, int p) { return r * DP * 2 + ((p ^ (r & 7)) << 4); }
-  static __device__ __forceinline__ int val_at(int d, int p) {
-    return kKeyBytes + d * kTile * 2 + ((p ^ (((d / NT) ^ (d / (8 * NT))) & 7)) << 4);
+  // Byte of 16-byte piece p of key row r, and of the values' row of element d.
+  static __device__ __forceinline__ int key_at(int r, int p) {
+    return r * DP * 2 + ((p ^ (DP >= 128 ? r & 15 : (r >> 1) & 7)) << 4);
+  }
+  static __device__ __forceinline__ int val_at(int r, int t, int p) {
+    return kKeyBytes + (32 * t + r) * kTile * 2 + ((p ^ ((r >> 1) & 7)) << 4);
   }
   // 8-byte place of the four keys 4 c on in a values' row: the order of the weights' registers.
   static __device__ __forceinline__ int quad_place(int c) {
@@ -63,27 +68,22 @@ struct Wide {
   u4_t key[kKeyLoads];
   unsigned val[kValLoads][4][kValElems / 2];
 
-  // A tile's keys k .. k + 63 (those behind k1 as the last one) on their way to registers.
-  template <class Offset>
-  __device__ __forceinline__ void load(const AttendArgs& a, Offset offset, int k, int k1) {
+  // A tile on its way to registers; offsets: the byte of each key's (and
+  // value's) first element.  Elements behind head_dim are read as others of the
+  // row: the queries hold 0 there, and the results are not written.
+  __device__ __forceinline__ void load(const AttendArgs& a, const int64_t* offsets) {
     const int tid = threadIdx.x, D = a.c.head_dim;
+    const char* const k = static_cast<const char*>(a.c.k) + (8 * (tid % kPieces) < D ? 16 * (tid % kPieces) : 0);
 #pragma unroll
-    for (int i = 0; i < kKeyLoads; ++i) {
-      const int r = tid / kPieces + i * (256 / kPieces), p = tid % kPieces;
-      key[i] = u4_t{0u, 0u, 0u, 0u};
-      if (8 * p < D) __builtin_memcpy(&key[i], static_cast<const T*>(a.c.k) + offset(min(k + r, k1 - 1)) + 8 * p, 16);
-    }
+    for (int i = 0; i < kKeyLoads; ++i)
+      __builtin_memcpy(&key[i], k + offsets[tid / kPieces + i * (256 / kPieces)], 16);
+    const int d = tid % kValPieces * kValElems;
+    const char* const v = static_cast<const char*>(a.c.v) + (d < D ? 2 * d : 0);
 #pragma unroll
-    for (int i = 0; i < kValLoads; ++i) {
-      const int c = tid / kValPieces + i * (256 / kValPieces), d = tid % kValPieces * kValElems;
+    for (int i = 0; i < kValLoads; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-#pragma unroll
-        for (int e = 0; e < kValElems / 2; ++e) val[i][j][e] = 0u;
-        if (d < D)
-          __builtin_memcpy(&val[i][j][0], static_cast<const T*>(a.c.v) + offset(min(k + 4 * c + j, k1 - 1)) + d, 2 * kValElems);
-      }
-    }
+      for (int j = 0; j < 4; ++j)
+        __builtin_memcpy(&val[i][j][0], v + offsets[4 * (tid / kValPieces + i * (256 / kValPieces)) + j], 2 * kValElems);
   }
   __device__ __forceinline__ void store(char* buf) const {
     const int tid = threadIdx.x;
@@ -100,7 +100,7 @@ struct Wide {
         const unsigned sel = e & 1 ? 0x07060302u : 0x05040100u;
         const u2_t x = {__builtin_amdgcn_perm(val[i][1][e / 2], val[i][0][e / 2], sel),
                         __builtin_amdgcn_perm(val[i][3][e / 2], val[i][2][e / 2], sel)};
-        *reinterpret_cast<u2_t*>(buf + val_at(d + e, at >> 1) + (at & 1) * 8) = x;
+        *reinterpret_cast<u2_t*>(buf + val_at((d + e) / NT, (d + e) % NT, at >> 1) + (at & 1) * 8) = x;
       }
     }
   }
@@ -170,9 +170,7 @@ __global__ __launch_bounds__(64 * kWaves, DP <= 128 ? 2 : 1) void k_cache_attend
   const int D = a.c.head_dim;
   const Place at = place_of(a, part, false);
   if (at.k0 >= at.k1 && !a.direct && !at.with_own) return;
-  int* pages = reinterpret_cast<int*>(room + 2 * W::kBufBytes);
-  const int page0 = at.k0 / a.c.page_size;
-  stage_pages(a, part, at, pages);
+  int64_t(*offsets)[kTile] = reinterpret_cast<int64_t(*)[kTile]>(room + 2 * W::kBufBytes);  // of three tiles
 
   const int n_queries = part.r * a.share, q0 = at.tile * kQueries + wave * 32, qi = q0 + r, qs = qi < n_queries ? qi : 0;
   const int64_t row = at.group * part.r + qs / a.share;
@@ -192,44 +190,78 @@ __global__ __launch_bounds__(64 * kWaves, DP <= 128 ? 2 : 1) void k_cache_attend
     }
   }
   WideState<T, DP> st;
-  __syncthreads();
 
-  const int64_t head_at = static_cast<int64_t>(at.kv_head) * a.c.head_stride;
-  const auto offset = [&](int key) {
+  // A step's page of this thread's key (of the first wavefront), and its offset.
+  const auto page_id = [&](int k) {
     int slot;
-    const int pg = page_of(a, key, slot);
-    return pages[pg - page0] * a.c.page_stride + slot * a.c.slot_stride + head_at;
+    const int pg = page_of(a, min(k + lane, at.k1 - 1), slot);
+    return part.table[at.group * part.width + pg];
   };
-  const uint64_t* mask = a.q.masks + row * a.q.mask_words;
-  const auto bits_of = [&](int k) {
+  const auto put_offset = [&](int k, int page, int64_t* to) {
+    int slot;
+    page_of(a, min(k + lane, at.k1 - 1), slot);
+    if (page < 0 || page >= a.c.num_pages) {
+      if (a.info) *a.info = 1;
+      page = 0;
+    }
+    to[lane] = 2 * (page * a.c.page_stride + slot * a.c.slot_stride + static_cast<int64_t>(at.kv_head) * a.c.head_stride);
+  };
+  // The mask bits of positions k .. k + 63: two words of the row, of which the
+  // second is the next step's first.
+  const uint64_t* const mask = a.q.masks + row * a.q.mask_words;
+  const bool masked = a.q.num_players > 0;
+  const auto word_of = [&](int64_t i) {
+    return i >= 0 && i < (a.q.num_players + 63) >> 6 ? mask[i] : 0ull;
+  };
+  const int shift = static_cast<int>((at.first + at.k0) & 63);
+  const auto bits_of = [&](int k, uint64_t lo, uint64_t hi) {
+    const int64_t p = at.first + k, n = a.q.num_players - p;  // players before position k: -p
+    uint64_t bits = shift ? lo >> shift | hi << (64 - shift) : lo;
+    if (p < 0) bits |= p <= -64 ? ~0ull : (1ull << -p) - 1;
+    if (n < 64) bits |= n <= 0 ? ~0ull : ~0ull << n;
+    if (!masked) bits = ~0ull;
     const int left = at.k1 - k;
-    const uint32_t there = left >= 32 ? ~0u : left <= 0 ? 0u : (1u << left) - 1u;
-    return a.q.num_players > 0 && left > 0 ? there & seen(mask, at.first + k, a.q.num_players) : there;
+    return left >= 64 ? bits : bits & ((1ull << left) - 1);
   };
 
   if (at.k0 < at.k1) {
+    const int steps = (at.k1 - at.k0 + kTile - 1) / kTile;
+    int page = 0;
+    if (wave == 0) {
+      put_offset(at.k0, page_id(at.k0), offsets[0]);
+      put_offset(at.k0 + kTile, page_id(at.k0 + kTile), offsets[1]);
+      page = page_id(at.k0 + 2 * kTile);
+    }
+    int64_t at_word = (at.first + at.k0) >> 6;
+    uint64_t lo = masked ? word_of(at_word) : 0ull, hi = masked ? word_of(at_word + 1) : 0ull;
+    __syncthreads();
     W next;
-    next.load(a, offset, at.k0, at.k1);
-    uint32_t bits[2] = {bits_of(at.k0), bits_of(at.k0 + 32)};
+    next.load(a, offsets[0]);
     next.store(room);
     __syncthreads();
-    int turn = 0;
-    for (int k = at.k0; k < at.k1; k += kTile, turn ^= 1) {
-      const char* buf = room + turn * W::kBufBytes;
-      const bool more = k + kTile < at.k1;
-      uint32_t bits_next[2] = {0u, 0u};
-      if (more) {
-        next.load(a, offset, k + kTile, at.k1);
-        bits_next[0] = bits_of(k + kTile);
-        bits_next[1] = bits_of(k + kTile + 32);
+    int third = 2;  // of the tile after the next
+    for (int i = 0; i < steps; ++i) {
+      const int k = at.k0 + i * kTile;
+      const char* buf = room + (i & 1) * W::kBufBytes;
+      const bool more = i + 1 < steps;
+      if (more) next.load(a, offsets[third == 0 ? 2 : third - 1]);
+      const uint64_t bits = bits_of(k, lo, hi);
+      lo = hi;
+      ++at_word;
+      if (masked && more) hi = word_of(at_word + 1);
+      if (wave == 0 && i + 2 < steps) {
+        put_offset(k + 2 * kTile, page, offsets[third]);
+        page = page_id(k + 3 * kTile);
       }
+      third = third == 2 ? 0 : third + 1;
       f16v_t s[2];
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
-        s[n] = __ballot(bits[n] != ~0u) ? WideState<T, DP>::unseen(bits[n]) : f16v_t{};
+        const uint32_t half = static_cast<uint32_t>(n ? bits >> 32 : bits);
+        s[n] = __ballot(half != ~0u) ? WideState<T, DP>::unseen(half) : f16v_t{};
 #pragma unroll
-        for (int i = 0; i < W::KS; ++i)
-          s[n] = W::mfma(*reinterpret_cast<const u4_t*>(buf + W::key_at(32 * n + r, 2 * i + h)), q[i], s[n]);
+        for (int j = 0; j < W::KS; ++j)
+          s[n] = W::mfma(*reinterpret_cast<const u4_t*>(buf + W::key_at(32 * n + r, 2 * j + h)), q[j], s[n]);
       }
       st.weigh(s, scale);
 #pragma unroll
@@ -239,11 +271,9 @@ __global__ __launch_bounds__(64 * kWaves, DP <= 128 ? 2 : 1) void k_cache_attend
           const u4_t p = WideState<T, DP>::operand(s[n], u);
 #pragma unroll
           for (int t = 0; t < W::NT; ++t)
-            st.o[t] = W::mfma(*reinterpret_cast<const u4_t*>(buf + W::val_at(W::NT * r + t, 4 * n + 2 * u + h)), p, st.o[t]);
+            st.o[t] = W::mfma(*reinterpret_cast<const u4_t*>(buf + W::val_at(r, t, 4 * n + 2 * u + h)), p, st.o[t]);
         }
-      if (more) next.store(room + (turn ^ 1) * W::kBufBytes);
-      bits[0] = bits_next[0];
-      bits[1] = bits_next[1];
+      if (more) next.store(room + ((i + 1) & 1) * W::kBufBytes);
       __syncthreads();
     }
   }
@@ -325,7 +355,7 @@ __global__ __launch_bounds__(64 * kWaves, DP <= 128 ? 2 : 1) void k_cache_attend
 template <class T, int DP>
 int launch(const AttendArgs& a, hipStream_t s) {
   const Part& p = a.shared;
-  const size_t bytes = 2 * Wide<T, DP>::kBufBytes + sizeof(int) * (p.split_keys / a.c.page_size + 2);
+  const size_t bytes = 2 * Wide<T, DP>::kBufBytes + 3 * kTile * sizeof(int64_t);
   const unsigned grid = static_cast<unsigned>(a.q.num_rows / p.r * a.c.kv_heads * p.tiles * p.splits);
   GS_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&k_cache_attend_wide<T, DP>),
                              hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)));

@@ -11,10 +11,11 @@
 //
 // Alternatives: a wavefront keeps a falling list of 64 keys, lane i the i-th
 // best; a key is (order-preserving image of x, ~token), so keys are unique
-// and of equal logits the lowest token wins.  A chunk of a row is looked at
-// again only if its maximum exceeds the list's k-th key; of the wavefront's
-// first chunk only the logits from the k-th largest of the lanes' maxima on
-// (at least k logits are no smaller).
+// and of equal logits the lowest token wins.  The list starts from a bound
+// that the k-th best cannot be below: the k-th largest of the maxima that the
+// lanes find in the row's first chunks.  A chunk, and of it what one load
+// brought, is looked at again only if its maximum exceeds the bound, which
+// rises to the list's k-th key once there is one.
 //
 // One wavefront reads chunks of 64 lanes x 4 x 16 bytes.  A row is one
 // wavefront's, or one workgroup's, or (few rows) several workgroups', whose
@@ -32,7 +33,8 @@ using gnnshap::store_pack;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kWaves = 4;      // wavefronts of a workgroup
-constexpr int kMaxParts = 64;  // workgroups of a row
+constexpr int kMaxParts = 64;        // workgroups of a row
+constexpr int kMaxPartKeys = 1024;  // of their alternatives
 
 struct Stats {
   float m, s, w;  // w = sum e_j log2(e_j)
@@ -80,53 +82,61 @@ __device__ __forceinline__ float unordered(uint32_t o) {
   return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
 }
 
-struct Key {
-  uint32_t v, i;  // i = ~token; (0, 0) is below every logit's key
-};
-__device__ __forceinline__ bool above(Key a, Key b) { return a.v > b.v || (a.v == b.v && a.i > b.i); }
-__device__ __forceinline__ Key lane_key(Key a, int lane) {
-  Key r;
-  r.v = __builtin_amdgcn_readlane(a.v, lane);
-  r.i = __builtin_amdgcn_readlane(a.i, lane);
-  return r;
+// (image of the logit, ~token); 0 is below every logit's key.
+typedef uint64_t Key;
+__device__ __forceinline__ Key key_of(float x, int64_t token) {
+  return static_cast<uint64_t>(ordered(x)) << 32 | static_cast<uint32_t>(~token);
+}
+__device__ __forceinline__ float logit_of(Key k) { return unordered(static_cast<uint32_t>(k >> 32)); }
+__device__ __forceinline__ int32_t token_of(Key k) { return static_cast<int32_t>(~static_cast<uint32_t>(k)); }
+__device__ __forceinline__ Key of_lane(Key k, int lane) {
+  return static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(k >> 32), lane))) << 32 |
+         static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(k), lane));
+}
+// The key of the lane below, moved within the vector unit.
+__device__ __forceinline__ Key from_below(Key k) {
+  constexpr int kWaveShr1 = 0x138;
+  const int hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(k >> 32), kWaveShr1, 0xF, 0xF, false);
+  const int lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(k), kWaveShr1, 0xF, 0xF, false);
+  return static_cast<uint64_t>(static_cast<uint32_t>(hi)) << 32 | static_cast<uint32_t>(lo);
 }
 
-// The 64 best keys of a wavefront, of which the first k are wanted.
+// The 64 best keys of a wavefront, lane i the i-th, of which the first k are wanted.
 struct TopList {
-  Key mine{0u, 0u}, kth{0u, 0u};
+  Key mine = 0, kth = 0;
   int k;
   __device__ __forceinline__ explicit TopList(int top) : k(top) {}
-  __device__ __forceinline__ void insert(Key c) {
+  // The keys of the lanes in `is`, the lowest lane first.
+  __device__ __forceinline__ void offer(Key c, uint64_t is) {
     const int lane = threadIdx.x & 63;
-    const int pos = __popcll(__ballot(above(mine, c)));
-    Key up;
-    up.v = __shfl_up(mine.v, 1);
-    up.i = __shfl_up(mine.i, 1);
-    if (lane > pos) mine = up;
-    if (lane == pos) mine = c;
-    kth = lane_key(mine, k - 1);
-  }
-  // Every lane's key; ends after at most 64 insertions.
-  __device__ __forceinline__ void offer(Key c, bool is) {
-    const int lane = threadIdx.x & 63;
-    uint64_t b = __ballot(is && above(c, kth));
-    while (b) {
-      const int src = __builtin_ctzll(b);
-      insert(lane_key(c, src));
-      is = is && lane != src;
-      b = __ballot(is && above(c, kth));
+    while (is) {
+      const int src = __builtin_ctzll(is);
+      is &= is - 1;
+      const Key in = of_lane(c, src);
+      if (in <= kth) continue;
+      const int pos = __popcll(__ballot(mine > in));
+      const Key up = from_below(mine);
+      mine = lane > pos ? up : lane == pos ? in : mine;
+      kth = of_lane(mine, k - 1);
     }
   }
 };
 
-// The k-th largest of the lanes' values.
+// A lower bound of the k-th largest of the lanes' values (the upper half of its bits).
 __device__ __forceinline__ uint32_t kth_of_lanes(uint32_t v, int k) {
   uint32_t t = 0;
-  for (int b = 31; b >= 0; --b) {
+#pragma unroll
+  for (int b = 31; b >= 16; --b) {
     const uint32_t u = t | (1u << b);
     if (__popcll(__ballot(v >= u)) >= k) t = u;
   }
   return t;
+}
+
+// The largest float below those whose image is `from` or more; NaN if -inf is among them.
+__device__ __forceinline__ float below(uint32_t from) {
+  constexpr uint32_t kLowest = 0x007FFFFFu, kZero = 0x80000000u;  // of -inf, of 0 (whose image below is -0)
+  return from <= kLowest ? NAN : unordered(from - (from == kZero ? 2u : 1u));
 }
 
 template <class T>
@@ -135,6 +145,7 @@ struct Chunk {
   static constexpr int kLoads = 4;
   static constexpr int kElems = kVec * kLoads;  // per lane
   static constexpr int kSize = 64 * kElems;     // per wavefront
+  typedef float Floats __attribute__((ext_vector_type(kElems)));
   Pack<T, kVec> p[kLoads];
   // Elements `base` on of a row of n; behind the row -inf.
   __device__ __forceinline__ void load(const T* row, int64_t base, int64_t n) {
@@ -166,23 +177,54 @@ struct LogprobArgs {
   Key* part_keys;    // [rows][parts][top]
 };
 
-// What a row's statistics and list give the caller; the whole wavefront calls it.
-__device__ __forceinline__ void write_row(const LogprobArgs& a, int64_t row, const Stats& st, int rank,
-                                          const TopList& list, bool has, float xt) {
-  const int lane = threadIdx.x & 63;
+// What a row's statistics give the caller; logs = log st.s.
+__device__ __forceinline__ void write_stats(const LogprobArgs& a, int64_t row, const Stats& st, float logs, int rank,
+                                            bool has, float xt) {
   const bool none = st.s == 0.f;  // every logit is -inf
+  if (a.l.lse) a.l.lse[row] = none ? -INFINITY : st.m + logs;
+  if (a.l.entropy) a.l.entropy[row] = none ? 0.f : logs - kLn2 * (st.w / st.s);
+  if (a.l.logprob) a.l.logprob[row] = !has ? 0.f : none ? -INFINITY : (xt - st.m) - logs;
+  if (a.l.rank) a.l.rank[row] = has ? rank : -1;
+}
+
+// The same and the alternatives, of which lane i holds the i-th; the whole wavefront calls it.
+__device__ __forceinline__ void write_row(const LogprobArgs& a, int64_t row, const Stats& st, int rank, Key mine,
+                                          bool has, float xt) {
+  const int lane = threadIdx.x & 63;
   const float logs = logf(st.s);
-  if (lane == 0) {
-    if (a.l.lse) a.l.lse[row] = none ? -INFINITY : st.m + logs;
-    if (a.l.entropy) a.l.entropy[row] = none ? 0.f : logs - kLn2 * (st.w / st.s);
-    if (a.l.logprob) a.l.logprob[row] = !has ? 0.f : none ? -INFINITY : (xt - st.m) - logs;
-    if (a.l.rank) a.l.rank[row] = has ? rank : -1;
-  }
+  if (lane == 0) write_stats(a, row, st, logs, rank, has, xt);
   if (lane < a.l.top) {
     const int64_t at = row * a.l.top + lane;
-    if (a.l.top_logprob) a.l.top_logprob[at] = none ? -INFINITY : (unordered(list.mine.v) - st.m) - logs;
-    if (a.l.top_id) a.l.top_id[at] = static_cast<int32_t>(~list.mine.i);
+    if (a.l.top_logprob) a.l.top_logprob[at] = st.s == 0.f ? -INFINITY : (logit_of(mine) - st.m) - logs;
+    if (a.l.top_id) a.l.top_id[at] = token_of(mine);
   }
+}
+
+// The k best of `lists` falling lists of k keys, into `best` (all in LDS;
+// threads tid = 0 .. n - 1 call it, behind a barrier, and all threads of the
+// workgroup together; it ends with one).  Keys below any list's last one are
+// not among them; the place of one of the others (which go to `left`) is the
+// number of those above it.  Keys are unique but for 0; where there are fewer
+// than k others, `best` ends with 0.
+__device__ __forceinline__ void join_lists(const Key* keys, int lists, int k, Key* left, int* n_left, Key* best, int tid,
+                                           int n) {
+  if (tid == 0) *n_left = 0;
+  if (tid < k) best[tid] = 0;
+  Key from = 1;
+  for (int j = 0; j < lists; ++j) from = max(from, keys[j * k + k - 1]);
+  __syncthreads();
+  for (int i = tid; i < lists * k; i += n)
+    if (keys[i] >= from) left[atomicAdd(n_left, 1)] = keys[i];
+  __syncthreads();
+  const int m = *n_left;
+  for (int i = tid; i < m; i += n) {
+    const Key mine = left[i];
+    int place = 0;
+#pragma unroll 8
+    for (int j = 0; j < m; ++j) place += left[j] > mine;
+    if (place < k) best[place] = mine;
+  }
+  __syncthreads();
 }
 
 // The row's given token and its logit; `has` false if there is none.
@@ -213,21 +255,46 @@ __global__ __launch_bounds__(64 * kWaves) void k_token_logprobs(LogprobArgs a) {
   int rank = 0;
   bool has = false;
   float xt = 0.f;
+  int64_t base = in ? (static_cast<int64_t>(part) * PER_ROW + way) * C::kSize : V;
+  const int64_t step = static_cast<int64_t>(a.parts) * PER_ROW * C::kSize;
+  C next;
+  if (base < V) next.load(x, base, V);
+  float bound = NAN;  // no logit up to it is wanted
+  if (a.l.top > 0) {
+    // at least top logits are no smaller than the top-th largest of the
+    // maxima of as many sets of logits: a lane's, in all of the row's wavefronts
+    uint32_t most = 0u;
+    if (base < V) {
+      float f = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < C::kElems; ++i) f = fmaxf(f, static_cast<float>(next.p[i / C::kVec].v[i % C::kVec]));
+      most = ordered(f);
+    }
+    if constexpr (PER_ROW > 1) {
+      __shared__ uint32_t all[kWaves][64];
+      all[wave][lane] = most;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < PER_ROW; ++i) most = max(most, all[wave - way + i][lane]);
+    }
+    bound = below(kth_of_lanes(most, a.l.top));
+  }
   if (in) {
-    int64_t base = (static_cast<int64_t>(part) * PER_ROW + way) * C::kSize;
-    const int64_t step = static_cast<int64_t>(a.parts) * PER_ROW * C::kSize;
-    C next;
-    if (base < V) next.load(x, base, V);
     xt = given(a, x, row, has);
-    bool first = true;
     for (; base < V; base += step) {
       const C c = next;
       if (base + step < V) next.load(x, base + step, V);
-      float f[C::kElems], most = -INFINITY;
+      typename C::Floats f;
+      float of_load[C::kLoads], most = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < C::kElems; ++i) {
-        f[i] = static_cast<float>(c.p[i / C::kVec].v[i % C::kVec]);
-        most = fmaxf(most, f[i]);
+      for (int u = 0; u < C::kLoads; ++u) {
+        of_load[u] = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < C::kVec; ++j) {
+          f[u * C::kVec + j] = static_cast<float>(c.p[u].v[j]);
+          of_load[u] = fmaxf(of_load[u], f[u * C::kVec + j]);
+        }
+        most = fmaxf(most, of_load[u]);
       }
       if (most > st.m) move_to(st, most);
       const float m = finite_max(st.m);
@@ -242,19 +309,23 @@ __global__ __launch_bounds__(64 * kWaves) void k_token_logprobs(LogprobArgs a) {
       st.s += s;
       st.w += w;
       if (a.l.top > 0) {
-        const uint32_t o = ordered(most);
-        if (__ballot(o > list.kth.v)) {
-          const uint32_t from = first ? kth_of_lanes(o, a.l.top) : 0u;
+        if (__ballot(!(most <= bound))) {
 #pragma unroll
-          for (int i = 0; i < C::kElems; ++i) {
-            const int64_t at = base + ((i / C::kVec) * 64 + lane) * C::kVec + i % C::kVec;
-            Key key;
-            key.v = ordered(f[i]);
-            key.i = ~static_cast<uint32_t>(at);
-            list.offer(key, at < V && key.v >= from);
+          for (int u = 0; u < C::kLoads; ++u) {
+            if (!__ballot(!(of_load[u] <= bound))) continue;
+            uint32_t any = 0u;  // elements of which some lane's may enter
+#pragma unroll
+            for (int j = 0; j < C::kVec; ++j) any |= __ballot(!(f[u * C::kVec + j] <= bound)) ? 1u << j : 0u;
+            while (any) {
+              const int j = __builtin_ctz(any);
+              any &= any - 1u;
+              const int64_t at = base + (u * 64 + lane) * C::kVec + j;
+              const float x = f[u * C::kVec + j];
+              list.offer(key_of(x, at), __ballot(!(x <= bound) && at < V));
+            }
           }
+          if (list.kth) bound = logit_of(list.kth);
         }
-        first = false;
       }
     }
     wave_sum(st);
@@ -262,59 +333,117 @@ __global__ __launch_bounds__(64 * kWaves) void k_token_logprobs(LogprobArgs a) {
 
   if constexpr (PER_ROW > 1) {
     __shared__ Stats stats[kWaves];
-    __shared__ int ranks[kWaves];
-    __shared__ Key keys[kWaves][64];
+    __shared__ int ranks[kWaves], n_left[kRows];
+    __shared__ Key keys[kWaves * GNNSHAP_MAX_TOP], left[kWaves * GNNSHAP_MAX_TOP], best[kRows * GNNSHAP_MAX_TOP];
+    const int k = a.l.top, r = wave / PER_ROW;
     if (lane == 0) {
       stats[wave] = st;
       ranks[wave] = rank;
     }
-    keys[wave][lane] = list.mine;
+    if (lane < k) keys[wave * k + lane] = list.mine;
     __syncthreads();
-    if (wave != 0 || !in) return;
+    if (k > 0)
+      join_lists(keys + r * PER_ROW * k, PER_ROW, k, left + r * PER_ROW * GNNSHAP_MAX_TOP, n_left + r,
+                 best + r * GNNSHAP_MAX_TOP, threadIdx.x % (64 * PER_ROW), 64 * PER_ROW);
+    if (way != 0 || !in) return;
     for (int i = 1; i < PER_ROW; ++i) {
-      add(st, stats[i]);
-      rank += ranks[i];
-      if (a.l.top > 0) list.offer(keys[i][lane], lane < a.l.top);
+      add(st, stats[wave + i]);
+      rank += ranks[wave + i];
     }
+    if (lane < k) list.mine = best[r * GNNSHAP_MAX_TOP + lane];
     if (a.parts > 1) {
       const int64_t at = row * a.parts + part;
       if (lane == 0) {
         a.part_stats[at] = st;
         a.part_rank[at] = rank;
       }
-      if (lane < a.l.top) a.part_keys[at * a.l.top + lane] = list.mine;
+      if (lane < k) a.part_keys[at * k + lane] = list.mine;
       return;
     }
   }
-  if (in) write_row(a, row, st, rank, list, has, xt);
+  if (in) write_row(a, row, st, rank, list.mine, has, xt);
 }
 
-// Joins the parts of rows that several workgroups read, a wavefront per row.
+// Joins the parts of a row that several workgroups read, a workgroup per row.
 template <class T>
 __global__ __launch_bounds__(64 * kWaves) void k_token_logprobs_join(LogprobArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * kWaves + (threadIdx.x >> 6);
-  if (row >= a.l.num_rows) return;
+  __shared__ Key keys[kMaxPartKeys], left[kMaxPartKeys], best[GNNSHAP_MAX_TOP];
+  __shared__ int n_left;
+  const int lane = threadIdx.x & 63, k = a.l.top, n = a.parts * k;
+  const int64_t row = blockIdx.x;
+  for (int i = threadIdx.x; i < n; i += 64 * kWaves) keys[i] = a.part_keys[row * n + i];
+  __syncthreads();
+  if (k > 0) join_lists(keys, a.parts, k, left, &n_left, best, threadIdx.x, blockDim.x);
+  if (threadIdx.x >= 64) return;
   Stats st = no_stats();
   int rank = 0;
   if (lane < a.parts) {
     st = a.part_stats[row * a.parts + lane];
     rank = a.part_rank[row * a.parts + lane];
   }
+  bool has;
+  const float xt = given(a, static_cast<const T*>(a.l.logits) + row * a.l.row_stride, row, has);
   wave_sum(st);
 #pragma unroll
   for (int off = 1; off < 64; off *= 2) rank += __shfl_xor(rank, off);
-  TopList list(a.l.top);
-  const int keys = a.parts * a.l.top;
-  for (int i = 0; i < keys; i += 64) {
-    const bool is = i + lane < keys;
-    Key key{0u, 0u};
-    if (is) key = a.part_keys[row * keys + i + lane];
-    list.offer(key, is);
+  write_row(a, row, st, rank, lane < k ? best[lane] : 0, has, xt);
+}
+
+// Rows of up to LANES x N logits, LANES lanes per row: a row is in registers,
+// so its maximum comes first and the alternatives are taken off one by one.
+template <class T, int LANES, int N>
+__global__ __launch_bounds__(256) void k_token_logprobs_short(LogprobArgs a) {
+  const int lane = threadIdx.x % LANES, V = static_cast<int>(a.l.vocab);
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * (256 / LANES) + threadIdx.x / LANES;
+  const bool in = row < a.l.num_rows;
+  const T* x = static_cast<const T*>(a.l.logits) + (in ? row : 0) * a.l.row_stride;
+  float f[N], m = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < N; ++i) f[i] = in && lane + LANES * i < V ? static_cast<float>(x[lane + LANES * i]) : -INFINITY;
+  bool has = false;
+  const float xt = in ? given(a, x, row, has) : 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) m = fmaxf(m, f[i]);
+#pragma unroll
+  for (int off = 1; off < LANES; off *= 2) m = fmaxf(m, __shfl_xor(m, off));
+  const float use = finite_max(m);
+  float s = 0.f, w = 0.f;
+  int rank = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float d = (f[i] - use) * kLog2e, e = __builtin_amdgcn_exp2f(d);
+    s += e;
+    w += e * fmaxf(d, -200.f);
+    rank += f[i] > xt;
   }
-  bool has;
-  const float xt = given(a, static_cast<const T*>(a.l.logits) + row * a.l.row_stride, row, has);
-  write_row(a, row, st, rank, list, has, xt);
+#pragma unroll
+  for (int off = 1; off < LANES; off *= 2) {
+    s += __shfl_xor(s, off);
+    w += __shfl_xor(w, off);
+    rank += __shfl_xor(rank, off);
+  }
+  const bool none = s == 0.f;
+  const float logs = logf(s);
+  if (in && lane == 0) write_stats(a, row, Stats{m, s, w}, logs, rank, has, xt);
+
+  Key last = ~0ull;
+  for (int k = 0; k < a.l.top; ++k) {
+    Key best = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const Key key = key_of(f[i], lane + LANES * i);
+      if (lane + LANES * i < V && key < last) best = max(best, key);
+    }
+#pragma unroll
+    for (int off = 1; off < LANES; off *= 2)
+      best = max(best, static_cast<Key>(__shfl_xor(static_cast<unsigned long long>(best), off)));
+    last = best;
+    if (in && lane == k % LANES) {
+      const int64_t at = row * a.l.top + k;
+      if (a.l.top_logprob) a.l.top_logprob[at] = none ? -INFINITY : (logit_of(best) - m) - logs;
+      if (a.l.top_id) a.l.top_id[at] = token_of(best);
+    }
+  }
 }
 
 struct GradArgs {
@@ -382,16 +511,24 @@ int check_logits(const gnnshap_logits* l) {
   return GNNSHAP_OK;
 }
 
-// Wavefronts per row: one where there are rows for all of the chip's
-// wavefronts several times, else four, and with few rows several workgroups.
+// How a row is read: up to 1024 logits in registers, of 16 lanes or of a
+// wavefront; else by one wavefront where there are rows for all of the chip's
+// wavefronts several times, by four otherwise, and with few rows by several
+// workgroups.
+enum Way { kShort64, kShort256, kShort1024, kWavefront, kTwoWavefronts, kWorkgroup };
 struct Shape {
-  int per_row, parts;
+  Way way;
+  int parts;
 };
 Shape shape_of(const gnnshap_logits& l) {
+  if (l.vocab <= 64) return {kShort64, 1};
+  if (l.vocab <= 1024) return {l.vocab <= 256 ? kShort256 : kShort1024, 1};
   const int64_t chunk = 64 * 4 * (l.dtype == GNNSHAP_F32 ? 4 : 8), chunks = gnnshap::ceil_div(l.vocab, chunk);
-  if (l.num_rows >= 4096 || chunks == 1) return {1, 1};
+  if (chunks == 1 || (l.num_rows >= 4096 && chunks < 16)) return {kWavefront, 1};
+  if (l.num_rows >= 4096 && chunks < 32) return {kTwoWavefronts, 1};
   const int64_t want = gnnshap::ceil_div(1024, std::max<int64_t>(l.num_rows, 1));
-  return {kWaves, static_cast<int>(std::min<int64_t>({gnnshap::ceil_div(chunks, kWaves), want, kMaxParts}))};
+  return {kWorkgroup, static_cast<int>(std::min<int64_t>({gnnshap::ceil_div(chunks, kWaves), want, kMaxParts,
+                                                          l.top ? kMaxPartKeys / l.top : kMaxParts}))};
 }
 
 size_t carve(LogprobArgs& a, void* ws) {
@@ -438,18 +575,23 @@ extern "C" int gnnshap_token_logprobs(const gnnshap_logits* l, int32_t* info, vo
   hipStream_t s = static_cast<hipStream_t>(stream);
   return gnnshap::with_dtype(l->dtype, [&](auto* p) {
     using T = std::remove_pointer_t<decltype(p)>;
-    const unsigned groups = static_cast<unsigned>(gnnshap::ceil_div(l->num_rows, kWaves));
+    const auto groups = [&](int rows) { return static_cast<unsigned>(gnnshap::ceil_div(l->num_rows, rows)); };
     {
       GS_TIMED("k_token_logprobs", s);
-      if (shape.per_row == 1)
-        k_token_logprobs<T, 1><<<groups, 64 * kWaves, 0, s>>>(a);
-      else
-        k_token_logprobs<T, kWaves><<<static_cast<unsigned>(l->num_rows * a.parts), 64 * kWaves, 0, s>>>(a);
+      switch (shape.way) {
+        case kShort64: k_token_logprobs_short<T, 16, 4><<<groups(16), 256, 0, s>>>(a); break;
+        case kShort256: k_token_logprobs_short<T, 64, 4><<<groups(4), 256, 0, s>>>(a); break;
+        case kShort1024: k_token_logprobs_short<T, 64, 16><<<groups(4), 256, 0, s>>>(a); break;
+        case kWavefront: k_token_logprobs<T, 1><<<groups(kWaves), 64 * kWaves, 0, s>>>(a); break;
+        case kTwoWavefronts: k_token_logprobs<T, 2><<<groups(kWaves / 2), 64 * kWaves, 0, s>>>(a); break;
+        case kWorkgroup:
+          k_token_logprobs<T, kWaves><<<static_cast<unsigned>(l->num_rows * a.parts), 64 * kWaves, 0, s>>>(a);
+      }
     }
     GS_LAUNCHED();
     if (a.parts > 1) {
       GS_TIMED("k_token_logprobs_join", s);
-      k_token_logprobs_join<T><<<groups, 64 * kWaves, 0, s>>>(a);
+      k_token_logprobs_join<T><<<static_cast<unsigned>(l->num_rows), 64 * kWaves, 0, s>>>(a);
       GS_LAUNCHED();
     }
     return static_cast<int>(GNNSHAP_OK);
