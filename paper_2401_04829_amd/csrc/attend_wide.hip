@@ -2,11 +2,14 @@
 // coalition's new token, times the query heads of a kv head, against the same
 // keys.
 //
-// It is a matrix product with a softmax inside, bound by the matrix
-// instructions and, beside them, by the exponentials (one per query and key).
-// A workgroup takes 128 queries, a wavefront 32 of them, over all keys of a
-// split in tiles of 64, staged in LDS twice: while a tile is multiplied, the
-// next one is on its way from the cache to registers.
+// It is a matrix product with a softmax inside, bound by the vector
+// instructions of the softmax (one exponential per query and key among them)
+// and, beside them, by the matrix instructions.  A workgroup takes 128
+// queries, a wavefront 32 of them, over all keys of a split in tiles of 64 (32
+// where a head is wider than 128), staged in LDS twice.  A step multiplies the
+// next tile's keys while it weighs this tile's scores, so that the two kinds
+// of instructions run side by side, then this tile's values, while the tiles
+// after come from the cache to registers.
 //
 // The layout is the transposed one of the other kernels on 32 x 32 x 16
 // instructions: S^T = K Q^T leaves query = lane % 32 and keys in registers,
@@ -31,20 +34,22 @@ using namespace gnnshap;
 typedef float f16v_t __attribute__((ext_vector_type(16)));
 typedef unsigned u2_t __attribute__((ext_vector_type(2)));
 
-constexpr int kTile = 64;      // keys of a step
 constexpr int kQueries = 128;  // queries of a workgroup
+constexpr int kAhead = 4;      // tiles whose keys' offsets are in LDS
 
 template <class T, int DP>
 struct Wide {
   typedef T vec8 __attribute__((ext_vector_type(8)));
+  static constexpr int kTile = DP <= 128 ? 64 : 32;  // keys of a step
+  static constexpr int NK = kTile / 32;       // tiles of S^T
   static constexpr int NT = DP / 32;          // tiles of O^T, elements on end of a lane
   static constexpr int KS = DP / 16;          // steps of K Q^T
   static constexpr int kPieces = DP / 8;      // 16-byte pieces of a key's row
-  static constexpr int kKeyLoads = kPieces / 4;         // of a thread, per tile
+  static constexpr int kKeyLoads = kTile * kPieces / 256;  // of a thread, per tile
   static constexpr int kValElems = DP >= 128 ? 8 : 4;   // elements on end that a thread turns over, of four keys
   static constexpr int kValPieces = DP / kValElems;
   static constexpr int kValLoads = kTile / 4 * kValPieces / 256;  // times four keys
-  static constexpr int kKeyBytes = kTile * DP * 2, kBufBytes = 2 * kKeyBytes;
+  static constexpr int kBytes = kTile * DP * 2;  // of a tile's keys or values: LDS holds two of each
 
   static __device__ __forceinline__ f16v_t mfma(u4_t a, u4_t b, f16v_t c) {
     if constexpr (std::is_same_v<T, bf16_t>)
@@ -52,12 +57,12 @@ struct Wide {
     else
       return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(vec8, a), __builtin_bit_cast(vec8, b), c, 0, 0, 0);
   }
-  // Byte of 16-byte piece p of key row r, and of the values' row of element d.
+  // Byte of 16-byte piece p of key row r, and of the values' row r of product tile t.
   static __device__ __forceinline__ int key_at(int r, int p) {
     return r * DP * 2 + ((p ^ (DP >= 128 ? r & 15 : (r >> 1) & 7)) << 4);
   }
   static __device__ __forceinline__ int val_at(int r, int t, int p) {
-    return kKeyBytes + (32 * t + r) * kTile * 2 + ((p ^ ((r >> 1) & 7)) << 4);
+    return 2 * kBytes + (32 * t + r) * kTile * 2 + ((p ^ (kTile == 64 ? (r >> 1) & 7 : (r >> 2) & 3)) << 4);
   }
   // 8-byte place of the four keys 4 c on in a values' row: the order of the weights' registers.
   static __device__ __forceinline__ int quad_place(int c) {
@@ -68,30 +73,33 @@ struct Wide {
   u4_t key[kKeyLoads];
   unsigned val[kValLoads][4][kValElems / 2];
 
-  // A tile on its way to registers; offsets: the byte of each key's (and
-  // value's) first element.  Elements behind head_dim are read as others of the
-  // row: the queries hold 0 there, and the results are not written.
-  __device__ __forceinline__ void load(const AttendArgs& a, const int64_t* offsets) {
-    const int tid = threadIdx.x, D = a.c.head_dim;
-    const char* const k = static_cast<const char*>(a.c.k) + (8 * (tid % kPieces) < D ? 16 * (tid % kPieces) : 0);
+  // A tile's keys, or values, on their way to registers; offsets: the byte of
+  // each one's first element.  Elements behind head_dim are read as others of
+  // the row: the queries hold 0 there, and the results are not written.
+  __device__ __forceinline__ void load_keys(const AttendArgs& a, const int64_t* offsets) {
+    const int tid = threadIdx.x;
+    const char* const k = static_cast<const char*>(a.c.k) + (8 * (tid % kPieces) < a.c.head_dim ? 16 * (tid % kPieces) : 0);
 #pragma unroll
     for (int i = 0; i < kKeyLoads; ++i)
       __builtin_memcpy(&key[i], k + offsets[tid / kPieces + i * (256 / kPieces)], 16);
-    const int d = tid % kValPieces * kValElems;
-    const char* const v = static_cast<const char*>(a.c.v) + (d < D ? 2 * d : 0);
+  }
+  __device__ __forceinline__ void load_values(const AttendArgs& a, const int64_t* offsets) {
+    const int tid = threadIdx.x, d = tid % kValPieces * kValElems;
+    const char* const v = static_cast<const char*>(a.c.v) + (d < a.c.head_dim ? 2 * d : 0);
 #pragma unroll
     for (int i = 0; i < kValLoads; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         __builtin_memcpy(&val[i][j][0], v + offsets[4 * (tid / kValPieces + i * (256 / kValPieces)) + j], 2 * kValElems);
   }
-  __device__ __forceinline__ void store(char* buf) const {
+  __device__ __forceinline__ void store_keys(char* buf) const {
     const int tid = threadIdx.x;
 #pragma unroll
-    for (int i = 0; i < kKeyLoads; ++i) {
-      const int r = tid / kPieces + i * (256 / kPieces), p = tid % kPieces;
-      *reinterpret_cast<u4_t*>(buf + key_at(r, p)) = key[i];
-    }
+    for (int i = 0; i < kKeyLoads; ++i)
+      *reinterpret_cast<u4_t*>(buf + key_at(tid / kPieces + i * (256 / kPieces), tid % kPieces)) = key[i];
+  }
+  __device__ __forceinline__ void store_values(char* buf) const {
+    const int tid = threadIdx.x;
 #pragma unroll
     for (int i = 0; i < kValLoads; ++i) {
       const int c = tid / kValPieces + i * (256 / kValPieces), d = tid % kValPieces * kValElems, at = quad_place(c);
@@ -127,10 +135,10 @@ struct WideState {
     }
     return c;
   }
-  // The weights of N tiles' scores, in place, after the running maximum has
-  // risen to theirs (or stays up to 2^8 below: O is scaled down less often).
+  // Raises the running maximum to that of the scores (or leaves it up to 2^8
+  // below: O is scaled down less often).
   template <int N>
-  __device__ __forceinline__ void weigh(f16v_t (&s)[N], float scale) {
+  __device__ __forceinline__ void raise(const f16v_t (&s)[N], float scale) {
     float top = s[0][0];
 #pragma unroll
     for (int n = 0; n < N; ++n)
@@ -144,33 +152,51 @@ struct WideState {
 #pragma unroll
       for (int t = 0; t < W::NT; ++t) o[t] *= down;
     }
-    const float use = m == -INFINITY ? 0.f : m;
-#pragma unroll
-    for (int n = 0; n < N; ++n)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], scale, -use));
-        l += s[n][i];
-      }
   }
+  // A score's weight.
+  __device__ __forceinline__ float weight(float s, float scale, float use) {
+    const float w = __builtin_amdgcn_exp2f(fmaf(s, scale, -use));
+    l += w;
+    return w;
+  }
+  __device__ __forceinline__ float maximum() const { return m == -INFINITY ? 0.f : m; }
   // Eight of a tile's weights, rounded to the values' type: an operand of 16 keys.
-  static __device__ __forceinline__ u4_t operand(const f16v_t& s, int u) {
+  __device__ __forceinline__ u4_t operand(const f16v_t& s, int u, float scale, float use) {
     typename W::vec8 w;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) w[j] = static_cast<T>(s[8 * u + j]);
+    for (int j = 0; j < 8; ++j) w[j] = static_cast<T>(weight(s[8 * u + j], scale, use));
     return __builtin_bit_cast(u4_t, w);
   }
 };
 
+// N matrix instructions mul(i, operand) whose LDS operands read(i) are read
+// kLead instructions ahead; the scheduler may move others between them, but
+// neither reads nor matrix instructions past each other.
+template <int N, class Read, class Mul>
+__device__ __forceinline__ void in_turn(Read read, Mul mul) {
+  constexpr int kLead = 6, kMayCross = 0x676;  // all but matrix instructions and LDS reads
+  u4_t x[kLead];
+#pragma unroll
+  for (int i = 0; i < kLead && i < N; ++i) x[i] = read(i);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_barrier(kMayCross);
+    mul(i, x[i % kLead]);
+    if (i + kLead < N) x[i % kLead] = read(i + kLead);
+  }
+  __builtin_amdgcn_sched_barrier(kMayCross);
+}
+
 template <class T, int DP>
 __global__ __launch_bounds__(64 * kWaves, DP <= 128 ? 2 : 1) void k_cache_attend_wide(AttendArgs a, Part part) {
   using W = Wide<T, DP>;
+  constexpr int kTile = W::kTile, NK = W::NK;
   extern __shared__ char room[];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, r = lane & 31, h = lane >> 5;
   const int D = a.c.head_dim;
   const Place at = place_of(a, part, false);
   if (at.k0 >= at.k1 && !a.direct && !at.with_own) return;
-  int64_t(*offsets)[kTile] = reinterpret_cast<int64_t(*)[kTile]>(room + 2 * W::kBufBytes);  // of three tiles
+  int64_t(*offsets)[kTile] = reinterpret_cast<int64_t(*)[kTile]>(room + 4 * W::kBytes);
 
   const int n_queries = part.r * a.share, q0 = at.tile * kQueries + wave * 32, qi = q0 + r, qs = qi < n_queries ? qi : 0;
   const int64_t row = at.group * part.r + qs / a.share;
@@ -191,89 +217,99 @@ __global__ __launch_bounds__(64 * kWaves, DP <= 128 ? 2 : 1) void k_cache_attend
   }
   WideState<T, DP> st;
 
-  // A step's page of this thread's key (of the first wavefront), and its offset.
+  // The page of this lane's key of a tile, and that key's offset.
+  const int key_lane = lane & (kTile - 1);
   const auto page_id = [&](int k) {
     int slot;
-    const int pg = page_of(a, min(k + lane, at.k1 - 1), slot);
+    const int pg = page_of(a, min(k + key_lane, at.k1 - 1), slot);
     return part.table[at.group * part.width + pg];
   };
   const auto put_offset = [&](int k, int page, int64_t* to) {
     int slot;
-    page_of(a, min(k + lane, at.k1 - 1), slot);
+    page_of(a, min(k + key_lane, at.k1 - 1), slot);
     if (page < 0 || page >= a.c.num_pages) {
       if (a.info) *a.info = 1;
       page = 0;
     }
-    to[lane] = 2 * (page * a.c.page_stride + slot * a.c.slot_stride + static_cast<int64_t>(at.kv_head) * a.c.head_stride);
+    to[key_lane] = 2 * (page * a.c.page_stride + slot * a.c.slot_stride + static_cast<int64_t>(at.kv_head) * a.c.head_stride);
   };
-  // The mask bits of positions k .. k + 63: two words of the row, of which the
-  // second is the next step's first.
+  // The mask bits of a tile's positions.  For 64 of them, two words of the row
+  // are shifted together, of which the second is the next tile's first.
   const uint64_t* const mask = a.q.masks + row * a.q.mask_words;
   const bool masked = a.q.num_players > 0;
-  const auto word_of = [&](int64_t i) {
-    return i >= 0 && i < (a.q.num_players + 63) >> 6 ? mask[i] : 0ull;
-  };
+  int64_t at_word = (at.first + at.k0) >> 6;
   const int shift = static_cast<int>((at.first + at.k0) & 63);
-  const auto bits_of = [&](int k, uint64_t lo, uint64_t hi) {
-    const int64_t p = at.first + k, n = a.q.num_players - p;  // players before position k: -p
-    uint64_t bits = shift ? lo >> shift | hi << (64 - shift) : lo;
-    if (p < 0) bits |= p <= -64 ? ~0ull : (1ull << -p) - 1;
-    if (n < 64) bits |= n <= 0 ? ~0ull : ~0ull << n;
-    if (!masked) bits = ~0ull;
+  const auto word = [&]() {
+    const int64_t i = at_word++;
+    return masked && i >= 0 && i < (a.q.num_players + 63) >> 6 ? mask[i] : 0ull;
+  };
+  uint64_t lo = 0, hi = 0;
+  const auto bits_of = [&](int k) {
     const int left = at.k1 - k;
-    return left >= 64 ? bits : bits & ((1ull << left) - 1);
+    uint64_t bits = ~0ull;
+    if (masked) {
+      const int64_t p = at.first + k, n = a.q.num_players - p;  // p < 0: before the players; n: players from here on
+      if constexpr (NK == 2) {
+        bits = shift ? lo >> shift | hi << (64 - shift) : lo;
+        if (p < 0) bits |= p <= -64 ? ~0ull : (1ull << -p) - 1;
+        if (n < 64) bits |= n <= 0 ? ~0ull : ~0ull << n;
+      } else {
+        bits = seen(mask, p, a.q.num_players);
+      }
+    }
+    return left >= 64 ? bits : left <= 0 ? 0ull : bits & ((1ull << left) - 1);
   };
 
   if (at.k0 < at.k1) {
     const int steps = (at.k1 - at.k0 + kTile - 1) / kTile;
-    int page = 0;
-    if (wave == 0) {
-      put_offset(at.k0, page_id(at.k0), offsets[0]);
-      put_offset(at.k0 + kTile, page_id(at.k0 + kTile), offsets[1]);
-      page = page_id(at.k0 + 2 * kTile);
-    }
-    int64_t at_word = (at.first + at.k0) >> 6;
-    uint64_t lo = masked ? word_of(at_word) : 0ull, hi = masked ? word_of(at_word + 1) : 0ull;
+    // wavefront w finds out where the keys of tiles w, w + 4, ... are
+    put_offset(at.k0 + wave * kTile, page_id(at.k0 + wave * kTile), offsets[wave]);
+    int page = page_id(at.k0 + (wave + kAhead) * kTile);
+    lo = word();
+    hi = word();
     __syncthreads();
     W next;
-    next.load(a, offsets[0]);
-    next.store(room);
+    next.load_keys(a, offsets[0]);
+    next.load_values(a, offsets[0]);
+    next.store_keys(room);
+    next.store_values(room);
     __syncthreads();
-    int third = 2;  // of the tile after the next
     for (int i = 0; i < steps; ++i) {
-      const int k = at.k0 + i * kTile;
-      const char* buf = room + (i & 1) * W::kBufBytes;
-      const bool more = i + 1 < steps;
-      if (more) next.load(a, offsets[third == 0 ? 2 : third - 1]);
-      const uint64_t bits = bits_of(k, lo, hi);
+      if (i + 1 < steps) {
+        next.load_keys(a, offsets[(i + 1) & 3]);
+        next.load_values(a, offsets[(i + 1) & 3]);
+      }
+      const uint64_t bits = bits_of(at.k0 + i * kTile);
       lo = hi;
-      ++at_word;
-      if (masked && more) hi = word_of(at_word + 1);
-      if (wave == 0 && i + 2 < steps) {
-        put_offset(k + 2 * kTile, page, offsets[third]);
-        page = page_id(k + 3 * kTile);
+      hi = word();
+      if (wave == (i & 3)) {  // tile i's offsets have been read
+        put_offset(at.k0 + (i + kAhead) * kTile, page, offsets[wave]);
+        page = page_id(at.k0 + (i + 2 * kAhead) * kTile);
       }
-      third = third == 2 ? 0 : third + 1;
-      f16v_t s[2];
+      const char* buf = room + (i & 1) * W::kBytes;
+      f16v_t s[NK];
 #pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        const uint32_t half = static_cast<uint32_t>(n ? bits >> 32 : bits);
-        s[n] = __ballot(half != ~0u) ? WideState<T, DP>::unseen(half) : f16v_t{};
+      for (int n = 0; n < NK; ++n) s[n] = WideState<T, DP>::unseen(static_cast<uint32_t>(n ? bits >> 32 : bits));
+      in_turn<NK * W::KS>(
+          [&](int x) { return *reinterpret_cast<const u4_t*>(buf + W::key_at(32 * (x % NK) + r, 2 * (x / NK) + h)); },
+          [&](int x, u4_t k) { s[x % NK] = W::mfma(k, q[x / NK], s[x % NK]); });
+      st.raise(s, scale);
+      u4_t p[NK][2];
+      const float use = st.maximum();
 #pragma unroll
-        for (int j = 0; j < W::KS; ++j)
-          s[n] = W::mfma(*reinterpret_cast<const u4_t*>(buf + W::key_at(32 * n + r, 2 * j + h)), q[j], s[n]);
+      for (int n = 0; n < NK; ++n)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) p[n][u] = st.operand(s[n], u, scale, use);
+      in_turn<NK * 2 * W::NT>(
+          [&](int x) { return *reinterpret_cast<const u4_t*>(buf + W::val_at(r, x % W::NT, 2 * (x / W::NT) + h)); },
+          [&](int x, u4_t v) {
+            const int u = x / W::NT, t = x % W::NT;
+            st.o[t] = W::mfma(v, p[u / 2][u % 2], st.o[t]);
+          });
+      if (i + 1 < steps) {
+        next.store_keys(room + ((i + 1) & 1) * W::kBytes);
+        next.store_values(room + ((i + 1) & 1) * W::kBytes);
       }
-      st.weigh(s, scale);
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const u4_t p = WideState<T, DP>::operand(s[n], u);
-#pragma unroll
-          for (int t = 0; t < W::NT; ++t)
-            st.o[t] = W::mfma(*reinterpret_cast<const u4_t*>(buf + W::val_at(r, t, 4 * n + 2 * u + h)), p, st.o[t]);
-        }
-      if (more) next.store(room + ((i + 1) & 1) * W::kBufBytes);
       __syncthreads();
     }
   }
@@ -303,10 +339,11 @@ __global__ __launch_bounds__(64 * kWaves, DP <= 128 ? 2 : 1) void k_cache_attend
           const int d = W::NT * r;
           if (x >= 0 && d < D) __builtin_memcpy(&v[u][j][0], static_cast<const T*>(a.c.v) + x + d, 2 * W::NT);
         }
-      st.weigh(s, scale);
+      st.raise(s, scale);
+      const float use = st.maximum();
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const u4_t p = WideState<T, DP>::operand(s[0], u);
+        const u4_t p = st.operand(s[0], u, scale, use);
 #pragma unroll
         for (int t = 0; t < W::NT; ++t) {
           u4_t x;
@@ -355,7 +392,7 @@ __global__ __launch_bounds__(64 * kWaves, DP <= 128 ? 2 : 1) void k_cache_attend
 template <class T, int DP>
 int launch(const AttendArgs& a, hipStream_t s) {
   const Part& p = a.shared;
-  const size_t bytes = 2 * Wide<T, DP>::kBufBytes + 3 * kTile * sizeof(int64_t);
+  const size_t bytes = 4 * Wide<T, DP>::kBytes + kAhead * Wide<T, DP>::kTile * sizeof(int64_t);
   const unsigned grid = static_cast<unsigned>(a.q.num_rows / p.r * a.c.kv_heads * p.tiles * p.splits);
   GS_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&k_cache_attend_wide<T, DP>),
                              hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)));
