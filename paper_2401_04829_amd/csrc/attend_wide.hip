@@ -5,11 +5,13 @@
 // It is a matrix product with a softmax inside, bound by the vector
 // instructions of the softmax (one exponential per query and key among them)
 // and, beside them, by the matrix instructions.  A workgroup takes 128
-// queries, a wavefront 32 of them, over all keys of a split in tiles of 64 (32
-// where a head is wider than 128), staged in LDS twice.  A step multiplies the
-// next tile's keys while it weighs this tile's scores, so that the two kinds
-// of instructions run side by side, then this tile's values, while the tiles
-// after come from the cache to registers.
+// queries, a wavefront 32 of them, over all keys of a split, 32 at a time.
+// While it weighs the scores of 32 keys it multiplies the next 32 keys, so
+// that the two kinds of instructions run side by side, then it adds up the
+// values of the 32 that it has weighed.  Keys and values come from the cache
+// to registers and from there to LDS in tiles of 64 (32 where a head is wider
+// than 128), one barrier per tile; keys are half a tile (a tile) further than
+// values.
 //
 // The layout is the transposed one of the other kernels on 32 x 32 x 16
 // instructions: S^T = K Q^T leaves query = lane % 32 and keys in registers,
@@ -57,7 +59,7 @@ struct Wide {
     else
       return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(vec8, a), __builtin_bit_cast(vec8, b), c, 0, 0, 0);
   }
-  // Byte of 16-byte piece p of key row r, and of the values' row r of product tile t.
+  // Byte of 16-byte piece p of key row r (of two tiles' keys), and of the values' row r of product tile t.
   static __device__ __forceinline__ int key_at(int r, int p) {
     return r * DP * 2 + ((p ^ (DP >= 128 ? r & 15 : (r >> 1) & 7)) << 4);
   }
@@ -73,48 +75,51 @@ struct Wide {
   u4_t key[kKeyLoads];
   unsigned val[kValLoads][4][kValElems / 2];
 
-  // A tile's keys, or values, on their way to registers; offsets: the byte of
-  // each one's first element.  Elements behind head_dim are read as others of
-  // the row: the queries hold 0 there, and the results are not written.
-  __device__ __forceinline__ void load_keys(const AttendArgs& a, const int64_t* offsets) {
+  // kTile keys from `from` on, or a tile's values, on their way to registers
+  // and then to LDS; offsets: the byte of each one's first element, for keys in
+  // a ring.  Elements behind head_dim are read as others of the row: the
+  // queries hold 0 there, and the results are not written.
+  // Each in kMoves moves, to go between other instructions.
+  static constexpr int kMoves = kKeyLoads + kValLoads * 4;
+  __device__ __forceinline__ void load(int move, const AttendArgs& a, const int64_t* offsets, int keys_from, int tile) {
     const int tid = threadIdx.x;
-    const char* const k = static_cast<const char*>(a.c.k) + (8 * (tid % kPieces) < a.c.head_dim ? 16 * (tid % kPieces) : 0);
-#pragma unroll
-    for (int i = 0; i < kKeyLoads; ++i)
-      __builtin_memcpy(&key[i], k + offsets[tid / kPieces + i * (256 / kPieces)], 16);
+    if (move < kKeyLoads) {
+      const char* const k = static_cast<const char*>(a.c.k) + (8 * (tid % kPieces) < a.c.head_dim ? 16 * (tid % kPieces) : 0);
+      const int r = keys_from + tid / kPieces + move * (256 / kPieces);
+      __builtin_memcpy(&key[move], k + offsets[r & (kAhead * kTile - 1)], 16);
+    } else {
+      const int i = (move - kKeyLoads) / 4, j = (move - kKeyLoads) % 4, d = tid % kValPieces * kValElems;
+      const char* const v = static_cast<const char*>(a.c.v) + (d < a.c.head_dim ? 2 * d : 0);
+      const int r = 4 * (tid / kValPieces + i * (256 / kValPieces)) + j;
+      __builtin_memcpy(&val[i][j][0], v + offsets[(tile & (kAhead - 1)) * kTile + r], 2 * kValElems);
+    }
   }
-  __device__ __forceinline__ void load_values(const AttendArgs& a, const int64_t* offsets) {
-    const int tid = threadIdx.x, d = tid % kValPieces * kValElems;
-    const char* const v = static_cast<const char*>(a.c.v) + (d < a.c.head_dim ? 2 * d : 0);
-#pragma unroll
-    for (int i = 0; i < kValLoads; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        __builtin_memcpy(&val[i][j][0], v + offsets[4 * (tid / kValPieces + i * (256 / kValPieces)) + j], 2 * kValElems);
-  }
-  __device__ __forceinline__ void store_keys(char* buf) const {
+  __device__ __forceinline__ void store(int move, char* room, int keys_from, int tile) const {
     const int tid = threadIdx.x;
-#pragma unroll
-    for (int i = 0; i < kKeyLoads; ++i)
-      *reinterpret_cast<u4_t*>(buf + key_at(tid / kPieces + i * (256 / kPieces), tid % kPieces)) = key[i];
-  }
-  __device__ __forceinline__ void store_values(char* buf) const {
-    const int tid = threadIdx.x;
-#pragma unroll
-    for (int i = 0; i < kValLoads; ++i) {
+    if (move < kKeyLoads) {
+      const int r = keys_from + tid / kPieces + move * (256 / kPieces);
+      *reinterpret_cast<u4_t*>(room + key_at(r & (2 * kTile - 1), tid % kPieces)) = key[move];
+    } else {
+      const int i = (move - kKeyLoads) / 4, part = (move - kKeyLoads) % 4;
       const int c = tid / kValPieces + i * (256 / kValPieces), d = tid % kValPieces * kValElems, at = quad_place(c);
 #pragma unroll
-      for (int e = 0; e < kValElems; ++e) {
+      for (int e = part * (kValElems / 4); e < (part + 1) * (kValElems / 4); ++e) {
         const unsigned sel = e & 1 ? 0x07060302u : 0x05040100u;
         const u2_t x = {__builtin_amdgcn_perm(val[i][1][e / 2], val[i][0][e / 2], sel),
                         __builtin_amdgcn_perm(val[i][3][e / 2], val[i][2][e / 2], sel)};
-        *reinterpret_cast<u2_t*>(buf + val_at((d + e) / NT, (d + e) % NT, at >> 1) + (at & 1) * 8) = x;
+        *reinterpret_cast<u2_t*>(room + (tile & 1) * kBytes + val_at((d + e) / NT, (d + e) % NT, at >> 1) + (at & 1) * 8) = x;
       }
     }
   }
 };
 
-// Tiles of 32 keys: their scores (the score of an unseen key is -inf).
+// The value that the lane 32 on or back has.
+__device__ __forceinline__ float other_half(float x) {
+  const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(threadIdx.x & 32 ? both[0] : both[1]);
+}
+
+// A query's running maximum and sum (this lane's half of it) and its column of O^T.
 template <class T, int DP>
 struct WideState {
   using W = Wide<T, DP>;
@@ -124,27 +129,17 @@ struct WideState {
 #pragma unroll
     for (int t = 0; t < W::NT; ++t) o[t] = f16v_t{};
   }
-  // The starting value of scores: -inf where the query does not see the key.
-  static __device__ __forceinline__ f16v_t unseen(uint32_t bits) {
-    f16v_t c;
-    const uint32_t off = ~bits >> (4 * (threadIdx.x >> 5 & 1));
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int bit = 8 * (i / 4) + i % 4;
-      c[i] = __uint_as_float(static_cast<uint32_t>(static_cast<int32_t>(off << (31 - bit)) >> 31) & 0xFF800000u);
-    }
-    return c;
+  // The starting value of a lane's i-th score: -inf where the query does not
+  // see the key; off: the unseen keys' bits, from the lane's first key on.
+  static __device__ __forceinline__ float unseen(uint32_t off, int i) {
+    const int bit = 8 * (i / 4) + i % 4;
+    return __uint_as_float(static_cast<uint32_t>(static_cast<int32_t>(off << (31 - bit)) >> 31) & 0xFF800000u);
   }
-  // Raises the running maximum to that of the scores (or leaves it up to 2^8
-  // below: O is scaled down less often).
-  template <int N>
-  __device__ __forceinline__ void raise(const f16v_t (&s)[N], float scale) {
-    float top = s[0][0];
-#pragma unroll
-    for (int n = 0; n < N; ++n)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
-    top = fmaxf(top, __shfl_xor(top, 32)) * scale;
+  static __device__ __forceinline__ uint32_t off_bits(uint32_t bits) { return ~bits >> (4 * (threadIdx.x >> 5 & 1)); }
+  // Raises the running maximum to `top`, this lane's largest score (or leaves
+  // it up to 2^8 below: O is scaled down less often).
+  __device__ __forceinline__ void raise(float top, float scale) {
+    top = fmaxf(top, other_half(top)) * scale;
     if (__ballot(top > m + 8.f)) {
       const float up = fmaxf(top, m), use = up == -INFINITY ? 0.f : up, down = __builtin_amdgcn_exp2f(m - use);
       m = up;
@@ -160,32 +155,14 @@ struct WideState {
     return w;
   }
   __device__ __forceinline__ float maximum() const { return m == -INFINITY ? 0.f : m; }
-  // Eight of a tile's weights, rounded to the values' type: an operand of 16 keys.
-  __device__ __forceinline__ u4_t operand(const f16v_t& s, int u, float scale, float use) {
+  // Eight weights, rounded to the values' type: an operand of 16 keys.
+  static __device__ __forceinline__ u4_t operand(const f16v_t& s, int u) {
     typename W::vec8 w;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) w[j] = static_cast<T>(weight(s[8 * u + j], scale, use));
+    for (int j = 0; j < 8; ++j) w[j] = static_cast<T>(s[8 * u + j]);
     return __builtin_bit_cast(u4_t, w);
   }
 };
-
-// N matrix instructions mul(i, operand) whose LDS operands read(i) are read
-// kLead instructions ahead; the scheduler may move others between them, but
-// neither reads nor matrix instructions past each other.
-template <int N, class Read, class Mul>
-__device__ __forceinline__ void in_turn(Read read, Mul mul) {
-  constexpr int kLead = 6, kMayCross = 0x676;  // all but matrix instructions and LDS reads
-  u4_t x[kLead];
-#pragma unroll
-  for (int i = 0; i < kLead && i < N; ++i) x[i] = read(i);
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    __builtin_amdgcn_sched_barrier(kMayCross);
-    mul(i, x[i % kLead]);
-    if (i + kLead < N) x[i % kLead] = read(i + kLead);
-  }
-  __builtin_amdgcn_sched_barrier(kMayCross);
-}
 
 template <class T, int DP>
 __global__ __launch_bounds__(64 * kWaves, DP <= 128 ? 2 : 1) void k_cache_attend_wide(AttendArgs a, Part part) {
@@ -196,7 +173,7 @@ __global__ __launch_bounds__(64 * kWaves, DP <= 128 ? 2 : 1) void k_cache_attend
   const int D = a.c.head_dim;
   const Place at = place_of(a, part, false);
   if (at.k0 >= at.k1 && !a.direct && !at.with_own) return;
-  int64_t(*offsets)[kTile] = reinterpret_cast<int64_t(*)[kTile]>(room + 4 * W::kBytes);
+  int64_t* const offsets = reinterpret_cast<int64_t*>(room + 4 * W::kBytes);  // of kAhead tiles
 
   const int n_queries = part.r * a.share, q0 = at.tile * kQueries + wave * 32, qi = q0 + r, qs = qi < n_queries ? qi : 0;
   const int64_t row = at.group * part.r + qs / a.share;
@@ -263,55 +240,114 @@ __global__ __launch_bounds__(64 * kWaves, DP <= 128 ? 2 : 1) void k_cache_attend
   if (at.k0 < at.k1) {
     const int steps = (at.k1 - at.k0 + kTile - 1) / kTile;
     // wavefront w finds out where the keys of tiles w, w + 4, ... are
-    put_offset(at.k0 + wave * kTile, page_id(at.k0 + wave * kTile), offsets[wave]);
+    put_offset(at.k0 + wave * kTile, page_id(at.k0 + wave * kTile), offsets + wave * kTile);
     int page = page_id(at.k0 + (wave + kAhead) * kTile);
     lo = word();
     hi = word();
+    const auto cover = [&](f16v_t& to, int first, int n, uint32_t which) {
+      const uint32_t off = WideState<T, DP>::off_bits(which);
+#pragma unroll
+      for (int i = first; i < first + n; ++i) to[i] = WideState<T, DP>::unseen(off, i);
+    };
     __syncthreads();
     W next;
-    next.load_keys(a, offsets[0]);
-    next.load_values(a, offsets[0]);
-    next.store_keys(room);
-    next.store_values(room);
+#pragma unroll
+    for (int x = 0; x < W::kMoves; ++x) next.load(x, a, offsets, 0, 0);
+#pragma unroll
+    for (int x = 0; x < W::kMoves; ++x) next.store(x, room, 0, 0);
+#pragma unroll
+    for (int x = 0; x < W::kKeyLoads; ++x) next.load(x, a, offsets, 32, 0);
+#pragma unroll
+    for (int x = 0; x < W::kKeyLoads; ++x) next.store(x, room, 32, 0);
     __syncthreads();
-    for (int i = 0; i < steps; ++i) {
-      if (i + 1 < steps) {
-        next.load_keys(a, offsets[(i + 1) & 3]);
-        next.load_values(a, offsets[(i + 1) & 3]);
-      }
-      const uint64_t bits = bits_of(at.k0 + i * kTile);
+    f16v_t s[2];  // scores of 32 keys, and of the next 32: unseen ones -inf before the others are there
+    const uint64_t bits = bits_of(at.k0);
+    cover(s[0], 0, 16, static_cast<uint32_t>(bits));
+    cover(s[1], 0, 16, static_cast<uint32_t>(NK == 2 ? bits >> 32 : bits_of(at.k0 + kTile)));
+#pragma unroll
+    for (int j = 0; j < W::KS; ++j) s[0] = W::mfma(*reinterpret_cast<const u4_t*>(room + W::key_at(r, 2 * j + h)), q[j], s[0]);
+    float top = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) top = fmaxf(top, s[0][x]);
+    st.raise(top, scale);
+
+    // A step: NK times KS products of the keys after, beside which the scores
+    // are weighed, and 2 NT of the values, beside which the scores after are
+    // looked through and those after them begun.  Their LDS operands are one
+    // sequence, read kLead products ahead; the scheduler may move no vector
+    // instruction, read or product out of its turn.
+    constexpr int kHalf = W::KS + 2 * W::NT, kProducts = NK * kHalf, kLead = 6, kMayCross = 0x274;
+    const auto step = [&](int i, auto odd) {
+      constexpr int kOdd = decltype(odd)::value;
+      const auto operand = [&](int x) {
+        const int n = x / kHalf, j = x % kHalf;
+        const char* at_x = room + (j < W::KS ? W::key_at((kTile * kOdd + 32 * (n + 1) + r) & (2 * kTile - 1), 2 * j + h)
+                                             : kOdd * W::kBytes + W::val_at(r, (j - W::KS) % W::NT,
+                                                                            4 * n + 2 * ((j - W::KS) / W::NT) + h));
+        return *reinterpret_cast<const u4_t*>(at_x);
+      };
+      u4_t lead[kLead];
+#pragma unroll
+      for (int x = 0; x < kLead; ++x) lead[x] = operand(x);
       lo = hi;
       hi = word();
-      if (wave == (i & 3)) {  // tile i's offsets have been read
-        put_offset(at.k0 + (i + kAhead) * kTile, page, offsets[wave]);
+      if (wave == (i & (kAhead - 1))) {  // tile i's offsets have been read
+        put_offset(at.k0 + (i + kAhead) * kTile, page, offsets + wave * kTile);
         page = page_id(at.k0 + (i + 2 * kAhead) * kTile);
       }
-      const char* buf = room + (i & 1) * W::kBytes;
-      f16v_t s[NK];
+      const uint64_t later = bits_of(at.k0 + i * kTile + 64);  // behind the last key: none
+      float use = st.maximum();
+      u4_t p[2];
 #pragma unroll
-      for (int n = 0; n < NK; ++n) s[n] = WideState<T, DP>::unseen(static_cast<uint32_t>(n ? bits >> 32 : bits));
-      in_turn<NK * W::KS>(
-          [&](int x) { return *reinterpret_cast<const u4_t*>(buf + W::key_at(32 * (x % NK) + r, 2 * (x / NK) + h)); },
-          [&](int x, u4_t k) { s[x % NK] = W::mfma(k, q[x / NK], s[x % NK]); });
-      st.raise(s, scale);
-      u4_t p[NK][2];
-      const float use = st.maximum();
+      for (int x = 0; x < kProducts; ++x) {
+        const int n = x / kHalf, j = x % kHalf;
+        f16v_t& now = s[NK == 2 ? n : kOdd];
+        f16v_t& then = s[NK == 2 ? 1 - n : 1 - kOdd];
+        __builtin_amdgcn_sched_barrier(kMayCross);
+        if (j < W::KS) {
+          then = W::mfma(lead[x % kLead], q[j], then);
+        } else {
+          if (j == W::KS) {
+            p[0] = WideState<T, DP>::operand(now, 0);
+            p[1] = WideState<T, DP>::operand(now, 1);
+            top = -INFINITY;
+          }
+          const int v = j - W::KS;
+          st.o[v % W::NT] = W::mfma(lead[x % kLead], p[v / W::NT], st.o[v % W::NT]);
+        }
+        if (x + kLead < kProducts) lead[x % kLead] = operand(x + kLead);
+        // the tile after (behind the last one: the last key again) from the
+        // cache in the first products, to LDS in the last ones
+        if (x < W::kMoves) next.load(x, a, offsets, i * kTile + kTile + 32, i + 1);
+        if (x >= kProducts - W::kMoves) next.store(x - (kProducts - W::kMoves), room, kTile * kOdd + kTile + 32, kOdd + 1);
+        if (j < W::KS) {
+          constexpr int kPart = 16 / W::KS;
 #pragma unroll
-      for (int n = 0; n < NK; ++n)
+          for (int e = 0; e < kPart; ++e) now[kPart * j + e] = st.weight(now[kPart * j + e], scale, use);
+        } else {
+          constexpr int kPart = 16 / W::NT;
+          const int v = j - W::KS;
+          if (v < W::NT) {
+            cover(now, v * kPart, kPart, static_cast<uint32_t>(n ? later >> 32 : later));  // for the keys after the next
+          } else {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) p[n][u] = st.operand(s[n], u, scale, use);
-      in_turn<NK * 2 * W::NT>(
-          [&](int x) { return *reinterpret_cast<const u4_t*>(buf + W::val_at(r, x % W::NT, 2 * (x / W::NT) + h)); },
-          [&](int x, u4_t v) {
-            const int u = x / W::NT, t = x % W::NT;
-            st.o[t] = W::mfma(v, p[u / 2][u % 2], st.o[t]);
-          });
-      if (i + 1 < steps) {
-        next.store_keys(room + ((i + 1) & 1) * W::kBytes);
-        next.store_values(room + ((i + 1) & 1) * W::kBytes);
+            for (int e = 0; e < kPart; ++e) top = fmaxf(top, then[(v - W::NT) * kPart + e]);
+          }
+        }
+        if (j == kHalf - 1) {
+          __builtin_amdgcn_sched_barrier(kMayCross);
+          st.raise(top, scale);
+          use = st.maximum();
+        }
       }
       __syncthreads();
+    };
+    int i = 0;
+    for (; i + 1 < steps; i += 2) {
+      step(i, std::integral_constant<int, 0>{});
+      step(i + 1, std::integral_constant<int, 1>{});
     }
+    if (i < steps) step(i, std::integral_constant<int, 0>{});
   }
 
   if (at.with_own) {
@@ -320,13 +356,16 @@ __global__ __launch_bounds__(64 * kWaves, DP <= 128 ? 2 : 1) void k_cache_attend
     const OwnTile own(a, part, at, q0, 32, len);
     for (int pass = 0; pass < own.passes; ++pass) {
       const int64_t mine = own.at(a, pass, r, at.kv_head);
-      f16v_t s[1] = {WideState<T, DP>::unseen(own.bits(a, pass, row, len, first))};
+      f16v_t s;
+      const uint32_t off = WideState<T, DP>::off_bits(own.bits(a, pass, row, len, first));
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = WideState<T, DP>::unseen(off, i);
 #pragma unroll
       for (int i = 0; i < W::KS; ++i) {
         u4_t k = {0u, 0u, 0u, 0u};
         if (mine >= 0 && 16 * i + 8 * h < D)
           __builtin_memcpy(&k, static_cast<const T*>(a.c.k) + mine + 16 * i + 8 * h, 16);
-        s[0] = W::mfma(k, q[i], s[0]);
+        s = W::mfma(k, q[i], s);
       }
       unsigned v[2][8][W::NT / 2];
 #pragma unroll
@@ -339,11 +378,16 @@ __global__ __launch_bounds__(64 * kWaves, DP <= 128 ? 2 : 1) void k_cache_attend
           const int d = W::NT * r;
           if (x >= 0 && d < D) __builtin_memcpy(&v[u][j][0], static_cast<const T*>(a.c.v) + x + d, 2 * W::NT);
         }
-      st.raise(s, scale);
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[i]);
+      st.raise(top, scale);
       const float use = st.maximum();
 #pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = st.weight(s[i], scale, use);
+#pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const u4_t p = st.operand(s[0], u, scale, use);
+        const u4_t p = st.operand(s, u);
 #pragma unroll
         for (int t = 0; t < W::NT; ++t) {
           u4_t x;
