@@ -55,14 +55,18 @@ __device__ __forceinline__ int page_of(const AttendArgs& a, int key, int& slot) 
   return p;
 }
 
-// The length of sequence `g` of a part, at most what its arrays hold.
-__device__ __forceinline__ int length_of(const AttendArgs& a, const Part& part, int64_t g) {
-  const int n = part.lengths[g];
+// A length as the caller's arrays can hold it.
+__device__ __forceinline__ int bounded(const AttendArgs& a, const Part& part, int n) {
   if (n < 0 || n > part.max_len) {
     if (a.info) *a.info = 1;
     return n < 0 ? 0 : part.max_len;
   }
   return n;
+}
+
+// The length of sequence `g` of a part.
+__device__ __forceinline__ int length_of(const AttendArgs& a, const Part& part, int64_t g) {
+  return bounded(a, part, part.lengths[g]);
 }
 
 // Which of the positions at .. at + 31 a row sees; `at` counts from the first player.
@@ -101,7 +105,7 @@ struct Place {  // what a workgroup works on
 // Decodes the workgroup's number.  Consecutive workgroups take consecutive kv
 // heads, so that those of one head, which read the same keys, meet in an
 // XCD's cache.
-__device__ __forceinline__ Place place_of(const AttendArgs& a, const Part& part, bool is_own) {
+__device__ __forceinline__ Place place_of(const AttendArgs& a, const Part& part) {
   Place at;
   int64_t b = blockIdx.x;
   at.kv_head = b % a.c.kv_heads;
@@ -110,14 +114,17 @@ __device__ __forceinline__ Place place_of(const AttendArgs& a, const Part& part,
   b /= part.splits;
   at.tile = b % part.tiles;
   at.group = b / part.tiles;
-  const int len = length_of(a, part, at.group);
   at.k0 = at.split * part.split_keys;
+  at.with_own = a.fused && at.split == 0;
+  return at;
+}
+
+// The rest of it, which depends on the sequence's length.
+__device__ __forceinline__ void bound(const AttendArgs& a, const Part& part, Place& at, int len, bool is_own) {
   at.k1 = len - at.k0 < part.split_keys ? len : at.k0 + part.split_keys;
   if (at.k1 < at.k0) at.k1 = at.k0;
   at.first = -a.q.first_player;
   if (is_own && a.shared.table) at.first += length_of(a, a.shared, at.group / a.shared.r);
-  at.with_own = a.fused && at.split == 0;
-  return at;
 }
 
 // The split's pages into LDS, from that of its first key on.
@@ -151,18 +158,20 @@ __device__ __forceinline__ int64_t token_at(const AttendArgs& a, const Part& par
 struct OwnTile {
   int64_t row0;  // first row
   int rows, per;
-  int passes;
-  // q0: the tile's first query; n of the group's queries at most
-  __device__ __forceinline__ OwnTile(const AttendArgs& a, const Part& part, const Place& at, int q0, int size, int len) {
+  // q0: the tile's first query; size: how many it has
+  __device__ __forceinline__ OwnTile(const AttendArgs& a, const Part& part, const Place& at, int q0, int size) {
     const int n = part.r * a.share, q1 = q0 + size - 1 < n - 1 ? q0 + size - 1 : n - 1;
     const int r0 = q0 / a.share;
     row0 = at.group * part.r + r0;
     rows = q0 < n ? q1 / a.share - r0 + 1 : 0;
     per = rows > 0 ? kChunk / rows : 1;
+  }
+  // Passes that the lanes' rows take, of `len` own tokens.
+  __device__ __forceinline__ int passes(int len) const {
     int most = rows > 0 ? len : 0;
 #pragma unroll
     for (int off = 1; off < 64; off *= 2) most = max(most, __shfl_xor(most, off));
-    passes = (most + per - 1) / per;
+    return (most + per - 1) / per;
   }
   // Where the key in slot s of a pass is; -1: there is none.
   __device__ __forceinline__ int64_t at(const AttendArgs& a, int pass, int s, int kv_head) const {

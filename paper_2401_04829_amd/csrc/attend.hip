@@ -193,7 +193,8 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_attend(AttendArgs a, Part
   extern __shared__ int lds[];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, r = lane & 15, g = lane >> 4;
   const int D = a.c.head_dim;
-  const Place at = place_of(a, part, IS_OWN);
+  Place at = place_of(a, part);
+  bound(a, part, at, length_of(a, part, at.group), IS_OWN);
   if (at.k0 >= at.k1 && !a.direct && !at.with_own) return;
   const int page0 = at.k0 / a.c.page_size;
   int* pages = lds;
@@ -245,8 +246,9 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_attend(AttendArgs a, Part
     for (int t = 0; t < RT; ++t) {
       if (!BY_QUERY && t % kWaves != wave) continue;
       const int len = length_of(a, a.own, row[t]);
-      const OwnTile own(a, part, at, q0 + t * 16, 16, len);
-      for (int p = 0; p < own.passes; ++p) {
+      const OwnTile own(a, part, at, q0 + t * 16, 16);
+      const int passes = own.passes(len);
+      for (int p = 0; p < passes; ++p) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int64_t x = own.at(a, p, 16 * i + r, at.kv_head);

@@ -171,8 +171,10 @@ __global__ __launch_bounds__(64 * kWaves, DP <= 128 ? 2 : 1) void k_cache_attend
   extern __shared__ char room[];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, r = lane & 31, h = lane >> 5;
   const int D = a.c.head_dim;
-  const Place at = place_of(a, part, false);
-  if (at.k0 >= at.k1 && !a.direct && !at.with_own) return;
+  // The first loads of all chains (queries; lengths, pages, then keys and
+  // values, of the shared part and of the rows' own) before anything waits.
+  Place at = place_of(a, part);
+  const int raw_len = part.lengths[at.group];
   int64_t* const offsets = reinterpret_cast<int64_t*>(room + 4 * W::kBytes);  // of kAhead tiles
 
   const int n_queries = part.r * a.share, q0 = at.tile * kQueries + wave * 32, qi = q0 + r, qs = qi < n_queries ? qi : 0;
@@ -180,35 +182,54 @@ __global__ __launch_bounds__(64 * kWaves, DP <= 128 ? 2 : 1) void k_cache_attend
   const int head = at.kv_head * a.share + qs % a.share;
   const float scale = fabsf(a.scale2);
   u4_t q[W::KS];
-  {
-    const T* p = static_cast<const T*>(a.q.q) + row * a.q.q_row_stride + head * a.q.q_head_stride;
-    const unsigned flip = a.scale2 < 0.f ? 0x80008000u : 0u;
 #pragma unroll
-    for (int i = 0; i < W::KS; ++i) {
-      const int d = 16 * i + 8 * h;
-      q[i] = u4_t{0u, 0u, 0u, 0u};
-      if (d < D) __builtin_memcpy(&q[i], p + d, 16);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) q[i][e] ^= flip;
-    }
+  for (int i = 0; i < W::KS; ++i) {
+    const int d = 16 * i + 8 * h;
+    q[i] = u4_t{0u, 0u, 0u, 0u};
+    if (d < D)
+      __builtin_memcpy(&q[i], static_cast<const T*>(a.q.q) + row * a.q.q_row_stride + head * a.q.q_head_stride + d, 16);
   }
-  WideState<T, DP> st;
-
-  // The page of this lane's key of a tile, and that key's offset.
+  // The page of this lane's key of a tile (behind the part's last one some page of the row).
   const int key_lane = lane & (kTile - 1);
   const auto page_id = [&](int k) {
     int slot;
-    const int pg = page_of(a, min(k + key_lane, at.k1 - 1), slot);
-    return part.table[at.group * part.width + pg];
+    const int pg = page_of(a, min(k + key_lane, part.max_len - 1), slot);
+    return part.max_len > 0 ? part.table[at.group * part.width + pg] : 0;
   };
-  const auto put_offset = [&](int k, int page, int64_t* to) {
+  const int page0 = page_id(at.k0 + wave * kTile);
+  int page = page_id(at.k0 + (wave + kAhead) * kTile);
+  // The own token of this lane's slot in the first pass.
+  const OwnTile own(a, part, at, q0, 32);
+  const int own_r = r / own.per, own_key = r - own_r * own.per;
+  const int64_t own_row = own.row0 + (own_r < own.rows ? own_r : 0);
+  int own_slot, own_page = -1, raw_own = 0, raw_slot = 0;
+  const int own_pg = page_of(a, own_key, own_slot);
+  if (at.with_own && own.rows > 0) {
+    raw_own = a.own.lengths[row];
+    raw_slot = a.own.lengths[own_row];
+    if (own_pg < a.own.width) own_page = a.own.table[own_row * a.own.width + own_pg];
+  }
+  bound(a, part, at, bounded(a, part, raw_len), false);
+  if (at.k0 >= at.k1 && !a.direct && !at.with_own) return;
+  if (a.scale2 < 0.f)
+#pragma unroll
+    for (int i = 0; i < W::KS; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) q[i][e] ^= 0x80008000u;
+  WideState<T, DP> st;
+
+  // The offset of this lane's key of a tile; behind the last key that of the
+  // tile's first one (in a tile of none any: nothing of it is used).
+  const auto put_offset = [&](int k, int id, int64_t* to) {
     int slot;
-    page_of(a, min(k + key_lane, at.k1 - 1), slot);
-    if (page < 0 || page >= a.c.num_pages) {
-      if (a.info) *a.info = 1;
-      page = 0;
-    }
-    to[key_lane] = 2 * (page * a.c.page_stride + slot * a.c.slot_stride + static_cast<int64_t>(at.kv_head) * a.c.head_stride);
+    page_of(a, min(k + key_lane, part.max_len - 1), slot);
+    if (k + key_lane < at.k1 && (id < 0 || id >= a.c.num_pages) && a.info) *a.info = 1;
+    if (id < 0 || id >= a.c.num_pages) id = 0;
+    const bool in = k + key_lane < at.k1;
+    const int first_id = __builtin_amdgcn_readfirstlane(id), first_slot = __builtin_amdgcn_readfirstlane(slot);
+    id = in ? id : first_id;
+    slot = in ? slot : first_slot;
+    to[key_lane] = 2 * (id * a.c.page_stride + slot * a.c.slot_stride + static_cast<int64_t>(at.kv_head) * a.c.head_stride);
   };
   // The mask bits of a tile's positions.  For 64 of them, two words of the row
   // are shifted together, of which the second is the next tile's first.
@@ -237,11 +258,72 @@ __global__ __launch_bounds__(64 * kWaves, DP <= 128 ? 2 : 1) void k_cache_attend
     return left >= 64 ? bits : left <= 0 ? 0ull : bits & ((1ull << left) - 1);
   };
 
+  // One pass over own tokens: `mine` is where that of this lane's slot is, or -1.
+  const auto own_pass = [&](int pass, int64_t mine, int len) {
+    const int64_t first = bounded(a, part, raw_len) - a.q.first_player;
+    f16v_t s;
+    const uint32_t off = WideState<T, DP>::off_bits(own.bits(a, pass, row, len, first));
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = WideState<T, DP>::unseen(off, i);
+#pragma unroll
+    for (int i = 0; i < W::KS; ++i) {
+      u4_t k = {0u, 0u, 0u, 0u};
+      if (mine >= 0 && 16 * i + 8 * h < D)
+        __builtin_memcpy(&k, static_cast<const T*>(a.c.k) + mine + 16 * i + 8 * h, 16);
+      s = W::mfma(k, q[i], s);
+    }
+    unsigned v[2][8][W::NT / 2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int64_t x = __shfl(mine, 16 * u + 8 * (j / 4) + 4 * h + j % 4);
+#pragma unroll
+        for (int e = 0; e < W::NT / 2; ++e) v[u][j][e] = 0u;
+        const int d = W::NT * r;
+        if (x >= 0 && d < D) __builtin_memcpy(&v[u][j][0], static_cast<const T*>(a.c.v) + x + d, 2 * W::NT);
+      }
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[i]);
+    st.raise(top, scale);
+    const float use = st.maximum();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = st.weight(s[i], scale, use);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const u4_t p = st.operand(s, u);
+#pragma unroll
+      for (int t = 0; t < W::NT; ++t) {
+        u4_t x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          x[j] = __builtin_amdgcn_perm(v[u][2 * j + 1][t / 2], v[u][2 * j][t / 2], t & 1 ? 0x07060302u : 0x05040100u);
+        st.o[t] = W::mfma(x, p, st.o[t]);
+      }
+    }
+  };
+  const auto own_passes = [&]() {
+    if (!at.with_own || own.rows == 0) return;
+    const int len = bounded(a, a.own, raw_own);
+    int64_t mine = -1;
+    if (own_r < own.rows && own_key < bounded(a, a.own, raw_slot)) {
+      if (own_page >= 0 && own_page < a.c.num_pages)
+        mine = own_page * a.c.page_stride + own_slot * a.c.slot_stride + static_cast<int64_t>(at.kv_head) * a.c.head_stride;
+      else if (a.info)
+        *a.info = 1;
+    }
+    const int passes = own.passes(len);
+    for (int pass = 0; pass < passes; ++pass) {
+      if (pass > 0) mine = own.at(a, pass, r, at.kv_head);
+      own_pass(pass, mine, len);
+    }
+  };
+
   if (at.k0 < at.k1) {
     const int steps = (at.k1 - at.k0 + kTile - 1) / kTile;
     // wavefront w finds out where the keys of tiles w, w + 4, ... are
-    put_offset(at.k0 + wave * kTile, page_id(at.k0 + wave * kTile), offsets + wave * kTile);
-    int page = page_id(at.k0 + (wave + kAhead) * kTile);
+    put_offset(at.k0 + wave * kTile, page0, offsets + wave * kTile);
     lo = word();
     hi = word();
     const auto cover = [&](f16v_t& to, int first, int n, uint32_t which) {
@@ -253,6 +335,7 @@ __global__ __launch_bounds__(64 * kWaves, DP <= 128 ? 2 : 1) void k_cache_attend
     W next;
 #pragma unroll
     for (int x = 0; x < W::kMoves; ++x) next.load(x, a, offsets, 0, 0);
+    own_passes();
 #pragma unroll
     for (int x = 0; x < W::kMoves; ++x) next.store(x, room, 0, 0);
 #pragma unroll
@@ -348,59 +431,11 @@ __global__ __launch_bounds__(64 * kWaves, DP <= 128 ? 2 : 1) void k_cache_attend
       step(i + 1, std::integral_constant<int, 1>{});
     }
     if (i < steps) step(i, std::integral_constant<int, 0>{});
+  } else {
+    own_passes();
   }
 
-  if (at.with_own) {
-    const int len = length_of(a, a.own, row);
-    const int64_t first = length_of(a, part, at.group) - a.q.first_player;
-    const OwnTile own(a, part, at, q0, 32, len);
-    for (int pass = 0; pass < own.passes; ++pass) {
-      const int64_t mine = own.at(a, pass, r, at.kv_head);
-      f16v_t s;
-      const uint32_t off = WideState<T, DP>::off_bits(own.bits(a, pass, row, len, first));
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = WideState<T, DP>::unseen(off, i);
-#pragma unroll
-      for (int i = 0; i < W::KS; ++i) {
-        u4_t k = {0u, 0u, 0u, 0u};
-        if (mine >= 0 && 16 * i + 8 * h < D)
-          __builtin_memcpy(&k, static_cast<const T*>(a.c.k) + mine + 16 * i + 8 * h, 16);
-        s = W::mfma(k, q[i], s);
-      }
-      unsigned v[2][8][W::NT / 2];
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int64_t x = __shfl(mine, 16 * u + 8 * (j / 4) + 4 * h + j % 4);
-#pragma unroll
-          for (int e = 0; e < W::NT / 2; ++e) v[u][j][e] = 0u;
-          const int d = W::NT * r;
-          if (x >= 0 && d < D) __builtin_memcpy(&v[u][j][0], static_cast<const T*>(a.c.v) + x + d, 2 * W::NT);
-        }
-      float top = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[i]);
-      st.raise(top, scale);
-      const float use = st.maximum();
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = st.weight(s[i], scale, use);
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const u4_t p = st.operand(s, u);
-#pragma unroll
-        for (int t = 0; t < W::NT; ++t) {
-          u4_t x;
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            x[j] = __builtin_amdgcn_perm(v[u][2 * j + 1][t / 2], v[u][2 * j][t / 2], t & 1 ? 0x07060302u : 0x05040100u);
-          st.o[t] = W::mfma(x, p, st.o[t]);
-        }
-      }
-    }
-  }
-
-  const float l = st.l + __shfl_xor(st.l, 32);
+  const float l = st.l + other_half(st.l);
   bool bad = false;
   if (qi < n_queries) {
     const int64_t p = part_index(a, part.slot0 + at.split, row, head);
