@@ -15,16 +15,16 @@ constexpr int kChunk = 32;  // keys of a wavefront's step
 
 // One part of the rows' contexts: `r` consecutive rows share each row of its
 // table.  A group's rows times the query heads of a kv head are its queries,
-// in tiles; a workgroup takes a tile over split_keys keys.
+// in tiles; a wavefront (a workgroup of the wide kernel) takes a tile over
+// split_keys keys.
 struct Part {
   const int32_t* table;
   const int32_t* lengths;
   int64_t width;
   int max_len;
   int r;
-  int tile;       // queries of a workgroup
+  int tile;       // queries
   int tiles;
-  bool by_query;  // its wavefronts take queries, not keys, in turn
   bool wide;      // the kernel of many 16-bit queries takes it
   int splits;
   int split_keys;
@@ -94,7 +94,7 @@ __device__ __forceinline__ T* out_of(const AttendArgs& a, int64_t row, int head)
 
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : m * kLn2 + logf(l); }
 
-struct Place {  // what a workgroup works on
+struct Place {  // what a wavefront or workgroup works on
   int64_t group;
   int kv_head, tile, split;
   int64_t first;  // context position of the part's position 0, counted from the first player
@@ -102,12 +102,13 @@ struct Place {  // what a workgroup works on
   bool with_own;  // the rows' own parts too
 };
 
-// Decodes the workgroup's number.  Consecutive workgroups take consecutive kv
-// heads, so that those of one head, which read the same keys, meet in an
-// XCD's cache.
-__device__ __forceinline__ Place place_of(const AttendArgs& a, const Part& part) {
+// Decodes the number of a workgroup or wavefront.  Consecutive ones take
+// consecutive kv heads: workgroups of one head, which read the same keys, then
+// meet in an XCD's cache, and the wavefronts of a workgroup read neighbouring
+// parts of the same tokens.
+__device__ __forceinline__ Place place_of(const AttendArgs& a, const Part& part, int64_t number) {
   Place at;
-  int64_t b = blockIdx.x;
+  int64_t b = number;
   at.kv_head = b % a.c.kv_heads;
   b /= a.c.kv_heads;
   at.split = b % part.splits;
@@ -125,20 +126,6 @@ __device__ __forceinline__ void bound(const AttendArgs& a, const Part& part, Pla
   if (at.k1 < at.k0) at.k1 = at.k0;
   at.first = -a.q.first_player;
   if (is_own && a.shared.table) at.first += length_of(a, a.shared, at.group / a.shared.r);
-}
-
-// The split's pages into LDS, from that of its first key on.
-__device__ __forceinline__ void stage_pages(const AttendArgs& a, const Part& part, const Place& at, int* pages) {
-  if (at.k1 <= at.k0) return;
-  const int page0 = at.k0 / a.c.page_size, n = (at.k1 - 1) / a.c.page_size - page0 + 1;
-  for (int i = threadIdx.x; i < n; i += 64 * kWaves) {
-    int p = part.table[at.group * part.width + page0 + i];
-    if (p < 0 || p >= a.c.num_pages) {
-      if (a.info) *a.info = 1;
-      p = 0;
-    }
-    pages[i] = p;
-  }
 }
 
 // Where token `key` of sequence `seq` of a part is, straight from the table; -1 if its page is out of range.
@@ -189,32 +176,28 @@ struct OwnTile {
   }
 };
 
-// The slow path: queries one after the other, a thread per key and then per
-// element; a position that the row does not see enters no product.
+// The slow path, by a wavefront for n of a group's queries from q0 on, one
+// after the other: a lane per key, then per four elements; a position that the
+// row does not see enters no product.
 template <class T>
-__device__ void attend_slowly(const AttendArgs& a, const Part& part, const Place& at, int queries, float* lds) {
-  const int tid = threadIdx.x, D = a.c.head_dim, wave = tid >> 6, lane = tid & 63;
-  float* weight = lds;       // 256
-  float* red = lds + 256;    // 2 x kWaves
-  for (int i = 0; i < queries; ++i) {
-    const int qi = at.tile * queries + i;
-    if (qi >= part.r * a.share) break;
-    const int64_t row = at.group * part.r + qi / a.share;
-    const int head = at.kv_head * a.share + qi % a.share;
+__device__ void attend_slowly(const AttendArgs& a, const Part& part, const Place& at, int q0, int n) {
+  const int lane = threadIdx.x & 63, D = a.c.head_dim;
+  for (int i = q0; i < q0 + n && i < part.r * a.share; ++i) {
+    const int64_t row = at.group * part.r + i / a.share;
+    const int head = at.kv_head * a.share + i % a.share;
     const T* q = static_cast<const T*>(a.q.q) + row * a.q.q_row_stride + head * a.q.q_head_stride;
-    float m = -INFINITY, l = 0.f, o = 0.f;
+    float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
     for (int own = 0; own < 2; ++own) {
       if (own && !at.with_own) break;
       const Part& p = own ? a.own : part;
       const int64_t seq = own ? row : at.group;
       const int k0 = own ? 0 : at.k0, k1 = own ? length_of(a, a.own, row) : at.k1;
       const int64_t first = own ? length_of(a, part, at.group) - a.q.first_player : at.first;
-      for (int c = k0; c < k1; c += 256) {
-        const int key = c + tid;
-        bool sees = key < k1;
+      for (int c = k0; c < k1; c += 64) {
+        bool sees = c + lane < k1;
         if (sees && a.q.num_players > 0)
-          sees = seen(a.q.masks + row * a.q.mask_words, first + key, a.q.num_players) & 1u;
-        const int64_t where = sees ? token_at(a, p, seq, key, at.kv_head) : -1;
+          sees = seen(a.q.masks + row * a.q.mask_words, first + c + lane, a.q.num_players) & 1u;
+        const int64_t where = sees ? token_at(a, p, seq, c + lane, at.kv_head) : -1;
         sees = where >= 0;
         float s = -INFINITY;
         if (sees) {
@@ -223,42 +206,38 @@ __device__ void attend_slowly(const AttendArgs& a, const Part& part, const Place
           for (int d = 0; d < D; ++d) s += static_cast<float>(q[d]) * static_cast<float>(k[d]);
           s *= a.scale2;
         }
-        float top = s;
+        float top = fmaxf(m, s);
         for (int off = 1; off < 64; off *= 2) top = fmaxf(top, __shfl_xor(top, off));
-        if (lane == 0) red[wave] = top;
-        __syncthreads();
-        top = m;
-        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, red[w]);
         const float use = top == -INFINITY ? 0.f : top;
-        const float e = sees ? __builtin_amdgcn_exp2f(s - use) : -1.f;
-        weight[tid] = e;
-        float sum = sees ? e : 0.f;
-        for (int off = 1; off < 64; off *= 2) sum += __shfl_xor(sum, off);
-        if (lane == 0) red[kWaves + wave] = sum;
-        __syncthreads();
         const float down = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - use);
-        l *= down;
-        for (int w = 0; w < kWaves; ++w) l += red[kWaves + w];
-        o = m == -INFINITY ? 0.f : o * down;
+        const float e = sees ? __builtin_amdgcn_exp2f(s - use) : 0.f;
+        float sum = e;
+        for (int off = 1; off < 64; off *= 2) sum += __shfl_xor(sum, off);
+        l = l * down + sum;
+        for (int x = 0; x < 4; ++x) o[x] = m == -INFINITY ? 0.f : o[x] * down;
         m = top;
-        if (tid < D) {
-          const int n = k1 - c < 256 ? k1 - c : 256;
-          for (int j = 0; j < n; ++j) {
-            const float w = weight[j];
-            if (w < 0.f) continue;
-            o += w * static_cast<float>(static_cast<const T*>(a.c.v)[token_at(a, p, seq, c + j, at.kv_head) + tid]);
-          }
+        for (uint64_t left = __ballot(sees); left; left &= left - 1) {
+          const int j = __builtin_ctzll(left);
+          const float w = __shfl(e, j);
+          const T* v = static_cast<const T*>(a.c.v) + __shfl(where, j) + 4 * lane;
+          if (4 * lane < D)
+            for (int x = 0; x < 4; ++x) o[x] += w * static_cast<float>(v[x]);
         }
-        __syncthreads();
       }
     }
-    if (a.direct) {
-      if (tid < D) out_of<T>(a, row, head)[tid] = static_cast<T>(l == 0.f ? 0.f : o / l);
-      if (tid == 0 && a.q.lse) a.q.lse[row * a.q.heads + head] = lse_of(m, l);
-    } else {
-      const int64_t p = part_index(a, part.slot0 + at.split, row, head);
-      if (tid < D) a.part_o[p * D + tid] = l == 0.f ? 0.f : o;
-      if (tid == 0) a.part_ml[p] = make_float2(m, l);
+    const int64_t p = part_index(a, part.slot0 + at.split, row, head);
+    if (4 * lane < D)
+      for (int x = 0; x < 4; ++x) {
+        if (a.direct)
+          out_of<T>(a, row, head)[4 * lane + x] = static_cast<T>(l == 0.f ? 0.f : o[x] / l);
+        else
+          a.part_o[p * D + 4 * lane + x] = l == 0.f ? 0.f : o[x];
+      }
+    if (lane == 0) {
+      if (!a.direct)
+        a.part_ml[p] = make_float2(m, l);
+      else if (a.q.lse)
+        a.q.lse[row * a.q.heads + head] = lse_of(m, l);
     }
   }
 }

@@ -179,32 +179,38 @@ struct State {
   }
 };
 
-enum { kOwnPart, kShared, kSharedByQuery };
-
-// A workgroup: one split of keys against RT tiles of 16 queries, its four
-// wavefronts taking chunks of 32 keys in turn and joined through LDS
-// (kSharedByQuery: against RT tiles of each wavefront, every wavefront taking all
-// chunks, nothing to join).
-template <class T, int DP, int RT, int MODE>
-__global__ __launch_bounds__(64 * kWaves) void k_cache_attend(AttendArgs a, Part part) {
+// A wavefront: RT tiles of 16 queries of one kv head over one split of keys, 32
+// at a time, the next ones on their way while these are multiplied (where the
+// registers hold both).
+template <class T, int DP, int RT, bool IS_OWN>
+__global__ __launch_bounds__(64 * kWaves) void k_cache_attend(AttendArgs a, Part part, int64_t places) {
   using O = Ops<T, DP>;
-  constexpr bool BY_QUERY = MODE == kSharedByQuery, IS_OWN = MODE == kOwnPart;
-  constexpr int kStride = DP + 4, kQueries = 16 * RT * (BY_QUERY ? kWaves : 1);
+  constexpr int kQueries = 16 * RT;
+  constexpr bool kPrefetch = DP * sizeof(T) <= 256;
   extern __shared__ int lds[];
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, r = lane & 15, g = lane >> 4;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
   const int D = a.c.head_dim;
-  Place at = place_of(a, part);
-  bound(a, part, at, length_of(a, part, at.group), IS_OWN);
-  if (at.k0 >= at.k1 && !a.direct && !at.with_own) return;
-  const int page0 = at.k0 / a.c.page_size;
-  int* pages = lds;
-  stage_pages(a, part, at, pages);
-  float* merge = reinterpret_cast<float*>(lds + ((part.split_keys / a.c.page_size + 2 + 3) & ~3));
+  const int64_t number = static_cast<int64_t>(blockIdx.x) * kWaves + wave;
+  if (number >= places) return;
+  Place at = place_of(a, part, number);
+  const int raw_len = part.lengths[at.group];
+
+  // the pages of the split, as many as there may be, and which of them is the first out of range
+  const int page0 = at.k0 / a.c.page_size, room = part.split_keys / a.c.page_size + 2;
+  const int last = min(at.k0 + part.split_keys, part.max_len) - 1, n_pages = last < at.k0 ? 0 : last / a.c.page_size - page0 + 1;
+  int* pages = lds + wave * room;
+  int first_bad = INT32_MAX;
+  for (int i = lane; i < n_pages; i += 64) {
+    const int p = part.table[at.group * part.width + page0 + i];
+    const bool in = p >= 0 && p < a.c.num_pages;
+    if (!in) first_bad = min(first_bad, i);
+    pages[i] = in ? p : 0;
+  }
 
   typename O::Row q[RT];
   int64_t row[RT];
   State<T, DP> st[RT];
-  const int q0 = at.tile * kQueries + (BY_QUERY ? wave * RT * 16 : 0), n_queries = part.r * a.share;
+  const int q0 = at.tile * kQueries, n_queries = part.r * a.share;
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     const int qi = q0 + t * 16 + r, qs = qi < n_queries ? qi : 0;
@@ -212,7 +218,10 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_attend(AttendArgs a, Part
     const int head = at.kv_head * a.share + qs % a.share;
     q[t].load(static_cast<const T*>(a.q.q) + row[t] * a.q.q_row_stride + head * a.q.q_head_stride, D);
   }
-  __syncthreads();
+  bound(a, part, at, bounded(a, part, raw_len), IS_OWN);
+  if (at.k0 >= at.k1 && !a.direct && !at.with_own) return;
+  if (at.k0 < at.k1 && first_bad <= (at.k1 - 1) / a.c.page_size - page0 && a.info) *a.info = 1;
+  __builtin_amdgcn_wave_barrier();
 
   const int64_t head_at = static_cast<int64_t>(at.kv_head) * a.c.head_stride;
   const T* const kbase = static_cast<const T*>(a.c.k);
@@ -223,20 +232,41 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_attend(AttendArgs a, Part
     const int pg = page_of(a, key, slot);
     return pages[pg - page0] * a.c.page_stride + slot * a.c.slot_stride + head_at;
   };
-  typename O::Row key[2];
-  typename O::Values val;
-  constexpr int kTurn = BY_QUERY ? kChunk : kWaves * kChunk;
-  for (int k = at.k0 + (BY_QUERY ? 0 : wave * kChunk); k < at.k1; k += kTurn) {
+  struct Chunk {
+    typename O::Row key[2];
+    typename O::Values val;
+  };
+  const auto load = [&](Chunk& c, int k) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) key[i].load(kbase + offset(k + 16 * i + r), D);
+    for (int i = 0; i < 2; ++i) c.key[i].load(kbase + offset(k + 16 * i + r), D);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) val.load(j, vbase + offset(k + 16 * (j >> 2) + 4 * g + (j & 3)), D);
+    for (int j = 0; j < 8; ++j) c.val.load(j, vbase + offset(k + 16 * (j >> 2) + 4 * g + (j & 3)), D);
+  };
+  const auto add = [&](const Chunk& c, int k) {
     const uint32_t there = at.k1 - k >= 32 ? ~0u : (1u << (at.k1 - k)) - 1u;
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       uint32_t bits = there;
       if (a.q.num_players > 0) bits &= seen(a.q.masks + row[t] * a.q.mask_words, at.first + k, a.q.num_players);
-      st[t].step(key, val, q[t], bits, a.scale2);
+      st[t].step(c.key, c.val, q[t], bits, a.scale2);
+    }
+  };
+  Chunk now;
+  if constexpr (kPrefetch) {
+    Chunk next;
+    if (at.k0 < at.k1) load(now, at.k0);
+#pragma unroll 1
+    for (int k = at.k0; k < at.k1; k += 2 * kChunk) {
+      if (k + kChunk < at.k1) load(next, k + kChunk);
+      add(now, k);
+      if (k + 2 * kChunk < at.k1) load(now, k + 2 * kChunk);
+      if (k + kChunk < at.k1) add(next, k + kChunk);
+    }
+  } else {
+#pragma unroll 1
+    for (int k = at.k0; k < at.k1; k += kChunk) {
+      load(now, k);
+      add(now, k);
     }
   }
 
@@ -244,7 +274,6 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_attend(AttendArgs a, Part
     const int64_t first = length_of(a, part, at.group) - a.q.first_player;
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      if (!BY_QUERY && t % kWaves != wave) continue;
       const int len = length_of(a, a.own, row[t]);
       const OwnTile own(a, part, at, q0 + t * 16, 16);
       const int passes = own.passes(len);
@@ -252,114 +281,57 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_attend(AttendArgs a, Part
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int64_t x = own.at(a, p, 16 * i + r, at.kv_head);
-          key[i].load(kbase + (x < 0 ? 0 : x), x < 0 ? 0 : D);
+          now.key[i].load(kbase + (x < 0 ? 0 : x), x < 0 ? 0 : D);
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int64_t x = own.at(a, p, 16 * (j >> 2) + 4 * g + (j & 3), at.kv_head);
-          val.load(j, vbase + (x < 0 ? 0 : x), x < 0 ? 0 : D);
+          now.val.load(j, vbase + (x < 0 ? 0 : x), x < 0 ? 0 : D);
         }
-        st[t].step(key, val, q[t], own.bits(a, p, row[t], len, first), a.scale2);
+        st[t].step(now.key, now.val, q[t], own.bits(a, p, row[t], len, first), a.scale2);
       }
     }
   }
 
   bool bad = false;
-  if constexpr (BY_QUERY) {
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      float l = st[t].l;
-      l += __shfl_xor(l, 16);
-      l += __shfl_xor(l, 32);
-      const int qi = q0 + t * 16 + r;
-      if (qi >= n_queries) continue;
-      const int head = at.kv_head * a.share + qi % a.share;
-      const int64_t p = part_index(a, part.slot0 + at.split, row[t], head);
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      bad |= !isfinite(l);
+  for (int t = 0; t < RT; ++t) {
+    float l = st[t].l;
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    const int qi = q0 + t * 16 + r;
+    if (qi >= n_queries) continue;
+    const int head = at.kv_head * a.share + qi % a.share;
+    const int64_t p = part_index(a, part.slot0 + at.split, row[t], head);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    bad |= !isfinite(l);
 #pragma unroll
-      for (int i = 0; i < O::kGroups; ++i)
+    for (int i = 0; i < O::kGroups; ++i)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const int d = (16 * i + 4 * g + x) * O::kOwn;
-          if (d >= D) continue;
-          Pack<T, O::kOwn> done;
-          Pack<float, O::kOwn> part_done;
+      for (int x = 0; x < 4; ++x) {
+        const int d = (16 * i + 4 * g + x) * O::kOwn;
+        if (d >= D) continue;
+        Pack<T, O::kOwn> done;
+        Pack<float, O::kOwn> part_done;
 #pragma unroll
-          for (int e = 0; e < O::kOwn; ++e) {
-            bad |= !isfinite(st[t].o[i][e][x]);
-            done.v[e] = static_cast<T>(st[t].o[i][e][x] * inv);
-            part_done.v[e] = st[t].o[i][e][x];
-          }
-          if (a.direct)
-            store_pack(out_of<T>(a, row[t], head) + d, done);
-          else
-            store_pack(a.part_o + p * D + d, part_done);
+        for (int e = 0; e < O::kOwn; ++e) {
+          bad |= !isfinite(st[t].o[i][e][x]);
+          done.v[e] = static_cast<T>(st[t].o[i][e][x] * inv);
+          part_done.v[e] = st[t].o[i][e][x];
         }
-      if (g == 0) {
-        if (!a.direct)
-          a.part_ml[p] = make_float2(st[t].m, l);
-        else if (a.q.lse)
-          a.q.lse[row[t] * a.q.heads + head] = lse_of(st[t].m, l);
+        if (a.direct)
+          store_pack(out_of<T>(a, row[t], head) + d, done);
+        else
+          store_pack(a.part_o + p * D + d, part_done);
       }
-    }
-  } else {
-    // join the wavefronts
-    float* ml = merge + kWaves * 16 * kStride;  // [wave][query]: m, then l
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      float l = st[t].l;
-      l += __shfl_xor(l, 16);
-      l += __shfl_xor(l, 32);
-      if (t > 0) __syncthreads();
-      float* mine = merge + (wave * 16 + r) * kStride;
-#pragma unroll
-      for (int i = 0; i < O::kGroups; ++i)
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-#pragma unroll
-          for (int e = 0; e < O::kOwn; ++e) mine[(16 * i + 4 * g + x) * O::kOwn + e] = st[t].o[i][e][x];
-      if (g == 0) {
-        ml[wave * 16 + r] = st[t].m;
-        ml[kWaves * 16 + wave * 16 + r] = l;
-      }
-      __syncthreads();
-      const int ql = tid >> 4, qi = q0 + t * 16 + ql, d0 = (tid & 15) * (DP / 16);
-      if (qi < n_queries) {
-        float top = -INFINITY, sum = 0.f, f[kWaves];
-        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[w * 16 + ql]);
-        const float use = top == -INFINITY ? 0.f : top;
-        for (int w = 0; w < kWaves; ++w) {
-          f[w] = __builtin_amdgcn_exp2f(ml[w * 16 + ql] - use);
-          sum += f[w] * ml[kWaves * 16 + w * 16 + ql];
-        }
-        const int64_t row_t = at.group * part.r + qi / a.share;
-        const int head = at.kv_head * a.share + qi % a.share;
-        const int64_t p = part_index(a, part.slot0 + at.split, row_t, head);
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        bad |= !isfinite(sum);
-#pragma unroll
-        for (int e = 0; e < DP / 16; ++e) {
-          const int d = d0 + e;
-          float x = 0.f;
-          for (int w = 0; w < kWaves; ++w) x += f[w] * merge[(w * 16 + ql) * kStride + d];
-          if (d >= D) continue;
-          bad |= !isfinite(x);
-          if (a.direct)
-            out_of<T>(a, row_t, head)[d] = static_cast<T>(x * inv);
-          else
-            a.part_o[p * D + d] = x;
-        }
-        if ((tid & 15) == 0) {
-          if (!a.direct)
-            a.part_ml[p] = make_float2(top, sum);
-          else if (a.q.lse)
-            a.q.lse[row_t * a.q.heads + head] = lse_of(top, sum);
-        }
-      }
+    if (g == 0) {
+      if (!a.direct)
+        a.part_ml[p] = make_float2(st[t].m, l);
+      else if (a.q.lse)
+        a.q.lse[row[t] * a.q.heads + head] = lse_of(st[t].m, l);
     }
   }
-  if (__syncthreads_or(bad)) attend_slowly<T>(a, part, at, kQueries, merge);
+  if (__ballot(bad)) attend_slowly<T>(a, part, at, q0, kQueries);
 }
 
 // Joins the parts of each query, a wavefront per row and head: the lanes weigh
@@ -376,6 +348,7 @@ __global__ __launch_bounds__(256) void k_cache_attend_join(AttendArgs a) {
   if (a.fused) ns = max(ns, 1);
   if (a.own.table && !a.fused) no = (length_of(a, a.own, row) + a.own.split_keys - 1) / a.own.split_keys;
   const auto slot_of = [&](int n) { return n < ns ? a.shared.slot0 + n : a.own.slot0 + n - ns; };
+  const int d = 4 * lane < D ? 4 * lane : 0;
   float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
   for (int n0 = 0; n0 < ns + no; n0 += 64) {
     const int n = min(64, ns + no - n0);
@@ -393,19 +366,17 @@ __global__ __launch_bounds__(256) void k_cache_attend_join(AttendArgs a) {
     l = l * down + sum;
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] *= down;
-    if (4 * lane < D) {
-      for (int j0 = 0; j0 < n; j0 += 8) {
-        Pack<float, 4> x[8];
+    // all lanes take part, so that every lane's weight is there to be read
+    for (int j0 = 0; j0 < n; j0 += 8) {
+      Pack<float, 4> x[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          x[j] = load_pack<float, 4>(a.part_o + part_index(a, slot_of(n0 + min(j0 + j, n - 1)), row, head) * D + 4 * lane);
+      for (int j = 0; j < 8; ++j) x[j] = load_pack<float, 4>(a.part_o + part_index(a, slot_of(n0 + min(j0 + j, n - 1)), row, head) * D + d);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float w = j0 + j < n ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(up), j0 + j)) : 0.f;
-          if (w != 0.f)
+      for (int j = 0; j < 8; ++j) {
+        const float w = j0 + j < n ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(up), j0 + j)) : 0.f;
+        if (w != 0.f)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] += x[j].v[e] * w;
-        }
+          for (int e = 0; e < 4; ++e) o[e] += x[j].v[e] * w;
       }
     }
   }
@@ -459,12 +430,6 @@ int check_queries(const gnnshap_cache* c, const gnnshap_queries* q) {
 
 int padded_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 
-// Tiles of 16 queries that a workgroup takes: more where many queries read the
-// same keys, as far as the registers of a lane go.
-int tile_of(int64_t queries, int head_dim) {
-  return std::min(queries > 32 ? 4 : queries > 16 ? 2 : 1, 256 / padded_dim(head_dim));
-}
-
 // How the work is laid out over workgroups.
 int lay_out(AttendArgs& a, const gnnshap_cache* c, const gnnshap_queries* q) {
   using gnnshap::ceil_div;
@@ -493,17 +458,21 @@ int lay_out(AttendArgs& a, const gnnshap_cache* c, const gnnshap_queries* q) {
     if (queries > INT32_MAX - 1024)
       return gnnshap::fail(GNNSHAP_EUNSUPPORTED, "%lld queries of a group", static_cast<long long>(queries));
     p.wide = !i && queries >= 64 && c->dtype != GNNSHAP_F32;
-    p.by_query = !i && queries >= 64 && !p.wide;
-    p.tile = p.wide ? 128 : p.by_query ? 64 : 16 * tile_of(queries, c->head_dim);
+    // Tiles of 16 queries that a wavefront takes: as many as its registers
+    // hold where there are wavefronts enough, as few as hold all queries.
+    int tiles = 256 / padded_dim(c->head_dim);
+    const auto few = [&](int n) { return q->num_rows / p.r * c->kv_heads * ceil_div(queries, 16 * n) < 2048; };
+    while (tiles > 1 && (queries <= 8 * tiles || (queries > 64 && few(tiles)))) tiles /= 2;
+    p.tile = p.wide ? 128 : 16 * tiles;
     p.tiles = static_cast<int>(ceil_div(queries, p.tile));
-    // Splits: as many as all the workgroups that the chip holds at a time
-    // (two per compute unit of the wide kernel, four of the others), of 256
-    // keys at least; own parts of unlike lengths in pieces of at most 512.
+    // Splits: as many as give the chip 16 wavefronts per compute unit (two
+    // workgroups of the wide kernel), of 64 keys at least (256); at most 256
+    // keys of own parts, whose lengths may be unlike, at most 1024 of a
+    // shared part's.
     const int64_t base = q->num_rows / p.r * c->kv_heads * p.tiles;
-    const int64_t want = std::max<int64_t>(1, (p.wide ? 512 : 1024) / std::max<int64_t>(base, 1));
-    int64_t keys = ceil_div(std::max(p.max_len, 1), want);
-    keys = std::max<int64_t>(ceil_div(keys, 128) * 128, 256);
-    if (!p.wide) keys = std::min<int64_t>(keys, i ? 512 : 4096);
+    const int64_t want = std::max<int64_t>(1, (p.wide ? 512 : 4096) / std::max<int64_t>(base, 1));
+    int64_t keys = ceil_div(ceil_div(std::max(p.max_len, 1), want), 64) * 64;
+    keys = p.wide ? std::max<int64_t>(keys, 256) : std::min<int64_t>(keys, i ? 256 : 1024);
     p.split_keys = static_cast<int>(std::min<int64_t>(keys, INT32_MAX / 2));
     p.splits = static_cast<int>(std::max<int64_t>(1, ceil_div(p.max_len, p.split_keys)));
     p.slot0 = slots;
@@ -523,40 +492,33 @@ size_t carve(AttendArgs& a, void* ws) {
   return c.bytes();
 }
 
-template <class T, int DP, int RT, int MODE>
+template <class T, int DP, int RT, bool IS_OWN>
 int launch_part(const AttendArgs& a, const Part& p, hipStream_t s) {
-  const int pages = p.split_keys / a.c.page_size + 2;
-  const size_t bytes = sizeof(int) * ((pages + 3) & ~3) + sizeof(float) * (kWaves * 16 * (DP + 4) + 2 * kWaves * 16);
-  const unsigned grid = static_cast<unsigned>(a.q.num_rows / p.r * a.c.kv_heads * p.tiles * p.splits);
-  if (bytes > 65536)
-    GS_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&k_cache_attend<T, DP, RT, MODE>),
-                               hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)));
+  const int64_t places = a.q.num_rows / p.r * a.c.kv_heads * p.tiles * p.splits;
+  const size_t bytes = sizeof(int) * kWaves * (p.split_keys / a.c.page_size + 2);
   {
     GS_TIMED("k_cache_attend", s);
-    k_cache_attend<T, DP, RT, MODE><<<grid, 64 * kWaves, bytes, s>>>(a, p);
+    k_cache_attend<T, DP, RT, IS_OWN>
+        <<<static_cast<unsigned>(ceil_div(places, kWaves)), 64 * kWaves, bytes, s>>>(a, p, places);
   }
   GS_LAUNCHED();
   return GNNSHAP_OK;
 }
 
-template <class T, int DP, int MODE>
+template <class T, int DP, bool IS_OWN>
 int launch_tiles(const AttendArgs& a, const Part& p, hipStream_t s) {
-  if (p.tile == 16) return launch_part<T, DP, 1, MODE>(a, p, s);
-  if constexpr (DP <= 128)
-    if (p.tile == 32) return launch_part<T, DP, 2, MODE>(a, p, s);
   if constexpr (DP <= 64)
-    if (p.tile == 64) return launch_part<T, DP, 4, MODE>(a, p, s);
-  return fail(GNNSHAP_EHIP, "no kernel for tiles of %d", p.tile);
+    if (p.tile == 64) return launch_part<T, DP, 4, IS_OWN>(a, p, s);
+  if constexpr (DP <= 128)
+    if (p.tile == 32) return launch_part<T, DP, 2, IS_OWN>(a, p, s);
+  return launch_part<T, DP, 1, IS_OWN>(a, p, s);
 }
 
 template <class T, int DP>
 int launch_all(const AttendArgs& a, hipStream_t s) {
   int st = GNNSHAP_OK;
-  if (a.shared.table)
-    st = a.shared.wide ? launch_attend_wide(a, s)
-         : a.shared.by_query ? launch_part<T, DP, 1, kSharedByQuery>(a, a.shared, s)
-                             : launch_tiles<T, DP, kShared>(a, a.shared, s);
-  if (!st && a.own.table && !a.fused) st = launch_tiles<T, DP, kOwnPart>(a, a.own, s);
+  if (a.shared.table) st = a.shared.wide ? launch_attend_wide(a, s) : launch_tiles<T, DP, false>(a, a.shared, s);
+  if (!st && a.own.table && !a.fused) st = launch_tiles<T, DP, true>(a, a.own, s);
   if (st) return st;
   if (!a.direct || (!a.shared.table && !a.own.table)) {
     GS_TIMED("k_cache_attend_join", s);

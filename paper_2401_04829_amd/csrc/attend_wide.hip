@@ -173,7 +173,7 @@ __global__ __launch_bounds__(64 * kWaves, DP <= 128 ? 2 : 1) void k_cache_attend
   const int D = a.c.head_dim;
   // The first loads of all chains (queries; lengths, pages, then keys and
   // values, of the shared part and of the rows' own) before anything waits.
-  Place at = place_of(a, part);
+  Place at = place_of(a, part, blockIdx.x);
   const int raw_len = part.lengths[at.group];
   int64_t* const offsets = reinterpret_cast<int64_t*>(room + 4 * W::kBytes);  // of kAhead tiles
 
@@ -465,7 +465,7 @@ __global__ __launch_bounds__(64 * kWaves, DP <= 128 ? 2 : 1) void k_cache_attend
         a.q.lse[row * a.q.heads + head] = lse_of(st.m, l);
     }
   }
-  if (__syncthreads_or(bad)) attend_slowly<T>(a, part, at, kQueries, reinterpret_cast<float*>(room));
+  if (__ballot(bad)) attend_slowly<T>(a, part, at, q0, 32);
 }
 
 template <class T, int DP>
