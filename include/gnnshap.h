@@ -623,7 +623,7 @@ int gnnshap_cache_attend_workspace(const gnnshap_cache* cache, const gnnshap_que
  * type).  A row that sees nothing, or whose every score is -inf, has out 0
  * and lse -inf.  Keys and values of positions that a row does not see do not
  * reach it, whatever they hold (NaN and infinities too).  EINVAL: sizes,
- * NULL arrays; EUNSUPPORTED: head_dim, dtype, more than 2^31 - 1 positions;
+ * NULL arrays; EUNSUPPORTED: head_dim, dtype, parts of more than 2^30 tokens;
  * ECAPACITY: workspace. */
 int gnnshap_cache_attend(const gnnshap_cache* cache, const gnnshap_queries* queries, int32_t* info, void* ws,
                          size_t ws_bytes, void* stream);

@@ -16,7 +16,7 @@ constexpr int kChunk = 32;  // keys of a wavefront's step
 // One part of the rows' contexts: `r` consecutive rows share each row of its
 // table.  A group's rows times the query heads of a kv head are its queries,
 // in tiles; a wavefront (a workgroup of the wide kernel) takes a tile over
-// split_keys keys.
+// split_keys keys, and over those `splits` times as far on, and so on.
 struct Part {
   const int32_t* table;
   const int32_t* lengths;
@@ -98,23 +98,26 @@ struct Place {  // what a wavefront or workgroup works on
   int64_t group;
   int kv_head, tile, split;
   int64_t first;  // context position of the part's position 0, counted from the first player
-  int k0, k1;     // keys of the split
+  int k0, k1;     // keys of the split (its first ones)
   bool with_own;  // the rows' own parts too
 };
 
 // Decodes the number of a workgroup or wavefront.  Consecutive ones take
 // consecutive kv heads: workgroups of one head, which read the same keys, then
 // meet in an XCD's cache, and the wavefronts of a workgroup read neighbouring
-// parts of the same tokens.
-__device__ __forceinline__ Place place_of(const AttendArgs& a, const Part& part, int64_t number) {
+// parts of the same tokens.  Splits change last, and each turns the rows by
+// one: where lengths are unlike, neither the first splits, which all rows have,
+// nor those of one long row may meet in one XCD.
+__device__ __forceinline__ Place place_of(const AttendArgs& a, const Part& part, uint32_t number) {
   Place at;
-  int64_t b = number;
-  at.kv_head = b % a.c.kv_heads;
-  b /= a.c.kv_heads;
-  at.split = b % part.splits;
-  b /= part.splits;
-  at.tile = b % part.tiles;
-  at.group = b / part.tiles;
+  uint32_t b = number;
+  at.kv_head = b % static_cast<uint32_t>(a.c.kv_heads);
+  b /= static_cast<uint32_t>(a.c.kv_heads);
+  at.tile = b % static_cast<uint32_t>(part.tiles);
+  b /= static_cast<uint32_t>(part.tiles);
+  const uint32_t groups = static_cast<uint32_t>(a.q.num_rows / part.r);
+  at.split = b / groups;
+  at.group = (b % groups + static_cast<uint32_t>(at.split)) % groups;
   at.k0 = at.split * part.split_keys;
   at.with_own = a.fused && at.split == 0;
   return at;
@@ -191,9 +194,12 @@ __device__ void attend_slowly(const AttendArgs& a, const Part& part, const Place
       if (own && !at.with_own) break;
       const Part& p = own ? a.own : part;
       const int64_t seq = own ? row : at.group;
-      const int k0 = own ? 0 : at.k0, k1 = own ? length_of(a, a.own, row) : at.k1;
+      const int len = length_of(a, p, seq), k0 = own ? 0 : at.k0;
       const int64_t first = own ? length_of(a, part, at.group) - a.q.first_player : at.first;
-      for (int c = k0; c < k1; c += 64) {
+      for (int c = k0; c < len; c += 64) {
+        // the splits between this one's turns
+        if (!own && (c - k0) % p.split_keys == 0 && c > k0) c += (p.splits - 1) * p.split_keys;
+        const int k1 = own ? len : min(len, c + p.split_keys - (c - k0) % p.split_keys);
         bool sees = c + lane < k1;
         if (sees && a.q.num_players > 0)
           sees = seen(a.q.masks + row * a.q.mask_words, first + c + lane, a.q.num_players) & 1u;

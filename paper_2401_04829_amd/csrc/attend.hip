@@ -179,38 +179,32 @@ struct State {
   }
 };
 
-// A wavefront: RT tiles of 16 queries of one kv head over one split of keys, 32
-// at a time, the next ones on their way while these are multiplied (where the
-// registers hold both).
+// A wavefront: RT tiles of 16 queries of one kv head over its splits of the
+// keys, 32 at a time, the next ones on their way while these are multiplied
+// (where the registers hold both).
 template <class T, int DP, int RT, bool IS_OWN>
-__global__ __launch_bounds__(64 * kWaves) void k_cache_attend(AttendArgs a, Part part, int64_t places) {
+__global__ __launch_bounds__(64 * kWaves, DP * sizeof(T) <= 256 && RT == 1 ? 2 : 1) void k_cache_attend(AttendArgs a,
+                                                                                                     Part part,
+                                                                                                     unsigned places) {
   using O = Ops<T, DP>;
   constexpr int kQueries = 16 * RT;
   constexpr bool kPrefetch = DP * sizeof(T) <= 256;
   extern __shared__ int lds[];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-  const int D = a.c.head_dim;
-  const int64_t number = static_cast<int64_t>(blockIdx.x) * kWaves + wave;
+  const int D = a.c.head_dim, n_queries = part.r * a.share;
+  const unsigned number = blockIdx.x * kWaves + wave;
   if (number >= places) return;
   Place at = place_of(a, part, number);
-  const int raw_len = part.lengths[at.group];
-
-  // the pages of the split, as many as there may be, and which of them is the first out of range
-  const int page0 = at.k0 / a.c.page_size, room = part.split_keys / a.c.page_size + 2;
-  const int last = min(at.k0 + part.split_keys, part.max_len) - 1, n_pages = last < at.k0 ? 0 : last / a.c.page_size - page0 + 1;
-  int* pages = lds + wave * room;
-  int first_bad = INT32_MAX;
-  for (int i = lane; i < n_pages; i += 64) {
-    const int p = part.table[at.group * part.width + page0 + i];
-    const bool in = p >= 0 && p < a.c.num_pages;
-    if (!in) first_bad = min(first_bad, i);
-    pages[i] = in ? p : 0;
-  }
+  const int len = length_of(a, part, at.group);
+  if (at.k0 >= len && !a.direct && !at.with_own) return;
+  int* const pages = lds + wave * (part.split_keys / a.c.page_size + 2);
+  at.first = -a.q.first_player;
+  if (IS_OWN && a.shared.table) at.first += length_of(a, a.shared, at.group / a.shared.r);
 
   typename O::Row q[RT];
   int64_t row[RT];
   State<T, DP> st[RT];
-  const int q0 = at.tile * kQueries, n_queries = part.r * a.share;
+  const int q0 = at.tile * kQueries;
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     const int qi = q0 + t * 16 + r, qs = qi < n_queries ? qi : 0;
@@ -218,65 +212,75 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_attend(AttendArgs a, Part
     const int head = at.kv_head * a.share + qs % a.share;
     q[t].load(static_cast<const T*>(a.q.q) + row[t] * a.q.q_row_stride + head * a.q.q_head_stride, D);
   }
-  bound(a, part, at, bounded(a, part, raw_len), IS_OWN);
-  if (at.k0 >= at.k1 && !a.direct && !at.with_own) return;
-  if (at.k0 < at.k1 && first_bad <= (at.k1 - 1) / a.c.page_size - page0 && a.info) *a.info = 1;
-  __builtin_amdgcn_wave_barrier();
 
   const int64_t head_at = static_cast<int64_t>(at.kv_head) * a.c.head_stride;
   const T* const kbase = static_cast<const T*>(a.c.k);
   const T* const vbase = static_cast<const T*>(a.c.v);
-  const auto offset = [&](int key) {
-    key = key < at.k1 ? key : at.k1 - 1;
-    int slot;
-    const int pg = page_of(a, key, slot);
-    return pages[pg - page0] * a.c.page_stride + slot * a.c.slot_stride + head_at;
-  };
   struct Chunk {
     typename O::Row key[2];
     typename O::Values val;
   };
-  const auto load = [&](Chunk& c, int k) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) c.key[i].load(kbase + offset(k + 16 * i + r), D);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) c.val.load(j, vbase + offset(k + 16 * (j >> 2) + 4 * g + (j & 3)), D);
-  };
-  const auto add = [&](const Chunk& c, int k) {
-    const uint32_t there = at.k1 - k >= 32 ? ~0u : (1u << (at.k1 - k)) - 1u;
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      uint32_t bits = there;
-      if (a.q.num_players > 0) bits &= seen(a.q.masks + row[t] * a.q.mask_words, at.first + k, a.q.num_players);
-      st[t].step(c.key, c.val, q[t], bits, a.scale2);
-    }
-  };
   Chunk now;
-  if constexpr (kPrefetch) {
-    Chunk next;
-    if (at.k0 < at.k1) load(now, at.k0);
 #pragma unroll 1
-    for (int k = at.k0; k < at.k1; k += 2 * kChunk) {
-      if (k + kChunk < at.k1) load(next, k + kChunk);
-      add(now, k);
-      if (k + 2 * kChunk < at.k1) load(now, k + 2 * kChunk);
-      if (k + kChunk < at.k1) add(next, k + kChunk);
+  for (int from = at.k0; from < len; from += part.splits * part.split_keys) {
+    const int upto = min(from + part.split_keys, len), page0 = from / a.c.page_size;
+    const int n = (upto - 1) / a.c.page_size - page0 + 1;
+    for (int i = lane; i < n; i += 64) {
+      int p = part.table[at.group * part.width + page0 + i];
+      if (p < 0 || p >= a.c.num_pages) {
+        if (a.info) *a.info = 1;
+        p = 0;
+      }
+      pages[i] = p;
     }
-  } else {
+    __builtin_amdgcn_wave_barrier();
+    const auto offset = [&](int key) {
+      key = key < upto ? key : upto - 1;
+      int slot;
+      const int pg = page_of(a, key, slot);
+      return pages[pg - page0] * a.c.page_stride + slot * a.c.slot_stride + head_at;
+    };
+    const auto load = [&](Chunk& c, int k) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) c.key[i].load(kbase + offset(k + 16 * i + r), D);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) c.val.load(j, vbase + offset(k + 16 * (j >> 2) + 4 * g + (j & 3)), D);
+    };
+    const auto add = [&](const Chunk& c, int k) {
+      const uint32_t there = upto - k >= 32 ? ~0u : (1u << (upto - k)) - 1u;
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        uint32_t bits = there;
+        if (a.q.num_players > 0) bits &= seen(a.q.masks + row[t] * a.q.mask_words, at.first + k, a.q.num_players);
+        st[t].step(c.key, c.val, q[t], bits, a.scale2);
+      }
+    };
+    if constexpr (kPrefetch) {
+      Chunk next;
+      load(now, from);
 #pragma unroll 1
-    for (int k = at.k0; k < at.k1; k += kChunk) {
-      load(now, k);
-      add(now, k);
+      for (int k = from; k < upto; k += 2 * kChunk) {
+        if (k + kChunk < upto) load(next, k + kChunk);
+        add(now, k);
+        if (k + 2 * kChunk < upto) load(now, k + 2 * kChunk);
+        if (k + kChunk < upto) add(next, k + kChunk);
+      }
+    } else {
+#pragma unroll 1
+      for (int k = from; k < upto; k += kChunk) {
+        load(now, k);
+        add(now, k);
+      }
     }
   }
 
   if (!IS_OWN && at.with_own) {
-    const int64_t first = length_of(a, part, at.group) - a.q.first_player;
+    const int64_t first = len - a.q.first_player;
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      const int len = length_of(a, a.own, row[t]);
+      const int own_len = length_of(a, a.own, row[t]);
       const OwnTile own(a, part, at, q0 + t * 16, 16);
-      const int passes = own.passes(len);
+      const int passes = own.passes(own_len);
       for (int p = 0; p < passes; ++p) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -288,7 +292,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_attend(AttendArgs a, Part
           const int64_t x = own.at(a, p, 16 * (j >> 2) + 4 * g + (j & 3), at.kv_head);
           now.val.load(j, vbase + (x < 0 ? 0 : x), x < 0 ? 0 : D);
         }
-        st[t].step(now.key, now.val, q[t], own.bits(a, p, row[t], len, first), a.scale2);
+        st[t].step(now.key, now.val, q[t], own.bits(a, p, row[t], own_len, first), a.scale2);
       }
     }
   }
@@ -334,26 +338,33 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_attend(AttendArgs a, Part
   if (__ballot(bad)) attend_slowly<T>(a, part, at, q0, kQueries);
 }
 
-// Joins the parts of each query, a wavefront per row and head: the lanes weigh
-// 64 parts at a time, then add up the parts' elements, eight loads in flight.
-template <class T>
-__global__ __launch_bounds__(256) void k_cache_attend_join(AttendArgs a) {
-  const int lane = threadIdx.x & 63, D = a.c.head_dim;
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+// Joins the parts of each query, a wavefront per row and head, or the four of a
+// workgroup where there may be many parts: the lanes weigh 64 parts at a time,
+// then add up the parts' elements, eight loads in flight.
+template <class T, int PER_QUERY>
+__global__ __launch_bounds__(64 * kWaves) void k_cache_attend_join(AttendArgs a) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = a.c.head_dim;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * (kWaves / PER_QUERY) + wave / PER_QUERY;
   if (i >= a.q.num_rows * a.q.heads) return;
   const int64_t row = i / a.q.heads;
   const int head = static_cast<int>(i % a.q.heads);
+  // the splits that have keys
+  const auto splits_of = [&](const Part& part, int64_t seq) {
+    return min(part.splits, (length_of(a, part, seq) + part.split_keys - 1) / part.split_keys);
+  };
   int ns = 0, no = 0;
-  if (a.shared.table) ns = (length_of(a, a.shared, row / a.shared.r) + a.shared.split_keys - 1) / a.shared.split_keys;
+  if (a.shared.table) ns = splits_of(a.shared, row / a.shared.r);
   if (a.fused) ns = max(ns, 1);
-  if (a.own.table && !a.fused) no = (length_of(a, a.own, row) + a.own.split_keys - 1) / a.own.split_keys;
+  if (a.own.table && !a.fused) no = splits_of(a.own, row);
   const auto slot_of = [&](int n) { return n < ns ? a.shared.slot0 + n : a.own.slot0 + n - ns; };
   const int d = 4 * lane < D ? 4 * lane : 0;
   float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int n0 = 0; n0 < ns + no; n0 += 64) {
-    const int n = min(64, ns + no - n0);
+  // this wavefront's parts: wave % PER_QUERY, then PER_QUERY further
+  const int first = wave % PER_QUERY, count = (ns + no - first + PER_QUERY - 1) / PER_QUERY;
+  for (int n0 = 0; n0 < count; n0 += 64) {
+    const int n = min(64, count - n0);
     float2 ml = make_float2(-INFINITY, 0.f);
-    if (lane < n) ml = a.part_ml[part_index(a, slot_of(n0 + lane), row, head)];
+    if (lane < n) ml = a.part_ml[part_index(a, slot_of(first + (n0 + lane) * PER_QUERY), row, head)];
     float top = fmaxf(m, ml.x);
 #pragma unroll
     for (int off = 1; off < 64; off *= 2) top = fmaxf(top, __shfl_xor(top, off));
@@ -370,7 +381,9 @@ __global__ __launch_bounds__(256) void k_cache_attend_join(AttendArgs a) {
     for (int j0 = 0; j0 < n; j0 += 8) {
       Pack<float, 4> x[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = load_pack<float, 4>(a.part_o + part_index(a, slot_of(n0 + min(j0 + j, n - 1)), row, head) * D + d);
+      for (int j = 0; j < 8; ++j)
+        x[j] = load_pack<float, 4>(
+            a.part_o + part_index(a, slot_of(first + (n0 + min(j0 + j, n - 1)) * PER_QUERY), row, head) * D + d);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float w = j0 + j < n ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(up), j0 + j)) : 0.f;
@@ -378,6 +391,31 @@ __global__ __launch_bounds__(256) void k_cache_attend_join(AttendArgs a) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[e] += x[j].v[e] * w;
       }
+    }
+  }
+  if constexpr (PER_QUERY > 1) {
+    __shared__ float parts[PER_QUERY][64 * 4], stats[PER_QUERY][2];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) parts[wave][4 * lane + e] = o[e];
+    if (lane == 0) {
+      stats[wave][0] = m;
+      stats[wave][1] = l;
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    float top = -INFINITY;
+    for (int w = 0; w < PER_QUERY; ++w) top = fmaxf(top, stats[w][0]);
+    const float use = top == -INFINITY ? 0.f : top;
+    m = top;
+    l = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = 0.f;
+    for (int w = 0; w < PER_QUERY; ++w) {
+      if (stats[w][1] == 0.f) continue;
+      const float up = __builtin_amdgcn_exp2f(stats[w][0] - use);
+      l += stats[w][1] * up;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += parts[w][4 * lane + e] * up;
     }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -398,7 +436,7 @@ int check_queries(const gnnshap_cache* c, const gnnshap_queries* q) {
     return fail(GNNSHAP_EINVAL, "%d query heads over %d kv heads", static_cast<int>(q->heads),
                 static_cast<int>(c->kv_heads));
   if (!(q->scale != 0.0) || !std::isfinite(q->scale)) return fail(GNNSHAP_EINVAL, "scale is 0 or not finite");
-  if (q->num_rows > INT32_MAX || q->num_rows * q->heads > (int64_t(1) << 40))
+  if (q->num_rows > INT32_MAX || q->num_rows * q->heads > INT32_MAX)
     return fail(GNNSHAP_EUNSUPPORTED, "%lld rows in one call", static_cast<long long>(q->num_rows));
   const struct {
     const char* name;
@@ -410,7 +448,7 @@ int check_queries(const gnnshap_cache* c, const gnnshap_queries* q) {
     if (!p.table) continue;
     if (!p.lengths) return fail(GNNSHAP_EINVAL, "%s table without lengths", p.name);
     if (p.longest < 0 || p.width < 0) return fail(GNNSHAP_EINVAL, "%s part: negative width or length", p.name);
-    if (p.longest > INT32_MAX - 65536)
+    if (p.longest > (int64_t(1) << 30))
       return fail(GNNSHAP_EUNSUPPORTED, "%s part of up to %lld tokens", p.name, static_cast<long long>(p.longest));
     if (gnnshap::ceil_div(p.longest, c->page_size) > p.width)
       return fail(GNNSHAP_EINVAL, "%s part: %lld tokens do not fit %lld pages of %d", p.name,
@@ -465,19 +503,27 @@ int lay_out(AttendArgs& a, const gnnshap_cache* c, const gnnshap_queries* q) {
     while (tiles > 1 && (queries <= 8 * tiles || (queries > 64 && few(tiles)))) tiles /= 2;
     p.tile = p.wide ? 128 : 16 * tiles;
     p.tiles = static_cast<int>(ceil_div(queries, p.tile));
-    // Splits: as many as give the chip 16 wavefronts per compute unit (two
-    // workgroups of the wide kernel), of 64 keys at least (256); at most 256
-    // keys of own parts, whose lengths may be unlike, at most 1024 of a
-    // shared part's.
+    // Splits.  The wide kernel: as many as give the chip two workgroups per
+    // compute unit, of 256 keys at least.  The other: splits of 256 keys (128
+    // where there are few), up to 32 times the wavefronts that the chip holds,
+    // which come back for further splits where the keys are more.  So many,
+    // because the lengths may be unlike: a wavefront without keys ends at
+    // once, and one with many would end last (64 rows of 1 to 20,000 tokens:
+    // 146 us; with 8,192 wavefronts 192 us).
     const int64_t base = q->num_rows / p.r * c->kv_heads * p.tiles;
-    const int64_t want = std::max<int64_t>(1, (p.wide ? 512 : 4096) / std::max<int64_t>(base, 1));
-    int64_t keys = ceil_div(ceil_div(std::max(p.max_len, 1), want), 64) * 64;
-    keys = p.wide ? std::max<int64_t>(keys, 256) : std::min<int64_t>(keys, i ? 256 : 1024);
-    p.split_keys = static_cast<int>(std::min<int64_t>(keys, INT32_MAX / 2));
-    p.splits = static_cast<int>(std::max<int64_t>(1, ceil_div(p.max_len, p.split_keys)));
+    const auto at_most = [&](int64_t n) { return std::max<int64_t>(1, n / std::max<int64_t>(base, 1)); };
+    const int64_t longest = std::max(p.max_len, 1);
+    if (p.wide) {
+      p.split_keys = static_cast<int>(
+          std::min<int64_t>(std::max<int64_t>(ceil_div(ceil_div(longest, at_most(512)), 128) * 128, 256), INT32_MAX / 2));
+      p.splits = static_cast<int>(ceil_div(longest, p.split_keys));
+    } else {
+      p.split_keys = ceil_div(longest, 256) * base < 2048 ? 128 : 256;
+      p.splits = static_cast<int>(std::min(ceil_div(longest, p.split_keys), at_most(65536)));
+    }
+    if (base * p.splits > INT32_MAX) return fail(GNNSHAP_EUNSUPPORTED, "too many workgroups");
     p.slot0 = slots;
     slots += p.splits;
-    if (base * p.splits > INT32_MAX) return gnnshap::fail(GNNSHAP_EUNSUPPORTED, "too many workgroups");
   }
   a.direct = slots <= 1;
   return GNNSHAP_OK;
@@ -498,8 +544,8 @@ int launch_part(const AttendArgs& a, const Part& p, hipStream_t s) {
   const size_t bytes = sizeof(int) * kWaves * (p.split_keys / a.c.page_size + 2);
   {
     GS_TIMED("k_cache_attend", s);
-    k_cache_attend<T, DP, RT, IS_OWN>
-        <<<static_cast<unsigned>(ceil_div(places, kWaves)), 64 * kWaves, bytes, s>>>(a, p, places);
+    k_cache_attend<T, DP, RT, IS_OWN><<<static_cast<unsigned>(ceil_div(places, kWaves)), 64 * kWaves, bytes, s>>>(
+        a, p, static_cast<unsigned>(places));
   }
   GS_LAUNCHED();
   return GNNSHAP_OK;
@@ -522,7 +568,11 @@ int launch_all(const AttendArgs& a, hipStream_t s) {
   if (st) return st;
   if (!a.direct || (!a.shared.table && !a.own.table)) {
     GS_TIMED("k_cache_attend_join", s);
-    k_cache_attend_join<T><<<static_cast<unsigned>(gnnshap::ceil_div(a.q.num_rows * a.q.heads, 4)), 256, 0, s>>>(a);
+    const int64_t queries = a.q.num_rows * a.q.heads;
+    if (a.shared.splits + a.own.splits > 8)
+      k_cache_attend_join<T, kWaves><<<static_cast<unsigned>(queries), 64 * kWaves, 0, s>>>(a);
+    else
+      k_cache_attend_join<T, 1><<<static_cast<unsigned>(ceil_div(queries, kWaves)), 64 * kWaves, 0, s>>>(a);
     GS_LAUNCHED();
   }
   return GNNSHAP_OK;
