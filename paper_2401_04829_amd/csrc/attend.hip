@@ -518,7 +518,7 @@ int lay_out(AttendArgs& a, const gnnshap_cache* c, const gnnshap_queries* q) {
           std::min<int64_t>(std::max<int64_t>(ceil_div(ceil_div(longest, at_most(512)), 128) * 128, 256), INT32_MAX / 2));
       p.splits = static_cast<int>(ceil_div(longest, p.split_keys));
     } else {
-      p.split_keys = ceil_div(longest, 256) * base < 2048 ? 128 : 256;
+      p.split_keys = ceil_div(longest, 256) * base < 4096 ? 128 : 256;
       p.splits = static_cast<int>(std::min(ceil_div(longest, p.split_keys), at_most(65536)));
     }
     if (base * p.splits > INT32_MAX) return fail(GNNSHAP_EUNSUPPORTED, "too many workgroups");
