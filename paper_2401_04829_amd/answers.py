@@ -232,3 +232,81 @@ def token_logprobs_backward(logits, targets, lse, entropy=None, grad_logprob=Non
         _vector(grad_entropy, "grad_entropy", torch.float32, (rows,), dev), out.data_ptr(), out.stride(0),
         _vector(info, "info", torch.int32, (1,), dev))
     return out
+
+
+class _Logprob(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, targets):
+        r = token_logprobs(logits, targets)
+        ctx.save_for_backward(logits, targets, r.lse, r.entropy)
+        return r.logprob, r.entropy
+
+    @staticmethod
+    def backward(ctx, grad_logprob, grad_entropy):
+        logits, targets, lse, entropy = ctx.saved_tensors
+        grads = (None if g is None else g.float().contiguous() for g in (grad_logprob, grad_entropy))
+        return token_logprobs_backward(logits, targets, lse, entropy, *grads), None
+
+
+def differentiable_logprobs(logits, targets):
+    """Log probabilities of `targets` (int64 [rows]) and entropies of logits
+    [rows, vocabulary] with their gradient by the logits (autograd), for
+    gradient attributions and training."""
+    return _Logprob.apply(logits, targets)
+
+
+class AnswerExplainer:
+    """Shapley values of prompt tokens for a model's answer (Alg. 1 of the
+    paper with tokens as players): the sampler's coalitions, their values from
+    the caller's model, the constrained least squares.
+
+    `value(masks, num_players)` gives the model's value under each coalition,
+    float32 [rows], such as the answer's log probability by `attend` and
+    `token_logprobs`; masks are int64 [rows, words] (the sampler's bits).  It is
+    called with batches of at most `batch` coalitions, of which the last one
+    ends with the empty and the full coalition."""
+
+    def __init__(self, value, device="cuda", batch=16384):
+        _need(batch >= 2, "batches of at least two coalitions are needed")
+        L.load()
+        self.value, self.device, self.batch = value, torch.device(device), int(batch)
+
+    def explain(self, num_players, num_samples, seed, stream_id=0, iterative_threshold=0):
+        """Returns an AnswerExplanation, valid once the current stream has run."""
+        dev = self.device
+        plan, classes = L.gnnshap_plan_samples(int(num_players), int(num_samples), int(seed), int(stream_id),
+                                               int(iterative_threshold))
+        k, words, m = plan.num_rows, plan.words_per_row, plan.num_players
+        masks = torch.zeros((k + 2, words), dtype=torch.int64, device=dev)   # then none and all
+        masks[k + 1] = -1
+        if m % 64:
+            masks[k + 1, -1] = (1 << (m % 64)) - 1
+        weights = torch.empty(k, dtype=torch.float32, device=dev)
+        nbytes = L.gnnshap_sample_workspace(plan)
+        ws = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=dev)
+        _on(masks.device, L.gnnshap_sample_coalitions, plan, classes, masks.data_ptr(), weights.data_ptr(),
+            ws.data_ptr(), ws.numel())
+        y = torch.empty(k + 2, dtype=torch.float32, device=dev)
+        for b in range(0, k + 2, self.batch):
+            part = masks[b:b + self.batch]
+            got = self.value(part, m)
+            _need(got.shape == (part.shape[0],) and got.dtype == torch.float32,
+                  "value: one float32 number per coalition is needed")
+            y[b:b + self.batch] = got
+        phi = torch.empty(m, dtype=torch.float32, device=dev)
+        info = torch.empty(1, dtype=torch.int32, device=dev)
+        nbytes = L.gnnshap_solve_workspace(plan)
+        ws = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=dev)
+        _on(masks.device, L.gnnshap_solve_wls, plan, classes, masks.data_ptr(), y.data_ptr(), y[k:].data_ptr(),
+            phi.data_ptr(), info.data_ptr(), ws.data_ptr(), ws.numel())
+        return AnswerExplanation(phi, y[:k], y[k:], masks[:k], weights, info, plan)
+
+
+class AnswerExplanation(NamedTuple):
+    phi: torch.Tensor           # float32 [players]
+    y: torch.Tensor             # float32 [rows]: the coalitions' values
+    f_empty_full: torch.Tensor  # float32 [2]
+    masks: torch.Tensor         # int64 [rows, words]
+    weights: torch.Tensor       # float32 [rows]
+    info: torch.Tensor          # int32 [1], as gnnshap_solve_wls sets it
+    plan: L.gnnshap_sample_plan
