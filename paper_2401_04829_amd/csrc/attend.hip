@@ -504,12 +504,16 @@ int lay_out(AttendArgs& a, const gnnshap_cache* c, const gnnshap_queries* q) {
     p.tile = p.wide ? 128 : 16 * tiles;
     p.tiles = static_cast<int>(ceil_div(queries, p.tile));
     // Splits.  The wide kernel: as many as give the chip two workgroups per
-    // compute unit, of 256 keys at least.  The other: splits of 256 keys (128
-    // where there are few), up to 32 times the wavefronts that the chip holds,
-    // which come back for further splits where the keys are more.  So many,
-    // because the lengths may be unlike: a wavefront without keys ends at
-    // once, and one with many would end last (64 rows of 1 to 20,000 tokens:
-    // 146 us; with 8,192 wavefronts 192 us).
+    // compute unit, of 256 keys at least.  The other: splits of 256 keys, 128
+    // where there are few, and 64 where there are fewer still and the join has
+    // not too many parts (bf16, 32 heads over 8 of 128 elements, 64 against
+    // 128: one row of 500 keys 11.3 us against 14.6, of 4,000 13.2 against
+    // 15.5, of 16,000 26.8 against 22.9; 8 rows of 1,000 14.6 against 16.5).
+    // Up to 32 times the wavefronts that the chip holds, which come back for
+    // further splits where the keys are more.  So many, because the lengths may
+    // be unlike: a wavefront without keys ends at once, and one with many would
+    // end last (64 rows of 1 to 20,000 tokens: 146 us; with 8,192 wavefronts
+    // 192 us).
     const int64_t base = q->num_rows / p.r * c->kv_heads * p.tiles;
     const auto at_most = [&](int64_t n) { return std::max<int64_t>(1, n / std::max<int64_t>(base, 1)); };
     const int64_t longest = std::max(p.max_len, 1);
@@ -518,7 +522,9 @@ int lay_out(AttendArgs& a, const gnnshap_cache* c, const gnnshap_queries* q) {
           std::min<int64_t>(std::max<int64_t>(ceil_div(ceil_div(longest, at_most(512)), 128) * 128, 256), INT32_MAX / 2));
       p.splits = static_cast<int>(ceil_div(longest, p.split_keys));
     } else {
-      p.split_keys = ceil_div(longest, 256) * base < 4096 ? 128 : 256;
+      p.split_keys = ceil_div(longest, 128) * base < 1024 && longest <= 8192 ? 64
+                     : ceil_div(longest, 256) * base < 4096                  ? 128
+                                                                             : 256;
       p.splits = static_cast<int>(std::min(ceil_div(longest, p.split_keys), at_most(65536)));
     }
     if (base * p.splits > INT32_MAX) return fail(GNNSHAP_EUNSUPPORTED, "too many workgroups");
