@@ -43,6 +43,34 @@ __device__ __forceinline__ Stats no_stats() { return Stats{-INFINITY, 0.f, 0.f};
 
 __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.f : m; }
 
+// The value of a lane of the same 16, `Turn` lanes on, moved within the vector unit.
+template <int Turn>
+__device__ __forceinline__ uint32_t turned(uint32_t x) {
+  constexpr int kRowRor = 0x120;
+  return __builtin_amdgcn_update_dpp(0, static_cast<int>(x), kRowRor + Turn, 0xF, 0xF, false);
+}
+template <int Turn>
+__device__ __forceinline__ float turned(float x) {
+  return __uint_as_float(turned<Turn>(__float_as_uint(x)));
+}
+template <int Turn>
+__device__ __forceinline__ uint64_t turned(uint64_t x) {
+  return static_cast<uint64_t>(turned<Turn>(static_cast<uint32_t>(x >> 32))) << 32 | turned<Turn>(static_cast<uint32_t>(x));
+}
+// x of LANES lanes (16 or 64) put together by `f`, in all of them.
+template <int LANES, class X, class F>
+__device__ __forceinline__ X together(X x, F f) {
+  x = f(x, turned<8>(x));
+  x = f(x, turned<4>(x));
+  x = f(x, turned<2>(x));
+  x = f(x, turned<1>(x));
+  if constexpr (LANES == 64) {
+    x = f(x, static_cast<X>(__shfl_xor(x, 16)));
+    x = f(x, static_cast<X>(__shfl_xor(x, 32)));
+  }
+  return x;
+}
+
 // Moves a to the maximum m >= a.m.
 __device__ __forceinline__ void move_to(Stats& a, float m) {
   if (a.s != 0.f) {  // NaN too
@@ -404,11 +432,10 @@ __global__ __launch_bounds__(256) void k_token_logprobs_short(LogprobArgs a) {
   const float xt = in ? given(a, x, row, has) : 0.f;
 #pragma unroll
   for (int i = 0; i < N; ++i) m = fmaxf(m, f[i]);
-#pragma unroll
-  for (int off = 1; off < LANES; off *= 2) m = fmaxf(m, __shfl_xor(m, off));
+  m = together<LANES>(m, [](float x, float y) { return fmaxf(x, y); });
   const float use = finite_max(m);
   float s = 0.f, w = 0.f;
-  int rank = 0;
+  uint32_t rank = 0;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const float d = (f[i] - use) * kLog2e, e = __builtin_amdgcn_exp2f(d);
@@ -416,15 +443,13 @@ __global__ __launch_bounds__(256) void k_token_logprobs_short(LogprobArgs a) {
     w += e * fmaxf(d, -200.f);
     rank += f[i] > xt;
   }
-#pragma unroll
-  for (int off = 1; off < LANES; off *= 2) {
-    s += __shfl_xor(s, off);
-    w += __shfl_xor(w, off);
-    rank += __shfl_xor(rank, off);
-  }
+  const auto plus = [](auto x, auto y) { return x + y; };
+  s = together<LANES>(s, plus);
+  w = together<LANES>(w, plus);
+  rank = together<LANES>(rank, plus);
   const bool none = s == 0.f;
   const float logs = logf(s);
-  if (in && lane == 0) write_stats(a, row, Stats{m, s, w}, logs, rank, has, xt);
+  if (in && lane == 0) write_stats(a, row, Stats{m, s, w}, logs, static_cast<int>(rank), has, xt);
 
   Key last = ~0ull;
   for (int k = 0; k < a.l.top; ++k) {
@@ -434,9 +459,7 @@ __global__ __launch_bounds__(256) void k_token_logprobs_short(LogprobArgs a) {
       const Key key = key_of(f[i], lane + LANES * i);
       if (lane + LANES * i < V && key < last) best = max(best, key);
     }
-#pragma unroll
-    for (int off = 1; off < LANES; off *= 2)
-      best = max(best, static_cast<Key>(__shfl_xor(static_cast<unsigned long long>(best), off)));
+    best = together<LANES>(best, [](Key x, Key y) { return max(x, y); });
     last = best;
     if (in && lane == k % LANES) {
       const int64_t at = row * a.l.top + k;
@@ -455,8 +478,11 @@ struct GradArgs {
   int32_t* info;
 };
 
-// blockDim.x threads take a row's elements in packs of 16 bytes, blockDim.y
-// rows per workgroup; every element is read once and written once.
+constexpr int kGradPacks = 4;
+
+// blockDim.x threads take a row's elements in packs of 16 bytes, four in
+// flight, blockDim.y rows per workgroup; every element is read once and
+// written once.
 template <class T>
 __global__ __launch_bounds__(256) void k_token_logprobs_grad(GradArgs a) {
   constexpr int kVec = 16 / sizeof(T);
@@ -480,15 +506,30 @@ __global__ __launch_bounds__(256) void k_token_logprobs_grad(GradArgs a) {
     const float r = own - p * (gl + ge * ((p == 0.f ? 0.f : logp) + ent));
     return static_cast<T>(none ? 0.f : r);
   };
-  const int64_t step = static_cast<int64_t>(gridDim.y) * blockDim.x * kVec;
-  for (int64_t i = (static_cast<int64_t>(blockIdx.y) * blockDim.x + threadIdx.x) * kVec; i < V; i += step) {
-    if (i + kVec <= V) {
-      Pack<T, kVec> p = load_pack<T, kVec>(x + i);
+  const int64_t turn = static_cast<int64_t>(blockDim.x) * kVec, step = gridDim.y * turn * kGradPacks;
+  for (int64_t i = blockIdx.y * turn * kGradPacks + threadIdx.x * kVec; i < V; i += step) {
+    if (i + (kGradPacks - 1) * turn + kVec <= V) {
+      Pack<T, kVec> p[kGradPacks];
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) p.v[e] = d(p.v[e], i + e);
-      store_pack(out + i, p);
-    } else {
-      for (int64_t j = i; j < V; ++j) out[j] = d(x[j], j);
+      for (int u = 0; u < kGradPacks; ++u) p[u] = load_pack<T, kVec>(x + i + u * turn);
+#pragma unroll
+      for (int u = 0; u < kGradPacks; ++u) {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) p[u].v[e] = d(p[u].v[e], i + u * turn + e);
+        store_pack(out + i + u * turn, p[u]);
+      }
+      continue;
+    }
+    for (int u = 0; u < kGradPacks; ++u) {
+      const int64_t from = i + u * turn;
+      if (from + kVec <= V) {
+        Pack<T, kVec> p = load_pack<T, kVec>(x + from);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) p.v[e] = d(p.v[e], from + e);
+        store_pack(out + from, p);
+      } else {
+        for (int64_t j = from; j < V; ++j) out[j] = d(x[j], j);
+      }
     }
   }
 }
@@ -618,7 +659,7 @@ extern "C" int gnnshap_token_logprobs_backward(const gnnshap_logits* l, const fl
     int x = 8;
     while (x < 256 && x < packs) x *= 2;
     const dim3 grid(static_cast<unsigned>(gnnshap::ceil_div(l->num_rows, 256 / x)),
-                    static_cast<unsigned>(std::min<int64_t>(gnnshap::ceil_div(packs, x), 1024)));
+                    static_cast<unsigned>(std::min<int64_t>(gnnshap::ceil_div(packs, x * kGradPacks), 1024)));
     {
       GS_TIMED("k_token_logprobs_grad", s);
       k_token_logprobs_grad<T><<<grid, dim3(x, 256 / x), 0, s>>>(a);
