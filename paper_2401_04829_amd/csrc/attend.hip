@@ -478,8 +478,6 @@ int lay_out(AttendArgs& a, const gnnshap_cache* c, const gnnshap_queries* q) {
   a.page_shift = -1;
   for (int i = 0; i < 31; ++i)
     if (c->page_size == 1 << i) a.page_shift = i;
-  // own parts of few tokens ride along with the shared part
-  a.fused = q->shared_table && q->table && q->max_length <= 64;
   Part* parts[2] = {&a.shared, &a.own};
   int slots = 0;
   for (int i = 0; i < 2; ++i) {
@@ -495,13 +493,33 @@ int lay_out(AttendArgs& a, const gnnshap_cache* c, const gnnshap_queries* q) {
     const int64_t queries = static_cast<int64_t>(p.r) * a.share;
     if (queries > INT32_MAX - 1024)
       return gnnshap::fail(GNNSHAP_EUNSUPPORTED, "%lld queries of a group", static_cast<long long>(queries));
-    p.wide = !i && queries >= 64 && c->dtype != GNNSHAP_F32;
-    // Tiles of 16 queries that a wavefront takes: as many as its registers
-    // hold where there are wavefronts enough, as few as hold all queries.
-    int tiles = 256 / padded_dim(c->head_dim);
-    const auto few = [&](int n) { return q->num_rows / p.r * c->kv_heads * ceil_div(queries, 16 * n) < 2048; };
-    while (tiles > 1 && (queries <= 8 * tiles || (queries > 64 && few(tiles)))) tiles /= 2;
-    p.tile = p.wide ? 128 : 16 * tiles;
+    // The wide kernel leaves part of its 128 queries empty where there are
+    // fewer, and is still ahead from 32 on; where heads are wider than 128,
+    // from 128 (bf16, 4,000 shared keys: 32 queries 22 us against 34, 128
+    // queries 28 against 37; 512 keys and 16 queries 20.4 against 18.2; heads of
+    // 256: 64 queries 35 against 25, 128 queries 38.4 against 38.3).
+    p.wide = !i && queries >= (c->head_dim <= 128 ? 32 : 128) && c->dtype != GNNSHAP_F32;
+    // Tiles of 16 queries that a wavefront takes: two for heads of 65 to 128
+    // elements where there are wavefronts enough (64 heads over one, bf16: 512
+    // rows of 1,000 keys 146 us with two against 157 with one, one row of 4,000
+    // 16.8 against 14.2; 10,000 rows x 4 heads on 1,000 shared keys in fp32 752
+    // against 937, but with heads of 64 elements 226 against 166 at 2,000 rows).
+    const bool two = padded_dim(c->head_dim) == 128 && queries > 16 &&
+                     q->num_rows / p.r * c->kv_heads * ceil_div(queries, 32) *
+                             ceil_div(std::max(p.max_len, 1), 256) >= 2048;
+    // Own parts of few tokens ride along with the shared part: a wavefront
+    // takes its rows' tokens 32 at a time, one such pass after the other at
+    // about 3 us, where a launch for them costs about 4 us and their parts,
+    // written and joined, about 1 us for each 1,200 heads (bf16, 32 heads over
+    // 8, 512 shared keys, own tokens with the shared part against apart: 32
+    // rows with 4 each 21.6 us against 25.5, with 16 30.1 against 25.5; 1,000
+    // rows with 16 67 against 88, with 64 134 against 126).
+    if (!i && q->table && q->max_length <= 64) {
+      const int64_t rows = ceil_div(p.wide ? 32 : 16, a.share);
+      const int64_t passes = ceil_div(q->max_length, std::max<int64_t>(kChunk / rows, 1));
+      a.fused = 3 * passes <= 4 + q->num_rows * q->heads / 1200;
+    }
+    p.tile = p.wide ? 128 : two ? 32 : 16;
     p.tiles = static_cast<int>(ceil_div(queries, p.tile));
     // Splits.  The wide kernel: as many as give the chip two workgroups per
     // compute unit, of 256 keys at least.  The other: splits of 256 keys, 128
@@ -559,9 +577,7 @@ int launch_part(const AttendArgs& a, const Part& p, hipStream_t s) {
 
 template <class T, int DP, bool IS_OWN>
 int launch_tiles(const AttendArgs& a, const Part& p, hipStream_t s) {
-  if constexpr (DP <= 64)
-    if (p.tile == 64) return launch_part<T, DP, 4, IS_OWN>(a, p, s);
-  if constexpr (DP <= 128)
+  if constexpr (DP == 128)
     if (p.tile == 32) return launch_part<T, DP, 2, IS_OWN>(a, p, s);
   return launch_part<T, DP, 1, IS_OWN>(a, p, s);
 }

@@ -492,3 +492,36 @@ def test_gradient_of_a_row_without_numbers_is_zero(dev):
     one = torch.ones(2, device=dev)
     g = A.token_logprobs_backward(x, t, r.lse, r.entropy, one, one)
     assert (g == 0).all()
+
+
+# sizes on either side of the ways in which the work is laid out: two tiles of
+# queries to a wavefront, more parts than the lanes that join them, splits of
+# 64 keys, own tokens beside the shared part and apart from it
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,kv,share,dim,page,lengths", [
+    (260, 1, 20, 72, 16, [2000] + 259 * [1793]), (1, 2, 4, 128, 16, [12001]), (1, 1, 1, 64, 8, [8193]),
+    (5, 2, 3, 128, 16, [64, 65, 128, 0, 1000])])
+def test_attention_over_own_tokens_laid_out(dev, dtype, rows, kv, share, dim, page, lengths):
+    test_attention_over_own_tokens(dev, dtype, rows, kv, share, dim, page, lengths)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("groups,per,kv,share,dim,page,lengths,own,first", [
+    (1, 4100, 2, 4, 72, 16, [300], 2, 0), (1, 2000, 2, 4, 64, 16, [70], 19, 3), (1, 40, 2, 4, 64, 16, [130], 19, 3),
+    (1, 31, 1, 1, 128, 16, [200], 2, 0), (1, 33, 1, 1, 128, 16, [200], 33, 0), (1, 35, 1, 2, 256, 16, [97], 5, 9),
+    (1, 70, 1, 2, 200, 16, [97], 5, 9), (1, 128, 1, 1, 256, 16, [65], 1, 0)])
+def test_attention_of_coalitions_laid_out(dev, dtype, groups, per, kv, share, dim, page, lengths, own, first):
+    test_attention_of_coalitions(dev, dtype, groups, per, kv, share, dim, page, lengths, own, first)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,vocab,top,kind", [(3, 256, 6, "plain"), (3, 257, 6, "plain"), (3, 700, 0, "plain"),
+                                                 (3, 1024, 3, "plain"), (4100, 1000, 2, "plain")])
+def test_logprobs_laid_out(dev, dtype, rows, vocab, top, kind):
+    test_logprobs(dev, dtype, rows, vocab, top, kind)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,vocab,kind", [(2, 4096, "plain"), (2, 8191, "plain"), (2, 8193, "plain")])
+def test_logprobs_gradient_laid_out(dev, dtype, rows, vocab, kind):
+    test_logprobs_gradient(dev, dtype, rows, vocab, kind)
