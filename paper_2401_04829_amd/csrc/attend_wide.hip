@@ -11,7 +11,10 @@
 // values of the 32 that it has weighed.  Keys and values come from the cache
 // to registers and from there to LDS in tiles of 64 (32 where a head is wider
 // than 128), one barrier per tile; keys are half a tile (a tile) further than
-// values.
+// values.  32 bf16 heads over 8 of 128: 10,000 rows on 417 shared and up to 4 own
+// tokens 163 us, 2,002 rows on 3,851 shared ones 170 us (126 GFLOP with the
+// hidden pairs, 740 TFLOP/s; 950 per further key); by the kernel of 16 queries
+// to a wavefront 1,000 rows on 512 take 112 us, here 60.
 //
 // The layout is the transposed one of the other kernels on 32 x 32 x 16
 // instructions: S^T = K Q^T leaves query = lane % 32 and keys in registers,
