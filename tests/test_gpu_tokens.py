@@ -525,3 +525,28 @@ def test_logprobs_laid_out(dev, dtype, rows, vocab, top, kind):
 @pytest.mark.parametrize("rows,vocab,kind", [(2, 4096, "plain"), (2, 8191, "plain"), (2, 8193, "plain")])
 def test_logprobs_gradient_laid_out(dev, dtype, rows, vocab, kind):
     test_logprobs_gradient(dev, dtype, rows, vocab, kind)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,kv,share,dim,page,longest", [(700, 32, 1, 8, 64, 1500), (2100, 32, 2, 16, 16, 600)])
+def test_attention_of_more_keys_than_the_splits_hold(dev, dtype, rows, kv, share, dim, page, longest):
+    """So many rows that a wavefront comes back for further keys of its row;
+    the rows draw on one pool of pages, as rows with a common beginning do."""
+    print("further keys", dtype, rows, kv, share, dim, page, longest, flush=True)
+    gen = _gen(dev, rows)
+    cache = _cache(gen, dev, dtype, 97, page, kv, dim)
+    width = -(-longest // page)
+    table = torch.randint(0, 97, (rows, width), generator=gen, device=dev).to(torch.int32)
+    n = torch.randint(0, 300, (rows,), generator=gen, device=dev).to(torch.int32)
+    n[::50] = longest
+    n[1::50] = longest - 243
+    q = torch.randn((rows, kv * share, dim), generator=gen, device=dev).to(dtype)
+    out, lse = A.attend(cache, q, table, n, max_length=longest, return_lse=True)
+    few = torch.unique(torch.cat([torch.arange(0, rows, 50), torch.arange(1, rows, 50), torch.tensor([2, rows - 1])]))
+    ref = _attend64(cache, q[few], dim ** -0.5, table[few], n[few])
+    _check_attend(cache, q[few], out[few], lse[few], ref, float(cache.v.abs().max()))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_coalitions_of_more_keys_than_the_splits_hold(dev, dtype):
+    test_attention_of_coalitions(dev, dtype, 1, 20000, 32, 1, 8, 16, [600], 1, 0)
