@@ -18,7 +18,7 @@
 //
 // Rows that do not see a position must not be reached by what it holds.  Its
 // score is replaced by -inf, and 0 times a finite value is 0; where a result
-// comes out non-finite, the workgroup's queries are done again by a slow path
+// comes out non-finite, the queries beside it are done again by a slow path
 // that skips the positions each row does not see.
 #include "attend.h"
 

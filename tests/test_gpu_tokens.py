@@ -550,3 +550,50 @@ def test_attention_of_more_keys_than_the_splits_hold(dev, dtype, rows, kv, share
 @pytest.mark.parametrize("dtype", TYPES)
 def test_coalitions_of_more_keys_than_the_splits_hold(dev, dtype):
     test_attention_of_coalitions(dev, dtype, 1, 20000, 32, 1, 8, 16, [600], 1, 0)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_a_cache_past_32_bits(dev, dim):
+    """Pages whose elements lie beyond 2^31 give what the same pages give in a
+    small cache, bit for bit: append, own tokens, shared parts of few and of
+    many queries."""
+    print("large cache", dim, flush=True)
+    gen, page, kv, rows = _gen(dev, dim), 16, 2, 64
+    per = page * kv * dim
+    last = 2 ** 31 // per + 80                    # pages; the last ones are used
+    big = A.PagedCache(torch.empty((last, page, kv, dim), dtype=torch.bfloat16, device=dev),
+                       torch.empty((last, page, kv, dim), dtype=torch.bfloat16, device=dev))
+    small = _cache(gen, dev, torch.bfloat16, 80, page, kv, dim)
+    big.k[-80:], big.v[-80:] = small.k, small.v
+    table = torch.arange(rows, device=dev).view(rows, 1).to(torch.int32)
+    shared = (64 + torch.randperm(16, generator=gen, device=dev)).view(1, 16).to(torch.int32)
+    n = torch.randint(1, 16, (rows,), generator=gen, device=dev).to(torch.int32)
+    sl = torch.tensor([251], dtype=torch.int32, device=dev)
+    masks = torch.randint(-2 ** 62, 2 ** 62, (rows, 4), generator=gen, device=dev)
+    q = torch.randn((rows, 2 * kv, dim), generator=gen, device=dev).to(torch.bfloat16)
+    new = torch.randn((rows, kv, dim), generator=gen, device=dev).to(torch.bfloat16)
+    got = []
+    for cache, add in ((small, 0), (big, last - 80)):
+        A.append_tokens(cache, new, -new, table + add, n)
+        got.append([A.attend(cache, q, table + add, n + 1, return_lse=True),
+                    A.attend(cache, q, table + add, n + 1, shared_table=shared + add, shared_lengths=sl, masks=masks,
+                             num_players=251, return_lse=True),
+                    A.attend(cache, q[:5], table[:5] + add, n[:5] + 1, shared_table=shared + add, shared_lengths=sl,
+                             masks=masks[:5], num_players=251, return_lse=True), (cache.k[-80:], cache.v[-80:])])
+    for a, b in zip(*got):
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    ref = _attend64(small, q, dim ** -0.5, table, n + 1)
+    _check_attend(small, q, *got[1][0], ref, float(small.v.abs().max()))
+
+
+def test_logits_past_32_bits(dev):
+    gen, vocab = _gen(dev, 5), 5001
+    flat = torch.empty(2 ** 31 + 4 * vocab, dtype=torch.bfloat16, device=dev)
+    x = flat.as_strided((2, vocab), (2 ** 31 + 3, 1))
+    x.copy_(torch.randn((2, vocab), generator=gen, device=dev))
+    t = torch.tensor([17, 4999], device=dev)
+    a, b = A.token_logprobs(x, t, 7), A.token_logprobs(x.contiguous(), t, 7)
+    assert all(torch.equal(i, j) for i, j in zip(a, b))
+    g = torch.tensor([1.0, -2.0], device=dev)
+    want = A.token_logprobs_backward(x.contiguous(), t, b.lse, b.entropy, g, g)
+    assert torch.equal(A.token_logprobs_backward(x, t, a.lse, a.entropy, g, g, out=x), want)
