@@ -597,3 +597,48 @@ def test_logits_past_32_bits(dev):
     g = torch.tensor([1.0, -2.0], device=dev)
     want = A.token_logprobs_backward(x.contiguous(), t, b.lse, b.entropy, g, g)
     assert torch.equal(A.token_logprobs_backward(x, t, a.lse, a.entropy, g, g, out=x), want)
+
+
+def test_calls_replay_from_a_graph(dev):
+    """Append, attention (split and joined, with a shared part and masks), log
+    probabilities and their gradient, captured once and replayed on new inputs
+    with other work between, give what the calls themselves give."""
+    gen, kv, dim, rows, page = _gen(dev, 3), 2, 64, 40, 16
+    cache = _cache(gen, dev, torch.bfloat16, 200, page, kv, dim)
+    table = (100 + torch.arange(rows, device=dev)).view(rows, 1).to(torch.int32)
+    shared = torch.randperm(100, generator=gen, device=dev).view(1, 100).to(torch.int32)
+    sl = torch.tensor([1511], dtype=torch.int32, device=dev)
+    n = torch.zeros(rows, dtype=torch.int32, device=dev)
+    ins = [torch.empty((rows, kv, dim), dtype=torch.bfloat16, device=dev) for _ in range(2)]
+    q = torch.empty((rows, 2 * kv, dim), dtype=torch.bfloat16, device=dev)
+    masks = torch.empty((rows, 24), dtype=torch.int64, device=dev)
+    head = torch.randn((2 * kv * dim, 5001), generator=gen, device=dev)
+    logits, t = torch.empty((rows, 5001), device=dev), torch.randint(0, 5001, (rows,), generator=gen, device=dev)
+
+    def draw():
+        for x in (*ins, q, logits):
+            x.copy_(torch.randn(x.shape, generator=gen, device=dev))
+        masks.copy_(torch.randint(-2 ** 62, 2 ** 62, masks.shape, generator=gen, device=dev))
+
+    def calls():
+        A.append_tokens(cache, *ins, table, n)
+        out, lse = A.attend(cache, q, table, n + 1, shared_table=shared, shared_lengths=sl, masks=masks, num_players=1511,
+                            return_lse=True)
+        r = A.token_logprobs(logits, t, 9)
+        return [out, lse, *r, A.token_logprobs_backward(logits, t, r.lse, grad_logprob=r.logprob)]
+    draw()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        calls()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = calls()
+    for _ in range(4):
+        draw()
+        graph.replay()
+        torch.cuda.synchronize()
+        kept = [x.clone() for x in got]
+        assert all(torch.equal(a, b) for a, b in zip(kept, calls()))
+        (head @ head.T).sum().item()
