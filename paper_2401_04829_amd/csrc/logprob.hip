@@ -103,10 +103,11 @@ __device__ __forceinline__ void wave_sum(Stats& a) {
   }
 }
 
-// Whole numbers in the order of the floats (-0 and 0 alike, NaN above all).
+// Whole numbers in the order of the floats (-0 and 0 alike, NaN above all; none
+// is all ones, so that every key is below the one that a search starts from).
 __device__ __forceinline__ uint32_t ordered(float x) {
   const uint32_t b = __float_as_uint(x + 0.f);
-  if (x != x) return 0xFFFFFFFFu;
+  if (x != x) return 0xFFFFFFFEu;
   return b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float unordered(uint32_t o) {
