@@ -243,15 +243,27 @@ class _Logprob(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, grad_logprob, grad_entropy):
-        logits, targets, lse, entropy = ctx.saved_tensors
+        return _LogprobGradient.apply(*ctx.saved_tensors, grad_logprob, grad_entropy), None
+
+
+class _LogprobGradient(torch.autograd.Function):
+    """The gradient as a node of its own, so that differentiating it again (by
+    the logits or the incoming gradients) raises and is not taken for 0."""
+    @staticmethod
+    def forward(ctx, logits, targets, lse, entropy, grad_logprob, grad_entropy):
         grads = (None if g is None else g.float().contiguous() for g in (grad_logprob, grad_entropy))
-        return token_logprobs_backward(logits, targets, lse, entropy, *grads), None
+        return token_logprobs_backward(logits, targets, lse, entropy, *grads)
+
+    @staticmethod
+    def backward(ctx, grad):
+        raise RuntimeError("differentiable_logprobs has a first derivative only")
 
 
 def differentiable_logprobs(logits, targets):
     """Log probabilities of `targets` (int64 [rows]) and entropies of logits
     [rows, vocabulary] with their gradient by the logits (autograd), for
-    gradient attributions and training."""
+    gradient attributions and training.  The gradient is of first order:
+    differentiating it again raises."""
     return _Logprob.apply(logits, targets)
 
 
