@@ -9,11 +9,15 @@ values with the library's sampler and least squares.
 
 Torch provides device memory and streams; the work runs in libgnnshap.so on
 the current stream.  Every tensor must be on the cache's (the logits') device.
+Of these calls only `differentiable_logprobs` has a derivative: the others
+refuse tensors that require a gradient (unless under torch.no_grad()) or carry
+a tangent.
 """
 import math
 from typing import NamedTuple
 
 import torch
+from torch.autograd import forward_ad
 
 from . import _lib as L
 
@@ -30,6 +34,19 @@ def _need(ok, what):
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
+
+
+def _no_derivative(call, *tensors):
+    """Refuses tensors through which autograd would miss `call`'s derivative."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError(f"{call} has no derivative, and a tensor that it got requires a gradient: call it "
+                                 "under torch.no_grad() or with that tensor detached")
+    if forward_ad._current_level >= 0:
+        for t in tensors:
+            if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+                raise ValueError(f"{call} has no derivative, and a tensor that it got carries a tangent")
 
 
 def _on(device, call, *args):
@@ -96,6 +113,7 @@ def append_tokens(cache, k, v, table, index, rows=None, positions=None, q=None, 
     [tokens, heads, head dim] of the same tokens, which are returned (in
     q_out, which may be q).  info: int32 [1], set to 1 on an index out of
     range."""
+    _no_derivative("append_tokens", k, v, q, cache.k, cache.v)
     dtype, dev, dim = cache.dtype, cache.device, cache.head_dim
     n = k.shape[0]
     kp = _heads(k, "k", cache.kv_heads, dim, dtype, dev)
@@ -136,6 +154,7 @@ def attend(cache, q, table=None, lengths=None, max_length=None, shared_table=Non
     None for 1 / sqrt(head dim).  Returns out, or (out, lse) with the log of
     the sum of exponentials, float32 [rows, heads]; a row that sees nothing
     has out 0 and lse -inf."""
+    _no_derivative("attend", q, cache.k, cache.v)
     dtype, dev, dim = cache.dtype, cache.device, cache.head_dim
     qp = _heads(q, "q", None, dim, dtype, dev)
     rows, heads = q.shape[0], q.shape[1]
@@ -196,6 +215,7 @@ def token_logprobs(logits, targets=None, top=0, info=None):
     rank of the tokens `targets` (int64 [rows]; negative or None: no token, 0
     and -1), entropy, and the `top` most likely tokens (at most 64; of equal
     logits the lowest token first).  Returns a TokenLogprobs."""
+    _no_derivative("token_logprobs (but for differentiable_logprobs)", logits)
     dtype = _check_logits(logits)
     (rows, vocab), dev = logits.shape, logits.device
     logprob, entropy, lse = torch.empty((3, rows), dtype=torch.float32, device=dev).unbind(0)
@@ -218,6 +238,7 @@ def token_logprobs_backward(logits, targets, lse, entropy=None, grad_logprob=Non
     sum(grad_logprob * logprob) + sum(grad_entropy * entropy), in the logits'
     type.  lse and entropy as token_logprobs gave them; out may be the logits
     themselves."""
+    _no_derivative("token_logprobs_backward", logits, lse, entropy, grad_logprob, grad_entropy)
     dtype = _check_logits(logits)
     (rows, vocab), dev = logits.shape, logits.device
     out = torch.empty((rows, vocab), dtype=logits.dtype, device=dev) if out is None else out

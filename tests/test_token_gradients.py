@@ -58,3 +58,57 @@ def test_a_first_derivative_with_a_graph_and_without(stand_ins):
     assert not a.requires_grad and torch.equal(a, b)
     A.differentiable_logprobs(x, t)[0].sum().backward()
     assert torch.equal(x.grad, a)
+
+
+class _Reached(Exception):
+    pass
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """Each call without a derivative, given its floating tensors by name, up
+    to where the library would be called."""
+    def reached(*_):
+        raise _Reached
+    for name in ("gnnshap_cache_append", "gnnshap_cache_attend_workspace", "gnnshap_token_logprobs_workspace",
+                 "gnnshap_token_logprobs_backward"):
+        monkeypatch.setattr(A.L, name, reached)
+    monkeypatch.setattr(A, "_on", reached)
+    monkeypatch.setattr(A, "_check_logits", lambda x: 0)
+    i32 = dict(dtype=torch.int32)
+    t, table = torch.zeros(3, dtype=torch.int64), torch.zeros((3, 1), **i32)
+
+    def cache(x):
+        c = A.PagedCache.__new__(A.PagedCache)
+        c.k, c.v, c.kv_heads, c.head_dim, c.page_size = x["ck"], x["cv"], 2, 8, 4
+        c.dtype, c.device, c._c = torch.float32, torch.device("cpu"), None
+        return c
+    return {
+        "append": (dict(k=(3, 2, 8), v=(3, 2, 8), q=(3, 4, 8), ck=(1, 4, 2, 8), cv=(1, 4, 2, 8)),
+                   lambda x: A.append_tokens(cache(x), x["k"], x["v"], table, torch.zeros(3, **i32), q=x["q"])),
+        "attend": (dict(q=(3, 4, 8), ck=(1, 4, 2, 8), cv=(1, 4, 2, 8)),
+                   lambda x: A.attend(cache(x), x["q"], table, torch.zeros(3, **i32))),
+        "logprobs": (dict(x=(3, 5)), lambda x: A.token_logprobs(x["x"], t)),
+        "backward": (dict(x=(3, 5), lse=(3,), entropy=(3,), gl=(3,), ge=(3,)),
+                     lambda x: A.token_logprobs_backward(x["x"], t, x["lse"], x["entropy"], x["gl"], x["ge"]))}
+
+
+@pytest.mark.parametrize("name", ["append", "attend", "logprobs", "backward"])
+def test_calls_without_a_derivative_refuse_what_needs_one(calls, name):
+    shapes, call = calls[name]
+    x = {k: torch.zeros(s) for k, s in shapes.items()}
+    with pytest.raises(_Reached):
+        call(x)
+    for one in shapes:
+        y = dict(x, **{one: torch.zeros(shapes[one], requires_grad=True)})
+        with pytest.raises(ValueError, match="has no derivative"):
+            call(y)
+        with torch.no_grad(), pytest.raises(_Reached):
+            call(y)
+        with pytest.raises(_Reached):
+            call({k: v.detach() for k, v in y.items()})
+        with torch.autograd.forward_ad.dual_level():
+            with pytest.raises(_Reached):
+                call(x)
+            with pytest.raises(ValueError, match="carries a tangent"):
+                call(dict(x, **{one: torch.autograd.forward_ad.make_dual(x[one], torch.ones(shapes[one]))}))
