@@ -288,6 +288,16 @@ def differentiable_logprobs(logits, targets):
     return _Logprob.apply(logits, targets)
 
 
+def _batches(rows, batch):
+    """Bounds of batches of at most `batch` rows, of which the last has two at
+    least: one row alone would be the full coalition, so the batch before it
+    gives it one."""
+    ends = list(range(batch, rows, batch)) + [rows]
+    if len(ends) > 1 and rows - ends[-2] == 1:
+        ends[-2] -= 1
+    return list(zip([0] + ends[:-1], ends))
+
+
 class AnswerExplainer:
     """Shapley values of prompt tokens for a model's answer (Alg. 1 of the
     paper with tokens as players): the sampler's coalitions, their values from
@@ -320,12 +330,12 @@ class AnswerExplainer:
         _on(masks.device, L.gnnshap_sample_coalitions, plan, classes, masks.data_ptr(), weights.data_ptr(),
             ws.data_ptr(), ws.numel())
         y = torch.empty(k + 2, dtype=torch.float32, device=dev)
-        for b in range(0, k + 2, self.batch):
-            part = masks[b:b + self.batch]
+        for b, end in _batches(k + 2, self.batch):
+            part = masks[b:end]
             got = self.value(part, m)
             _need(got.shape == (part.shape[0],) and got.dtype == torch.float32,
                   "value: one float32 number per coalition is needed")
-            y[b:b + self.batch] = got
+            y[b:end] = got
         phi = torch.empty(m, dtype=torch.float32, device=dev)
         info = torch.empty(1, dtype=torch.int32, device=dev)
         nbytes = L.gnnshap_solve_workspace(plan)

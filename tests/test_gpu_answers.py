@@ -128,3 +128,21 @@ def test_gradient_through_autograd(dev):
     e = -(logp.exp() * logp).sum(1)
     (2 * logp.gather(1, t[:, None]).sum() - 0.3 * (e * torch.arange(7, device=dev)).sum()).backward()
     assert float((x.grad.double() - y.grad).abs().max()) <= 2.0 ** -20 * 8 * 4
+
+
+def test_last_batch_ends_with_the_empty_and_the_full_coalition(dev):
+    """Whatever the number of rows leaves over; and the batches do not change what comes out."""
+    want = None
+    for batch in (16384, 2, 3, 17, 33, 100):
+        parts = []
+
+        def value(masks, m):
+            parts.append(masks)
+            return masks[:, 0].float()
+        e = A.AnswerExplainer(value, dev, batch=batch).explain(10, 98, 1)
+        assert all(p.shape[0] <= batch for p in parts)
+        assert parts[-1].shape[0] >= 2 and parts[-1][-2:, 0].tolist() == [0, 1023]
+        got = torch.cat(parts), e.y, e.f_empty_full, e.phi
+        want = got if want is None else want
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert {(got[0].shape[0]) % b == 1 for b in (2, 3, 17, 33, 100)} == {False, True}

@@ -129,3 +129,13 @@ def test_tensors_that_are_refused():
         A.PagedCache(x[0], x[0])
     with pytest.raises(ValueError):
         A.token_logprobs(torch.zeros((2, 5)), None)     # not on a GPU
+
+
+@pytest.mark.parametrize("batch", [2, 3, 4, 7, 100])
+def test_batches_of_coalitions(batch):
+    """All rows once, in order, and the last two, the empty and the full coalition, in one batch."""
+    for rows in range(2, 60):
+        parts = A._batches(rows, batch)
+        assert [b for b, _ in parts] == [0] + [e for _, e in parts[:-1]] and parts[-1][1] == rows
+        sizes = [e - b for b, e in parts]
+        assert all(1 <= n <= batch for n in sizes) and sizes[-1] >= 2
