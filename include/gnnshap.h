@@ -620,7 +620,7 @@ int gnnshap_cache_attend_workspace(const gnnshap_cache* cache, const gnnshap_que
  * positions j, out = sum_j exp(s_j) v_j / sum_j exp(s_j) and lse =
  * log sum_j exp(s_j), per head, with the statistics and sums in fp32 (the
  * weights exp(s_j - max) enter the product with the values in the values'
- * type).  A row that sees nothing, or whose every score is -inf, has out 0
+ * type, fp16 ones 2^14 times larger, so that small ones keep their bits).  A row that sees nothing, or whose every score is -inf, has out 0
  * and lse -inf.  Keys and values of positions that a row does not see do not
  * reach it, whatever they hold (NaN and infinities too).  EINVAL: sizes,
  * NULL arrays; EUNSUPPORTED: head_dim, dtype, parts of more than 2^30 tokens;

@@ -13,6 +13,16 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kWaves = 4;
 constexpr int kChunk = 32;  // keys of a wavefront's step
 
+// The exponent of the largest weight.  Weights enter the product with the
+// values in the values' type; fp16 has no numbers below 2^-24, so a weight of 1
+// or less would be off by 2^-25 and many small ones would be lost (2,048 keys,
+// of which one weighs 1 and the others 2^-25.5 each: 12 % of those).  Carried
+// 2^14 larger, of which fp16 holds 65,504, they keep 11 bits down to 2^-28 of the
+// largest, at no cost: the running maximum m that scores are taken from is kept
+// that much lower, so that l and O belong to it as they always do.
+template <class T>
+constexpr float kUp = std::is_same_v<T, f16_t> ? 14.f : 0.f;
+
 // One part of the rows' contexts: `r` consecutive rows share each row of its
 // table.  A group's rows times the query heads of a kv head are its queries,
 // in tiles; a wavefront (a workgroup of the wide kernel) takes a tile over
@@ -92,7 +102,10 @@ __device__ __forceinline__ T* out_of(const AttendArgs& a, int64_t row, int head)
   return static_cast<T*>(a.q.out) + row * a.q.out_row_stride + head * a.q.out_head_stride;
 }
 
-__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : m * kLn2 + logf(l); }
+template <class T>
+__device__ __forceinline__ float lse_of(float m, float l) {
+  return l == 0.f ? -INFINITY : (m + kUp<T>) * kLn2 + logf(l * __builtin_exp2f(-kUp<T>));
+}
 
 struct Place {  // what a wavefront or workgroup works on
   int64_t group;
@@ -243,7 +256,7 @@ __device__ void attend_slowly(const AttendArgs& a, const Part& part, const Place
       if (!a.direct)
         a.part_ml[p] = make_float2(m, l);
       else if (a.q.lse)
-        a.q.lse[row * a.q.heads + head] = lse_of(m, l);
+        a.q.lse[row * a.q.heads + head] = lse_of<T>(m, l);
     }
   }
 }

@@ -162,7 +162,7 @@ struct State {
     }
     top = fmaxf(top, __shfl_xor(top, 16));
     top = fmaxf(top, __shfl_xor(top, 32));
-    top = fmaxf(top, m);
+    top = fmaxf(top - kUp<T>, m);
     const float use = top == -INFINITY ? 0.f : top, down = __builtin_amdgcn_exp2f(m - use);
     m = top;
     l *= down;
@@ -339,7 +339,7 @@ __global__ __launch_bounds__(64 * kWaves, DP * sizeof(T) <= 256 && RT == 1 ? 2 :
       if (!a.direct)
         a.part_ml[p] = make_float2(st[t].m, l);
       else if (a.q.lse)
-        a.q.lse[row[t] * a.q.heads + head] = lse_of(st[t].m, l);
+        a.q.lse[row[t] * a.q.heads + head] = lse_of<T>(st[t].m, l);
     }
   }
   if (__ballot(bad)) attend_slowly<T>(a, part, at, q0, kQueries);
@@ -434,7 +434,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_attend_join(AttendArgs a)
     for (int e = 0; e < 4; ++e) done.v[e] = static_cast<T>(o[e] * inv);
     store_pack(out_of<T>(a, row, head) + 4 * lane, done);
   }
-  if (lane == 0 && a.q.lse) a.q.lse[row * a.q.heads + head] = lse_of(m, l);
+  if (lane == 0 && a.q.lse) a.q.lse[row * a.q.heads + head] = lse_of<T>(m, l);
 }
 
 int check_queries(const gnnshap_cache* c, const gnnshap_queries* q) {

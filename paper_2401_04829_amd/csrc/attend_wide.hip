@@ -139,13 +139,13 @@ struct WideState {
     return __uint_as_float(static_cast<uint32_t>(static_cast<int32_t>(off << (31 - bit)) >> 31) & 0xFF800000u);
   }
   static __device__ __forceinline__ uint32_t off_bits(uint32_t bits) { return ~bits >> (4 * (threadIdx.x >> 5 & 1)); }
-  // Raises the running maximum to `top`, this lane's largest score.  O is
+  // Raises the running maximum (2^kUp below it) to `top`, this lane's largest score.  O is
   // scaled down whenever a query of the wavefront has a new maximum: leaving m
   // up to 2^8 below it saves 6 % of the time, but then the largest weights are
   // no longer rounded exactly, and the error of 16-bit outputs grows from 1.2
   // to 1.4 times that of their own rounding.
   __device__ __forceinline__ void raise(float top, float scale) {
-    top = fmaxf(top, other_half(top)) * scale;
+    top = fmaf(fmaxf(top, other_half(top)), scale, -kUp<T>);
     if (__ballot(top > m)) {
       const float up = fmaxf(top, m), use = up == -INFINITY ? 0.f : up, down = __builtin_amdgcn_exp2f(m - use);
       m = up;
@@ -468,7 +468,7 @@ __global__ __launch_bounds__(64 * kWaves, DP <= 128 ? 2 : 1) void k_cache_attend
       if (!a.direct)
         a.part_ml[p] = make_float2(st.m, l);
       else if (a.q.lse)
-        a.q.lse[row * a.q.heads + head] = lse_of(st.m, l);
+        a.q.lse[row * a.q.heads + head] = lse_of<T>(st.m, l);
     }
   }
   if (__ballot(bad)) attend_slowly<T>(a, part, at, q0, 32);

@@ -33,3 +33,41 @@ def test_alternatives_of_rows_with_nan_are_tokens(dev, dtype, vocab, top):
     for ids in r.top_id.tolist():
         assert all(0 <= i < vocab for i in ids) and len(set(ids)) == top, ids
     assert bool(r.top_logprob.isnan().all()) and bool(r.lse.isnan().all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,share,shared,own", [(1, 1, 0, 2048), (3, 5, 0, 700), (1, 4, 2048, 0), (260, 20, 0, 1100),
+                                                   (64, 4, 2048, 0), (33, 1, 900, 20), (5, 2, 900, 20), (1, 1, 200, 33)])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_small_weights_are_not_lost(dev, dtype, dim, rows, share, shared, own):
+    """The first of n keys has score 0 and value 0, the others score -25.5
+    (in powers of two) and value 1,024, so that only small weights give the
+    output, o = 1024 w / (1 + w) with w = (n - 1) 2^-25.5.  In fp16 a weight
+    times 2^14 is a normal number and off by 2^-11 relative, in bf16 by 2^-8;
+    the exponent is off by 2^-19, sums by (n + 32) 2^-24; then one rounding.
+    The lse is within 2^-22 of log(1 + w) by a sum of (n + 32) additions."""
+    print("small weights", dtype, dim, rows, share, shared, own, flush=True)
+    page, kv, n = 16, 2, shared + own
+    per_s, per_o = -(-shared // page), -(-own // page)
+    k = torch.zeros((per_s + rows * per_o, page, kv, dim), dtype=dtype, device=dev)
+    v = torch.full_like(k, 1024.0)
+    k[..., 0] = -25.5
+    first = torch.zeros(1, dtype=torch.int64, device=dev) if shared else per_o * torch.arange(rows, device=dev)
+    k[first, 0, :, 0] = 0.0
+    v[first, 0] = 0.0
+    cache = A.PagedCache(k, v)
+    q = torch.zeros((rows, kv * share, dim), dtype=dtype, device=dev)
+    q[..., 0] = 1.0
+    i32 = dict(dtype=torch.int32, device=dev)
+    a = {}
+    if own:
+        a = dict(table=per_s + torch.arange(rows * per_o, **i32).view(rows, per_o), lengths=torch.full((rows,), own, **i32))
+    if shared:
+        a |= dict(shared_table=torch.arange(per_s, **i32)[None], shared_lengths=torch.full((1,), shared, **i32))
+    out, lse = A.attend(cache, q, scale=math.log(2.0), return_lse=True, **a)
+    w = (n - 1) * 2.0 ** -25.5
+    want = 1024 * w / (1 + w)
+    u = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}[dtype]
+    tol = want * (2 * u + 2.0 ** -18 + (n + 32) * 2.0 ** -24)
+    assert float((out.double() - want).abs().max()) <= tol
+    assert float((lse.double() - math.log1p(w)).abs().max()) <= 2.0 ** -22 + (n + 32) * 2.0 ** -24
