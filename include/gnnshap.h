@@ -642,14 +642,16 @@ typedef struct {
   int32_t* rank;            /* [dev] num_rows: how many logits are larger than the given token's */
   float* top_logprob;       /* [dev] num_rows x top: log probabilities in falling order */
   int32_t* top_id;          /* [dev] num_rows x top: their tokens; of equal logits the lowest token first */
+  float* maximum;           /* [dev] num_rows: the largest logit */
+  float* log_sum;           /* [dev] num_rows: log sum exp(x - maximum); lse is the sum of the two, rounded */
 } gnnshap_logits;
 
 int gnnshap_token_logprobs_workspace(const gnnshap_logits* logits, size_t* bytes);
 
 /* One pass over the logits.  A logit of -inf is a token of probability 0 (log
- * probability -inf); a row of nothing else has lse, logprob and top_logprob
- * -inf and entropy 0.  A row with a NaN or +inf has lse, logprob, entropy and
- * top_logprob NaN, and its rank and top_id are unspecified (tokens of the
+ * probability -inf); a row of nothing else has lse, logprob, maximum and
+ * top_logprob -inf, entropy and log_sum 0.  A row with a NaN or +inf has lse,
+ * logprob, entropy, log_sum and top_logprob NaN, and its rank and top_id are unspecified (tokens of the
  * vocabulary).  EINVAL: sizes, NULL logits; EUNSUPPORTED: dtype, a vocabulary
  * over 2^30; ECAPACITY: workspace. */
 int gnnshap_token_logprobs(const gnnshap_logits* logits, int32_t* info, void* ws, size_t ws_bytes, void* stream);
@@ -660,7 +662,10 @@ int gnnshap_token_logprobs(const gnnshap_logits* logits, int32_t* info, void* ws
  * written in the logits' type to grad + b grad_stride (which may be the
  * logits themselves, with their stride).  Reads num_rows, vocab, dtype,
  * logits, row_stride, targets, and lse and entropy as
- * gnnshap_token_logprobs wrote them; g_logprob and g_entropy [dev, num_rows]
+ * gnnshap_token_logprobs wrote them, and in place of lse maximum and log_sum
+ * where both are given: p is then as exact for logits far from 0, of whose lse
+ * fp32 keeps few bits behind the point (2^-24 |lse|, which p is off by), as for
+ * others; g_logprob and g_entropy [dev, num_rows]
  * may be NULL (0); entropy is read with g_entropy only.  A row without a
  * target has no g_logprob.  A row of lse -inf has gradient 0.  EINVAL,
  * EUNSUPPORTED as above. */

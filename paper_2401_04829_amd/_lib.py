@@ -77,7 +77,7 @@ class gnnshap_queries(ctypes.Structure):
 class gnnshap_logits(ctypes.Structure):
     _fields_ = [("dtype", c_i32), ("top", c_i32), ("num_rows", c_i64), ("vocab", c_i64), ("logits", c_vp),
                 ("row_stride", c_i64), ("targets", c_vp), ("logprob", c_vp), ("entropy", c_vp), ("lse", c_vp),
-                ("rank", c_vp), ("top_logprob", c_vp), ("top_id", c_vp)]
+                ("rank", c_vp), ("top_logprob", c_vp), ("top_id", c_vp), ("maximum", c_vp), ("log_sum", c_vp)]
 
 
 _P = ctypes.POINTER

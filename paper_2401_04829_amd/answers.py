@@ -210,11 +210,13 @@ def _check_logits(x):
     return _DTYPES[x.dtype]
 
 
-def token_logprobs(logits, targets=None, top=0, info=None):
+def token_logprobs(logits, targets=None, top=0, info=None, maximum=None, log_sum=None):
     """gnnshap_token_logprobs of logits [rows, vocabulary]: log probability and
     rank of the tokens `targets` (int64 [rows]; negative or None: no token, 0
     and -1), entropy, and the `top` most likely tokens (at most 64; of equal
-    logits the lowest token first).  Returns a TokenLogprobs."""
+    logits the lowest token first).  Returns a TokenLogprobs.  maximum and
+    log_sum (float32 [rows], if given) get the largest logit and the log of the
+    sum of exp(x - maximum), for the gradient of logits far from 0."""
     _no_derivative("token_logprobs (but for differentiable_logprobs)", logits)
     dtype = _check_logits(logits)
     (rows, vocab), dev = logits.shape, logits.device
@@ -225,7 +227,8 @@ def token_logprobs(logits, targets=None, top=0, info=None):
     a = L.gnnshap_logits(dtype, top, rows, vocab, logits.data_ptr(), logits.stride(0),
                          _vector(targets, "targets", torch.int64, (rows,), dev), logprob.data_ptr(),
                          entropy.data_ptr(), lse.data_ptr(), rank.data_ptr(), r.top_logprob.data_ptr(),
-                         top_id.data_ptr())
+                         top_id.data_ptr(), _vector(maximum, "maximum", torch.float32, (rows,), dev),
+                         _vector(log_sum, "log_sum", torch.float32, (rows,), dev))
     nbytes = L.gnnshap_token_logprobs_workspace(a)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
     _on(dev, L.gnnshap_token_logprobs, a, _vector(info, "info", torch.int32, (1,), dev), _ptr(ws), nbytes)
@@ -233,12 +236,14 @@ def token_logprobs(logits, targets=None, top=0, info=None):
 
 
 def token_logprobs_backward(logits, targets, lse, entropy=None, grad_logprob=None, grad_entropy=None, out=None,
-                            info=None):
+                            info=None, maximum=None, log_sum=None):
     """gnnshap_token_logprobs_backward: the gradient by the logits of
     sum(grad_logprob * logprob) + sum(grad_entropy * entropy), in the logits'
     type.  lse and entropy as token_logprobs gave them; out may be the logits
-    themselves."""
-    _no_derivative("token_logprobs_backward", logits, lse, entropy, grad_logprob, grad_entropy)
+    themselves.  With maximum and log_sum, as token_logprobs gave them, which
+    are then read in place of lse, the gradient of logits far from 0 is as exact
+    as that of others (by lse, p is off by 2^-24 |lse|)."""
+    _no_derivative("token_logprobs_backward", logits, lse, entropy, grad_logprob, grad_entropy, maximum, log_sum)
     dtype = _check_logits(logits)
     (rows, vocab), dev = logits.shape, logits.device
     out = torch.empty((rows, vocab), dtype=logits.dtype, device=dev) if out is None else out
@@ -247,7 +252,9 @@ def token_logprobs_backward(logits, targets, lse, entropy=None, grad_logprob=Non
     a = L.gnnshap_logits(dtype, 0, rows, vocab, logits.data_ptr(), logits.stride(0),
                          _vector(targets, "targets", torch.int64, (rows,), dev), None,
                          _vector(entropy, "entropy", torch.float32, (rows,), dev),
-                         _vector(lse, "lse", torch.float32, (rows,), dev))
+                         _vector(lse, "lse", torch.float32, (rows,), dev), None, None, None,
+                         _vector(maximum, "maximum", torch.float32, (rows,), dev),
+                         _vector(log_sum, "log_sum", torch.float32, (rows,), dev))
     _on(dev, L.gnnshap_token_logprobs_backward, a,
         _vector(grad_logprob, "grad_logprob", torch.float32, (rows,), dev),
         _vector(grad_entropy, "grad_entropy", torch.float32, (rows,), dev), out.data_ptr(), out.stride(0),
@@ -258,8 +265,9 @@ def token_logprobs_backward(logits, targets, lse, entropy=None, grad_logprob=Non
 class _Logprob(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, targets):
-        r = token_logprobs(logits, targets)
-        ctx.save_for_backward(logits, targets, r.lse, r.entropy)
+        maximum, log_sum = torch.empty((2, logits.shape[0]), dtype=torch.float32, device=logits.device).unbind(0)
+        r = token_logprobs(logits, targets, maximum=maximum, log_sum=log_sum)
+        ctx.save_for_backward(logits, targets, r.lse, r.entropy, maximum, log_sum)
         return r.logprob, r.entropy
 
     @staticmethod
@@ -271,9 +279,9 @@ class _LogprobGradient(torch.autograd.Function):
     """The gradient as a node of its own, so that differentiating it again (by
     the logits or the incoming gradients) raises and is not taken for 0."""
     @staticmethod
-    def forward(ctx, logits, targets, lse, entropy, grad_logprob, grad_entropy):
+    def forward(ctx, logits, targets, lse, entropy, maximum, log_sum, grad_logprob, grad_entropy):
         grads = (None if g is None else g.float().contiguous() for g in (grad_logprob, grad_entropy))
-        return token_logprobs_backward(logits, targets, lse, entropy, *grads)
+        return token_logprobs_backward(logits, targets, lse, entropy, *grads, maximum=maximum, log_sum=log_sum)
 
     @staticmethod
     def backward(ctx, grad):

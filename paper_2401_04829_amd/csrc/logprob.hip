@@ -214,6 +214,8 @@ __device__ __forceinline__ void write_stats(const LogprobArgs& a, int64_t row, c
                                             bool has, float xt) {
   const bool none = st.s == 0.f;  // every logit is -inf
   if (a.l.lse) a.l.lse[row] = none ? -INFINITY : st.m + logs;
+  if (a.l.maximum) a.l.maximum[row] = st.m;
+  if (a.l.log_sum) a.l.log_sum[row] = none ? 0.f : logs;
   if (a.l.entropy) a.l.entropy[row] = none ? 0.f : logs - kLn2 * (st.w / st.s);
   if (a.l.logprob) a.l.logprob[row] = !has ? 0.f : none ? -INFINITY : (xt - st.m) - logs;
   if (a.l.rank) a.l.rank[row] = has ? rank : -1;
@@ -503,12 +505,13 @@ __global__ __launch_bounds__(256) void k_token_logprobs_grad(GradArgs a) {
     if (a.info) *a.info = 1;
     t = -1;
   }
-  const float lse = a.l.lse[row];
+  // log p = (x - top) - logs; by lse alone p is off by its rounding
+  const float top = a.l.maximum ? a.l.maximum[row] : a.l.lse[row], logs = a.l.maximum ? a.l.log_sum[row] : 0.f;
   const float gl = a.gl && t >= 0 ? a.gl[row] : 0.f;
   const float ge = a.ge ? a.ge[row] : 0.f, ent = a.ge ? a.l.entropy[row] : 0.f;
-  const bool none = lse == -INFINITY;
+  const bool none = top == -INFINITY && logs == 0.f;  // (a row of NaN alone has log_sum NaN)
   const auto d = [&](T xi, int64_t i) {
-    const float logp = static_cast<float>(xi) - lse, p = __builtin_amdgcn_exp2f(logp * kLog2e);
+    const float logp = (static_cast<float>(xi) - top) - logs, p = __builtin_amdgcn_exp2f(logp * kLog2e);
     const float own = i == t ? gl : 0.f;
     const float r = own - p * (gl + ge * ((p == 0.f ? 0.f : logp) + ent));
     return static_cast<T>(none ? 0.f : r);
@@ -660,7 +663,8 @@ extern "C" int gnnshap_token_logprobs_backward(const gnnshap_logits* l, const fl
   if (const int st = check_logits(l)) return st;
   if (grad_stride < 0) return fail(GNNSHAP_EINVAL, "negative stride of the gradient");
   if (l->num_rows == 0) return GNNSHAP_OK;
-  if (!l->logits || !l->lse || !grad || (g_entropy && !l->entropy))
+  if (!l->maximum != !l->log_sum) return fail(GNNSHAP_EINVAL, "maximum and log_sum: both are needed, or neither");
+  if (!l->logits || (!l->lse && !l->maximum) || !grad || (g_entropy && !l->entropy))
     return fail(GNNSHAP_EINVAL, "NULL logits, lse, grad or (with g_entropy) entropy");
   GradArgs a{*l, g_logprob, g_entropy, grad, grad_stride, info};
   hipStream_t s = static_cast<hipStream_t>(stream);

@@ -71,3 +71,55 @@ def test_small_weights_are_not_lost(dev, dtype, dim, rows, share, shared, own):
     tol = want * (2 * u + 2.0 ** -18 + (n + 32) * 2.0 ** -24)
     assert float((out.double() - want).abs().max()) <= tol
     assert float((lse.double() - math.log1p(w)).abs().max()) <= 2.0 ** -22 + (n + 32) * 2.0 ** -24
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("offset", [0.0, -300.0, 20000.0])
+@pytest.mark.parametrize("rows,vocab", [(5, 41), (3, 301), (2, 1000), (3, 5001), (2, 70001), (4100, 3001)])
+def test_gradient_of_logits_far_from_zero(dev, dtype, offset, rows, vocab):
+    """Through autograd, against the gradient from log_softmax in float64.  log
+    p is (x - max) - log s, off by 2^-23 (|log p| + 1) and by log s, whose sum
+    has at most 64 + vocab / 1024 fp32 additions in a row and exponentials off by
+    2^-22 of (1 + their average distance from the maximum, under log(vocab) + 2);
+    p by as much relative, the entropy by that times log(vocab) + 2.  Nothing of
+    it grows with the logits' offset."""
+    print("far", dtype, offset, rows, vocab, flush=True)
+    gen = torch.Generator(dev).manual_seed(vocab)
+    x = (2 * torch.randn((rows, vocab), generator=gen, device=dev) + offset).to(dtype).requires_grad_()
+    t = torch.randint(0, vocab, (rows,), generator=gen, device=dev)
+    gl, ge = (torch.randn(rows, generator=gen, device=dev) for _ in range(2))
+    logp, entropy = A.differentiable_logprobs(x, t)
+    ((logp * gl).sum() + (entropy * ge).sum()).backward()
+    y = x.detach().double()
+    lp = torch.log_softmax(y, 1)
+    p, ent = lp.exp(), -(lp.exp() * lp).sum(1, keepdim=True)
+    a, b = gl.double()[:, None], ge.double()[:, None]
+    hit = torch.arange(vocab, device=dev) == t[:, None]
+    want = a * (hit.double() - p) - b * p * (lp + ent)
+    lg = math.log(vocab) + 2
+    off = 2.0 ** -23 * (lp.abs() + 1) + 2.0 ** -24 * (64 + vocab / 1024 + 4 * lg)
+    u = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}[dtype]
+    tol = u * want.abs() + 2 * off * p * (a.abs() + b.abs() * (lp.abs() + ent + 1)) + off * p * b.abs() * lg \
+        + 2.0 ** -23 * (a.abs() * hit + p * (a.abs() + b.abs() * (lp.abs() + ent))) + 2.0 ** -25 * (dtype == torch.float16) + 1e-37
+    d = (x.grad.double() - want).abs()
+    assert bool((d <= tol).all()), float((d / tol).max())
+
+
+def test_maximum_and_log_sum(dev):
+    """The largest logit itself; -inf and 0 of a row of nothing; NaN where a row has one; for every length of rows."""
+    for vocab in (1, 41, 200, 1000, 3001, 131072):
+        x = torch.randn((7, vocab), generator=torch.Generator(dev).manual_seed(vocab), device=dev) + 1000
+        x[1] = -math.inf
+        x[2, 0] = math.nan
+        x[3, vocab // 2] = math.inf
+        x[5] = math.nan
+        x[6], x[6, -1] = -math.inf, math.nan
+        m, s = torch.full((2, 7), 7.0, device=dev).unbind(0)
+        r = A.token_logprobs(x, torch.zeros(7, dtype=torch.int64, device=dev), min(vocab, 3), maximum=m, log_sum=s)
+        assert torch.equal(m[[0, 1, 4]], x[[0, 1, 4]].amax(1)) and float(s[1]) == 0 and bool(s[[2, 3, 5, 6]].isnan().all())
+        want = torch.log(torch.exp(x.double() - x.double().amax(1, keepdim=True)).sum(1))
+        assert float((s.double() - want)[[0, 4]].abs().max()) <= 2.0 ** -23 * (64 + vocab / 1024 + 4 * (math.log(vocab) + 2))
+        assert torch.equal(r.lse[[0, 1, 4]], (m + s)[[0, 1, 4]])
+        one = torch.ones(7, device=dev)
+        g = A.token_logprobs_backward(x, None, None, r.entropy, None, one, maximum=m, log_sum=s)
+        assert bool((g[1] == 0).all()) and bool(g[[2, 3, 5, 6]].isnan().all())

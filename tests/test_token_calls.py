@@ -139,3 +139,12 @@ def test_batches_of_coalitions(batch):
         assert [b for b, _ in parts] == [0] + [e for _, e in parts[:-1]] and parts[-1][1] == rows
         sizes = [e - b for b, e in parts]
         assert all(1 <= n <= batch for n in sizes) and sizes[-1] >= 2
+
+
+def test_gradient_needs_both_parts_of_lse():
+    lib = L.load()
+    for change in (dict(maximum=P), dict(log_sum=P), dict(lse=None, maximum=P), dict(lse=None, log_sum=P)):
+        assert lib.gnnshap_token_logprobs_backward(_logits(**change), P, P, P, 10, None, None) == L.EINVAL
+    both = dict(lse=None, maximum=P, log_sum=P)
+    assert lib.gnnshap_token_logprobs_backward(_logits(**both, entropy=None), P, P, P, 10, None, None) == L.EINVAL
+    assert lib.gnnshap_token_logprobs_backward(_logits(**both, num_rows=0), P, P, P, 10, None, None) == L.OK
