@@ -74,11 +74,12 @@ __device__ __forceinline__ X together(X x, F f) {
   return x;
 }
 
-// Moves a to the maximum m >= a.m.
+// Moves a to the maximum m >= a.m.  Far below it f is 0, and what it multiplies
+// has to stay finite: up to 2^30 logits times 1e4.
 __device__ __forceinline__ void move_to(Stats& a, float m) {
   if (a.s != 0.f) {  // NaN too
     const float d = (a.m - finite_max(m)) * kLog2e, f = __builtin_amdgcn_exp2f(d);
-    a.w = f * (a.w + a.s * fmaxf(d, -1e30f));
+    a.w = f * (a.w + a.s * fmaxf(d, -1e4f));
     a.s *= f;
   }
   a.m = m;

@@ -123,3 +123,17 @@ def test_maximum_and_log_sum(dev):
         one = torch.ones(7, device=dev)
         g = A.token_logprobs_backward(x, None, None, r.entropy, None, one, maximum=m, log_sum=s)
         assert bool((g[1] == 0).all()) and bool(g[[2, 3, 5, 6]].isnan().all())
+
+
+def test_one_logit_far_above_the_longest_row(dev):
+    """2^30 equal logits and one 2^101 above them: its probability is 1, entropy and log probability 0."""
+    x = torch.zeros((1, 2 ** 30), dtype=torch.bfloat16, device=dev)
+    for at in (0, 5, 2 ** 29 + 77, 2 ** 30 - 1):
+        x[0, at] = 2.0 ** 101
+        r = A.token_logprobs(x, torch.tensor([at], device=dev), 2)
+        assert float(r.entropy) == 0 and float(r.logprob) == 0 and int(r.rank) == 0 and int(r.top_id[0, 0]) == at
+        r = A.token_logprobs(x)
+        assert float(r.entropy) == 0 and float(r.lse) == 2.0 ** 101
+        x[0, at] = 0
+    r = A.token_logprobs(x)
+    assert abs(float(r.entropy) - 30 * math.log(2.0)) < 2.0 ** -18
