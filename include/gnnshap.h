@@ -527,7 +527,9 @@ int gnnshap_gat_explain_batch(const gnnshap_subgraph* sgs, const gnnshap_sample_
  * int32, may be NULL] is set to 1 where a call meets a page, row, position,
  * length or token id out of its range, and left as it is otherwise; the call
  * then reads and writes nothing out of its buffers, and what it returns for
- * that token or row is unspecified. */
+ * that token or row is unspecified.  EUNSUPPORTED is also a size that would need
+ * more than the 2^32 threads of one launch: about 2^24 rows and heads, more where
+ * heads or rows are short. */
 
 enum gnnshap_dtype { GNNSHAP_F32 = 0, GNNSHAP_F16 = 1, GNNSHAP_BF16 = 2 };
 
@@ -620,11 +622,11 @@ int gnnshap_cache_attend_workspace(const gnnshap_cache* cache, const gnnshap_que
  * positions j, out = sum_j exp(s_j) v_j / sum_j exp(s_j) and lse =
  * log sum_j exp(s_j), per head, with the statistics and sums in fp32 (the
  * weights exp(s_j - max) enter the product with the values in the values'
- * type, fp16 ones 2^14 times larger, so that small ones keep their bits).  A row that sees nothing, or whose every score is -inf, has out 0
- * and lse -inf.  Keys and values of positions that a row does not see do not
- * reach it, whatever they hold (NaN and infinities too).  EINVAL: sizes,
- * NULL arrays; EUNSUPPORTED: head_dim, dtype, parts of more than 2^30 tokens;
- * ECAPACITY: workspace. */
+ * type, fp16 ones 2^14 times larger, so that small ones keep their bits).  A row
+ * that sees nothing, or whose every score is -inf, has out 0 and lse -inf.  Keys
+ * and values of positions that a row does not see do not reach it, whatever they
+ * hold (NaN and infinities too).  EINVAL: sizes, NULL arrays; EUNSUPPORTED:
+ * head_dim, dtype, parts of more than 2^30 tokens; ECAPACITY: workspace. */
 int gnnshap_cache_attend(const gnnshap_cache* cache, const gnnshap_queries* queries, int32_t* info, void* ws,
                          size_t ws_bytes, void* stream);
 

@@ -119,6 +119,7 @@ int launch(const AppendArgs& a, hipStream_t s) {
   const int units = a.c.head_dim / (2 * N);
   int x = 1;
   while (x < units && x < 64) x *= 2;
+  if (const int st = gnnshap::check_launch(a.t.num_tokens, x)) return st;
   const int heads = a.q_heads + 2 * a.c.kv_heads, y = std::min(256 / x, heads);
   dim3 grid(static_cast<unsigned>(a.t.num_tokens), static_cast<unsigned>(gnnshap::ceil_div(heads, y)));
   {

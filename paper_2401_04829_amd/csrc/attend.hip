@@ -477,6 +477,14 @@ int check_queries(const gnnshap_cache* c, const gnnshap_queries* q) {
 
 int padded_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 
+// Whether results come from the join (also where there is no context), and its
+// workgroups: one for each query's parts, or for kWaves queries'.
+bool joined(const AttendArgs& a) { return !a.direct || (!a.shared.table && !a.own.table); }
+bool many_parts(const AttendArgs& a) { return a.shared.splits + a.own.splits > 8; }
+int64_t join_workgroups(const AttendArgs& a) {
+  return gnnshap::ceil_div(a.q.num_rows * a.q.heads, many_parts(a) ? 1 : kWaves);
+}
+
 // How the work is laid out over workgroups.
 int lay_out(AttendArgs& a, const gnnshap_cache* c, const gnnshap_queries* q) {
   using gnnshap::ceil_div;
@@ -554,12 +562,13 @@ int lay_out(AttendArgs& a, const gnnshap_cache* c, const gnnshap_queries* q) {
                                                                              : 256;
       p.splits = static_cast<int>(std::min(ceil_div(longest, p.split_keys), at_most(65536)));
     }
-    if (base * p.splits > INT32_MAX) return fail(GNNSHAP_EUNSUPPORTED, "too many workgroups");
+    // a workgroup of the wide kernel per place, of the other one per kWaves
+    if (const int st = check_launch(p.wide ? base * p.splits : ceil_div(base * p.splits, kWaves), 64 * kWaves)) return st;
     p.slot0 = slots;
     slots += p.splits;
   }
   a.direct = slots <= 1;
-  return GNNSHAP_OK;
+  return joined(a) ? check_launch(join_workgroups(a), 64 * kWaves) : GNNSHAP_OK;
 }
 
 size_t carve(AttendArgs& a, void* ws) {
@@ -597,13 +606,13 @@ int launch_all(const AttendArgs& a, hipStream_t s) {
   if (a.shared.table) st = a.shared.wide ? launch_attend_wide(a, s) : launch_tiles<T, DP, false>(a, a.shared, s);
   if (!st && a.own.table && !a.fused) st = launch_tiles<T, DP, true>(a, a.own, s);
   if (st) return st;
-  if (!a.direct || (!a.shared.table && !a.own.table)) {
+  if (joined(a)) {
     GS_TIMED("k_cache_attend_join", s);
-    const int64_t queries = a.q.num_rows * a.q.heads;
-    if (a.shared.splits + a.own.splits > 8)
-      k_cache_attend_join<T, kWaves><<<static_cast<unsigned>(queries), 64 * kWaves, 0, s>>>(a);
+    const unsigned grid = static_cast<unsigned>(join_workgroups(a));
+    if (many_parts(a))
+      k_cache_attend_join<T, kWaves><<<grid, 64 * kWaves, 0, s>>>(a);
     else
-      k_cache_attend_join<T, 1><<<static_cast<unsigned>(ceil_div(queries, kWaves)), 64 * kWaves, 0, s>>>(a);
+      k_cache_attend_join<T, 1><<<grid, 64 * kWaves, 0, s>>>(a);
     GS_LAUNCHED();
   }
   return GNNSHAP_OK;

@@ -575,6 +575,14 @@ enum Way { kShort64, kShort256, kShort1024, kWavefront, kTwoWavefronts, kWorkgro
 struct Shape {
   Way way;
   int parts;
+  int64_t workgroups(int64_t rows) const {
+    switch (way) {
+      case kShort64: return gnnshap::ceil_div(rows, 16);
+      case kTwoWavefronts: return gnnshap::ceil_div(rows, kWaves / 2);
+      case kWorkgroup: return rows * parts;
+      default: return gnnshap::ceil_div(rows, kWaves);
+    }
+  }
 };
 Shape shape_of(const gnnshap_logits& l) {
   if (l.vocab <= 64) return {kShort64, 1};
@@ -606,7 +614,9 @@ extern "C" int gnnshap_token_logprobs_workspace(const gnnshap_logits* l, size_t*
   if (const int st = check_logits(l)) return st;
   LogprobArgs a{};
   a.l = *l;
-  a.parts = shape_of(*l).parts;
+  const Shape shape = shape_of(*l);
+  if (const int st = gnnshap::check_launch(shape.workgroups(l->num_rows), 64 * kWaves)) return st;
+  a.parts = shape.parts;
   *bytes = carve(a, nullptr);
   return GNNSHAP_OK;
   GS_TRY_END
@@ -624,6 +634,7 @@ extern "C" int gnnshap_token_logprobs(const gnnshap_logits* l, int32_t* info, vo
   a.l = *l;
   a.info = info;
   const Shape shape = shape_of(*l);
+  if (const int st = gnnshap::check_launch(shape.workgroups(l->num_rows), 64 * kWaves)) return st;
   a.parts = shape.parts;
   const size_t need = carve(a, ws);
   if (need > 0 && (!ws || ws_bytes < need))
@@ -631,17 +642,16 @@ extern "C" int gnnshap_token_logprobs(const gnnshap_logits* l, int32_t* info, vo
   hipStream_t s = static_cast<hipStream_t>(stream);
   return gnnshap::with_dtype(l->dtype, [&](auto* p) {
     using T = std::remove_pointer_t<decltype(p)>;
-    const auto groups = [&](int rows) { return static_cast<unsigned>(gnnshap::ceil_div(l->num_rows, rows)); };
+    const unsigned grid = static_cast<unsigned>(shape.workgroups(l->num_rows));
     {
       GS_TIMED("k_token_logprobs", s);
       switch (shape.way) {
-        case kShort64: k_token_logprobs_short<T, 16, 4><<<groups(16), 256, 0, s>>>(a); break;
-        case kShort256: k_token_logprobs_short<T, 64, 4><<<groups(4), 256, 0, s>>>(a); break;
-        case kShort1024: k_token_logprobs_short<T, 64, 16><<<groups(4), 256, 0, s>>>(a); break;
-        case kWavefront: k_token_logprobs<T, 1><<<groups(kWaves), 64 * kWaves, 0, s>>>(a); break;
-        case kTwoWavefronts: k_token_logprobs<T, 2><<<groups(kWaves / 2), 64 * kWaves, 0, s>>>(a); break;
-        case kWorkgroup:
-          k_token_logprobs<T, kWaves><<<static_cast<unsigned>(l->num_rows * a.parts), 64 * kWaves, 0, s>>>(a);
+        case kShort64: k_token_logprobs_short<T, 16, 4><<<grid, 256, 0, s>>>(a); break;
+        case kShort256: k_token_logprobs_short<T, 64, 4><<<grid, 256, 0, s>>>(a); break;
+        case kShort1024: k_token_logprobs_short<T, 64, 16><<<grid, 256, 0, s>>>(a); break;
+        case kWavefront: k_token_logprobs<T, 1><<<grid, 64 * kWaves, 0, s>>>(a); break;
+        case kTwoWavefronts: k_token_logprobs<T, 2><<<grid, 64 * kWaves, 0, s>>>(a); break;
+        case kWorkgroup: k_token_logprobs<T, kWaves><<<grid, 64 * kWaves, 0, s>>>(a);
       }
     }
     GS_LAUNCHED();
@@ -674,7 +684,9 @@ extern "C" int gnnshap_token_logprobs_backward(const gnnshap_logits* l, const fl
     const int64_t packs = gnnshap::ceil_div(l->vocab, 16 / sizeof(T));
     int x = 8;
     while (x < 256 && x < packs) x *= 2;
-    const dim3 grid(static_cast<unsigned>(gnnshap::ceil_div(l->num_rows, 256 / x)),
+    const int64_t groups = gnnshap::ceil_div(l->num_rows, 256 / x);
+    if (const int st = gnnshap::check_launch(groups, x)) return st;
+    const dim3 grid(static_cast<unsigned>(groups),
                     static_cast<unsigned>(std::min<int64_t>(gnnshap::ceil_div(packs, x * kGradPacks), 1024)));
     {
       GS_TIMED("k_token_logprobs_grad", s);

@@ -42,6 +42,13 @@ inline int with_dtype(int32_t dtype, F f) {
   }
 }
 
+// GNNSHAP_OK, or the refusal of more threads along an axis than a launch takes.
+inline int check_launch(int64_t workgroups, int64_t threads) {
+  if (workgroups <= INT32_MAX && workgroups * threads < int64_t(1) << 32) return GNNSHAP_OK;
+  return fail(GNNSHAP_EUNSUPPORTED, "%lld workgroups of %lld threads in one launch", static_cast<long long>(workgroups),
+              static_cast<long long>(threads));
+}
+
 // GNNSHAP_OK, or the failure that a cache's description is.
 inline int check_cache(const gnnshap_cache* c) {
   if (!c) return fail(GNNSHAP_EINVAL, "cache is NULL");

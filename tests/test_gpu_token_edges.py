@@ -137,3 +137,17 @@ def test_one_logit_far_above_the_longest_row(dev):
         x[0, at] = 0
     r = A.token_logprobs(x)
     assert abs(float(r.entropy) - 30 * math.log(2.0)) < 2.0 ** -18
+
+
+def test_as_many_rows_as_a_launch_takes(dev):
+    """2^28 - 16 short rows, 2^32 - 256 threads: the last ones as by themselves; 2^28 are refused."""
+    rows, vocab = 2 ** 28 - 16, 3
+    x = torch.empty((rows + 16, vocab), dtype=torch.bfloat16, device=dev)
+    x.normal_(generator=torch.Generator(dev).manual_seed(1))
+    t = torch.arange(rows + 16, device=dev) % vocab
+    with pytest.raises(RuntimeError, match="workgroups"):
+        A.token_logprobs(x, t, 1)
+    r = A.token_logprobs(x[:rows], t[:rows], 1)
+    for b in (0, 2 ** 27 + 5, rows - 40):
+        want = A.token_logprobs(x[b:b + 40], t[b:b + 40].contiguous(), 1)
+        assert all(torch.equal(p[b:min(b + 40, rows)], q[:rows - b]) for p, q in zip(r, want))

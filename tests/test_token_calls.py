@@ -148,3 +148,35 @@ def test_gradient_needs_both_parts_of_lse():
     both = dict(lse=None, maximum=P, log_sum=P)
     assert lib.gnnshap_token_logprobs_backward(_logits(**both, entropy=None), P, P, P, 10, None, None) == L.EINVAL
     assert lib.gnnshap_token_logprobs_backward(_logits(**both, num_rows=0), P, P, P, 10, None, None) == L.OK
+
+
+def test_more_threads_than_a_launch_takes_are_refused():
+    """HIP takes fewer than 2^32 threads along an axis of a launch: sizes past
+    it are unsupported (and no launch of the call is made), those up to it get
+    to the checks behind."""
+    lib, n = L.load(), ctypes.c_size_t()
+    # rows of a workgroup of 256 threads: 16 where rows are short, 4 to 1 where they are longer
+    for vocab, top, rows in ((41, 2, 16), (64, 0, 16), (200, 2, 4), (1000, 0, 4), (1000, 2, 4), (20000, 2, 2), (100000, 2, 1)):
+        a = dict(vocab=vocab, top=top, row_stride=vocab)
+        over, upto = rows << 24, (rows << 24) - rows
+        assert lib.gnnshap_token_logprobs_workspace(_logits(num_rows=over, **a), n) == L.EUNSUPPORTED, vocab
+        assert lib.gnnshap_token_logprobs(_logits(num_rows=over, **a), None, P, 1 << 40, None) == L.EUNSUPPORTED
+        assert lib.gnnshap_token_logprobs_workspace(_logits(num_rows=upto, **a), n) == L.OK
+    # the gradient: x threads side by side, 256 / x rows
+    for vocab, x in ((300, 128), (1025, 256), (50000, 256)):
+        a = _logits(num_rows=(1 << 32) // x * (256 // x), vocab=vocab, row_stride=vocab)
+        assert lib.gnnshap_token_logprobs_backward(a, P, P, P, vocab, None, None) == L.EUNSUPPORTED, vocab
+    # a token's heads: 1 to 16 threads side by side in 16 bits
+    for dim, x in ((256, 16), (128, 8), (8, 1)):
+        c, t = _cache(head_dim=dim), _tokens(num_tokens=min((1 << 32) // x, 1 << 31), rot_dim=0)
+        assert lib.gnnshap_cache_append(c, t, None, None) == L.EUNSUPPORTED, dim
+    # attention: a wavefront to a row and kv head
+    a = dict(num_rows=1 << 25, lengths=P, max_length=16, table_width=1)
+    assert lib.gnnshap_cache_attend_workspace(_cache(), _queries(**a), n) == L.EUNSUPPORTED
+    assert lib.gnnshap_cache_attend(_cache(), _queries(**a), None, None, 0, None) == L.EUNSUPPORTED
+    assert lib.gnnshap_cache_attend_workspace(_cache(), _queries(**dict(a, num_rows=(1 << 25) - 2)), n) == L.OK
+    # the join: one to a row and head (here of no context)
+    a = dict(table=None, num_rows=1 << 24)
+    assert lib.gnnshap_cache_attend_workspace(_cache(), _queries(**a), n) == L.EUNSUPPORTED
+    assert lib.gnnshap_cache_attend(_cache(), _queries(**a), None, None, 0, None) == L.EUNSUPPORTED
+    assert lib.gnnshap_cache_attend_workspace(_cache(), _queries(**dict(a, num_rows=(1 << 24) - 1)), n) == L.OK
