@@ -611,7 +611,7 @@ typedef struct {
   int64_t rows_per_group;        /* divides num_rows; read with shared_table only */
   const uint64_t* masks;         /* [dev] num_rows x mask_words, or NULL (num_players is then 0) */
   int64_t mask_words, num_players, first_player;
-  double scale;                  /* scores are scale q.k; not 0 */
+  double scale;                  /* scores are scale q.k; not 0, and scale log2 e finite in fp32 */
 } gnnshap_queries;
 
 /* Bytes of device workspace for gnnshap_cache_attend (it holds the parts of

@@ -437,6 +437,9 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_attend_join(AttendArgs a)
   if (lane == 0 && a.q.lse) a.q.lse[row * a.q.heads + head] = lse_of<T>(m, l);
 }
 
+// The scale of scores in powers of two.
+float scale2_of(const gnnshap_queries& q) { return static_cast<float>(q.scale * 1.4426950408889634074); }
+
 int check_queries(const gnnshap_cache* c, const gnnshap_queries* q) {
   using gnnshap::fail;
   if (const int st = gnnshap::check_cache(c)) return st;
@@ -444,7 +447,8 @@ int check_queries(const gnnshap_cache* c, const gnnshap_queries* q) {
   if (q->heads < 1 || q->heads % c->kv_heads != 0)
     return fail(GNNSHAP_EINVAL, "%d query heads over %d kv heads", static_cast<int>(q->heads),
                 static_cast<int>(c->kv_heads));
-  if (!(q->scale != 0.0) || !std::isfinite(q->scale)) return fail(GNNSHAP_EINVAL, "scale is 0 or not finite");
+  if (!(q->scale != 0.0) || !std::isfinite(scale2_of(*q)))
+    return fail(GNNSHAP_EINVAL, "scale %g is 0 or not finite in fp32", q->scale);
   if (q->num_rows > INT32_MAX || q->num_rows * q->heads > INT32_MAX)
     return fail(GNNSHAP_EUNSUPPORTED, "%lld rows in one call", static_cast<long long>(q->num_rows));
   const struct {
@@ -491,7 +495,7 @@ int lay_out(AttendArgs& a, const gnnshap_cache* c, const gnnshap_queries* q) {
   a.c = *c;
   a.q = *q;
   a.share = q->heads / c->kv_heads;
-  a.scale2 = static_cast<float>(q->scale * 1.4426950408889634074);
+  a.scale2 = scale2_of(*q);
   a.page_shift = -1;
   for (int i = 0; i < 31; ++i)
     if (c->page_size == 1 << i) a.page_shift = i;

@@ -151,3 +151,25 @@ def test_as_many_rows_as_a_launch_takes(dev):
     for b in (0, 2 ** 27 + 5, rows - 40):
         want = A.token_logprobs(x[b:b + 40], t[b:b + 40].contiguous(), 1)
         assert all(torch.equal(p[b:min(b + 40, rows)], q[:rows - b]) for p, q in zip(r, want))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows", [3, 70])
+def test_a_scale_of_almost_nothing(dev, dtype, rows):
+    """All scores are 0 in fp32, also those scaled down to it: the output is the mean of what a row sees."""
+    print("no scale", dtype, rows, flush=True)
+    gen = torch.Generator(dev).manual_seed(rows)
+    v = torch.randn((4, 16, 1, 64), generator=gen, device=dev).to(dtype)
+    cache = A.PagedCache(torch.randn((4, 16, 1, 64), generator=gen, device=dev).to(dtype), v)
+    q = torch.randn((rows, 2, 64), generator=gen, device=dev).to(dtype)
+    i32 = dict(dtype=torch.int32, device=dev)
+    keep = torch.rand((rows, 50), generator=gen, device=dev) < 0.5
+    keep[:, 0] = True
+    bits = (torch.nn.functional.pad(keep, (0, 14)).long() << torch.arange(64, device=dev)).sum(1, keepdim=True)
+    out, lse = A.attend(cache, q, shared_table=torch.arange(4, **i32)[None], shared_lengths=torch.full((1,), 50, **i32),
+                        masks=bits, num_players=50, scale=1e-50, return_lse=True)
+    n = keep.sum(1, keepdim=True).double()
+    want = (keep.double() @ v.view(64, 64)[:50].double() / n)[:, None]
+    u = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}[dtype]
+    assert float((out.double() - want).abs().max()) <= (u + 82 * 2.0 ** -24) * float(v.abs().max())
+    assert float((lse.double() - torch.log(n)).abs().max()) <= 2.0 ** -20

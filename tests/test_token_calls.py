@@ -180,3 +180,12 @@ def test_more_threads_than_a_launch_takes_are_refused():
     assert lib.gnnshap_cache_attend_workspace(_cache(), _queries(**a), n) == L.EUNSUPPORTED
     assert lib.gnnshap_cache_attend(_cache(), _queries(**a), None, None, 0, None) == L.EUNSUPPORTED
     assert lib.gnnshap_cache_attend_workspace(_cache(), _queries(**dict(a, num_rows=(1 << 24) - 1)), n) == L.OK
+
+
+@pytest.mark.parametrize("scale,status", [(1e39, L.EINVAL), (-1e39, L.EINVAL), (float("inf"), L.EINVAL), (3e38, L.EINVAL),
+                                          (2e38, L.OK), (-0.125, L.OK), (1e-50, L.OK)])
+def test_scales_that_fp32_cannot_hold_are_refused(scale, status):
+    lib, n = L.load(), ctypes.c_size_t()
+    assert lib.gnnshap_cache_attend_workspace(_cache(), _queries(scale=scale), n) == status
+    if status:
+        assert lib.gnnshap_cache_attend(_cache(), _queries(scale=scale), None, None, 0, None) == status
