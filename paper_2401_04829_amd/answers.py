@@ -151,7 +151,7 @@ def attend(cache, q, table=None, lengths=None, max_length=None, shared_table=Non
     pages hold).  masks (int64 [rows, words], the sampler's bits): position
     first_player + j of the context is player j of num_players, seen where bit
     j is set; other positions are always seen.  scale:
-    None for 1 / sqrt(head dim).  Returns out, or (out, lse) with the log of
+    None for 1 / sqrt(head dim).  out must not overlap q.  Returns out, or (out, lse) with the log of
     the sum of exponentials, float32 [rows, heads]; a row that sees nothing
     has out 0 and lse -inf."""
     _no_derivative("attend", q, cache.k, cache.v)

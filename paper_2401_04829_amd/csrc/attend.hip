@@ -650,6 +650,7 @@ extern "C" int gnnshap_cache_attend(const gnnshap_cache* cache, const gnnshap_qu
   const size_t need = carve(a, ws);
   if (need > 0 && (!ws || ws_bytes < need))
     return fail(GNNSHAP_ECAPACITY, "cache_attend workspace needs %zu bytes, has %zu", need, ws ? ws_bytes : 0);
+  if (q->q == q->out) return fail(GNNSHAP_EINVAL, "out is q: a query may be read again after its output is written");
   hipStream_t s = static_cast<hipStream_t>(stream);
   return gnnshap::with_dtype(cache->dtype, [&](auto* p) {
     using T = std::remove_pointer_t<decltype(p)>;

@@ -189,3 +189,9 @@ def test_scales_that_fp32_cannot_hold_are_refused(scale, status):
     assert lib.gnnshap_cache_attend_workspace(_cache(), _queries(scale=scale), n) == status
     if status:
         assert lib.gnnshap_cache_attend(_cache(), _queries(scale=scale), None, None, 0, None) == status
+
+
+def test_queries_as_their_own_output_are_refused():
+    """Where a result is not finite a query is read again after outputs have been written."""
+    assert L.load().gnnshap_cache_attend(_cache(), _queries(q=P, out=P), None, None, 0, None) == L.EINVAL
+    assert b"out is q" in L.load().gnnshap_last_error()
