@@ -25,6 +25,7 @@ _DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
 _raw_stream = torch._C._cuda_getCurrentRawStream   # torch.cuda.current_stream(device).cuda_stream without its object
+_grad_enabled, _any_requires_grad = torch.is_grad_enabled, torch._C._any_requires_grad
 
 
 def _need(ok, what):
@@ -38,11 +39,9 @@ def _ptr(t):
 
 def _no_derivative(call, *tensors):
     """Refuses tensors through which autograd would miss `call`'s derivative."""
-    if torch.is_grad_enabled():
-        for t in tensors:
-            if t is not None and t.requires_grad:
-                raise ValueError(f"{call} has no derivative, and a tensor that it got requires a gradient: call it "
-                                 "under torch.no_grad() or with that tensor detached")
+    if _grad_enabled() and _any_requires_grad(*tensors):
+        raise ValueError(f"{call} has no derivative, and a tensor that it got requires a gradient: call it under "
+                         "torch.no_grad() or with that tensor detached")
     if forward_ad._current_level >= 0:
         for t in tensors:
             if t is not None and forward_ad.unpack_dual(t).tangent is not None:
@@ -210,6 +209,14 @@ def _check_logits(x):
     return _DTYPES[x.dtype]
 
 
+def _give_parts(a, maximum, log_sum, size, device):
+    """Sets the two parts of lse, where they are given."""
+    if maximum is not None:
+        a.maximum = _vector(maximum, "maximum", torch.float32, size, device)
+    if log_sum is not None:
+        a.log_sum = _vector(log_sum, "log_sum", torch.float32, size, device)
+
+
 def token_logprobs(logits, targets=None, top=0, info=None, maximum=None, log_sum=None):
     """gnnshap_token_logprobs of logits [rows, vocabulary]: log probability and
     rank of the tokens `targets` (int64 [rows]; negative or None: no token, 0
@@ -227,8 +234,8 @@ def token_logprobs(logits, targets=None, top=0, info=None, maximum=None, log_sum
     a = L.gnnshap_logits(dtype, top, rows, vocab, logits.data_ptr(), logits.stride(0),
                          _vector(targets, "targets", torch.int64, (rows,), dev), logprob.data_ptr(),
                          entropy.data_ptr(), lse.data_ptr(), rank.data_ptr(), r.top_logprob.data_ptr(),
-                         top_id.data_ptr(), _vector(maximum, "maximum", torch.float32, (rows,), dev),
-                         _vector(log_sum, "log_sum", torch.float32, (rows,), dev))
+                         top_id.data_ptr())
+    _give_parts(a, maximum, log_sum, (rows,), dev)
     nbytes = L.gnnshap_token_logprobs_workspace(a)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
     _on(dev, L.gnnshap_token_logprobs, a, _vector(info, "info", torch.int32, (1,), dev), _ptr(ws), nbytes)
@@ -252,9 +259,8 @@ def token_logprobs_backward(logits, targets, lse, entropy=None, grad_logprob=Non
     a = L.gnnshap_logits(dtype, 0, rows, vocab, logits.data_ptr(), logits.stride(0),
                          _vector(targets, "targets", torch.int64, (rows,), dev), None,
                          _vector(entropy, "entropy", torch.float32, (rows,), dev),
-                         _vector(lse, "lse", torch.float32, (rows,), dev), None, None, None,
-                         _vector(maximum, "maximum", torch.float32, (rows,), dev),
-                         _vector(log_sum, "log_sum", torch.float32, (rows,), dev))
+                         _vector(lse, "lse", torch.float32, (rows,), dev))
+    _give_parts(a, maximum, log_sum, (rows,), dev)
     _on(dev, L.gnnshap_token_logprobs_backward, a,
         _vector(grad_logprob, "grad_logprob", torch.float32, (rows,), dev),
         _vector(grad_entropy, "grad_entropy", torch.float32, (rows,), dev), out.data_ptr(), out.stride(0),
