@@ -7,7 +7,7 @@
 // lose nothing to fp32 arguments), in fp32, rounded once to the element type.
 // Every element is read once and written once: the call is bound by the
 // copy, or by the launch when there are few tokens.  20,000 bf16 tokens of
-// 32 query and 2 x 8 key and value heads of 128: 88 us in the kernel, 5.6 TB/s
+// 32 query and 2 x 8 key and value heads of 128: 89 us in the kernel, 5.6 TB/s
 // (a large copy reaches 4.7); one token: 3 us.
 #include "tokens.h"
 

@@ -186,9 +186,12 @@ struct State {
 // wavefronts that do not wait for each other keep more loads in flight.  Bound
 // by memory where the keys are many: 64 rows of 2,000 tokens, 32 fp16 heads
 // over 8 of 128: 112 us, 4.7 TB/s, of 8,000 431 us, 4.9 TB/s (a large copy: 4.7);
-// 64 rows of 1 to 20,000 tokens (530 MB): 139 us, 3.8 TB/s.  One row of 4,000
-// waits for dependent loads (length, page, key): 9.5 us for 16 MB.  In fp32,
-// 2,000 rows x 8 heads of 64 over 59 shared keys and up to 3 own: 22 us.
+// 64 rows of 1 to 20,000 tokens (530 MB): 139 us, 3.8 TB/s; in fp32 318 us, 3.3
+// TB/s (heads of 128 leave registers for one wavefront per SIMD there).  One row
+// of 4,000 waits for dependent loads (length, page, key): 9.6 us for 16 MB.  In
+// fp32, 2,000 rows x 8 heads of 64 over 59 shared keys and up to 3 own: 21 us.
+// (Calls in a row; with other work between, which takes the caches, 158 us for
+// the unlike rows and 31 us for the last.)
 template <class T, int DP, int RT, bool IS_OWN>
 __global__ __launch_bounds__(64 * kWaves, DP * sizeof(T) <= 256 && RT == 1 ? 2 : 1) void k_cache_attend(AttendArgs a,
                                                                                                      Part part,
@@ -348,8 +351,8 @@ __global__ __launch_bounds__(64 * kWaves, DP * sizeof(T) <= 256 && RT == 1 ? 2 :
 // Joins the parts of each query, a wavefront per row and head, or the four of a
 // workgroup where there may be many parts: the lanes weigh 64 parts at a time,
 // then add up the parts' elements, eight loads in flight.  Four wavefronts
-// from 9 parts on: one row of 4,000 tokens in 63 parts 5 us (both kernels 13.7
-// us; 17.8 with one wavefront each).
+// from 9 parts on: one row of 4,000 tokens in 63 parts 6 us (4 us less than with
+// one wavefront each).
 template <class T, int PER_QUERY>
 __global__ __launch_bounds__(64 * kWaves) void k_cache_attend_join(AttendArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = a.c.head_dim;
@@ -523,8 +526,9 @@ int lay_out(AttendArgs& a, const gnnshap_cache* c, const gnnshap_queries* q) {
     // Tiles of 16 queries that a wavefront takes: two for heads of 65 to 128
     // elements where there are wavefronts enough (64 heads over one, bf16: 512
     // rows of 1,000 keys 146 us with two against 157 with one, one row of 4,000
-    // 16.8 against 14.2; 10,000 rows x 4 heads on 1,000 shared keys in fp32 752
-    // against 937, but with heads of 64 elements 226 against 166 at 2,000 rows).
+    // 16.8 against 14.2; 10,000 rows x 8 heads over 4 on 1,000 shared keys in
+    // fp32 736 against 925, x 4 heads over 4 380 against 467, but with heads of 64
+    // elements 226 against 166 at 2,000 rows).
     const bool two = padded_dim(c->head_dim) == 128 && queries > 16 &&
                      q->num_rows / p.r * c->kv_heads * ceil_div(queries, 32) *
                              ceil_div(std::max(p.max_len, 1), 256) >= 2048;

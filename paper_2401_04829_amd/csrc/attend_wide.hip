@@ -12,9 +12,11 @@
 // to registers and from there to LDS in tiles of 64 (32 where a head is wider
 // than 128), one barrier per tile; keys are half a tile (a tile) further than
 // values.  32 bf16 heads over 8 of 128: 10,000 rows on 417 shared and up to 4 own
-// tokens 163 us, 2,002 rows on 3,851 shared ones 170 us (126 GFLOP with the
-// hidden pairs, 740 TFLOP/s; 950 per further key); by the kernel of 16 queries
-// to a wavefront 1,000 rows on 512 take 112 us, here 60.
+// tokens 167 us, 2,002 rows on 3,851 shared ones 172 us (126 GFLOP with the
+// hidden pairs, 730 TFLOP/s; 900 per further key); by the kernel of 16 queries
+// to a wavefront 1,000 rows on 512 take 112 us, here 58.  In the longer of the two
+// the matrix units are busy in 34 % of the SIMDs' cycles and the vector units in
+// 53 %.  At two wavefronts per SIMD heads of 128 spill 12 of 256 registers.
 //
 // The layout is the transposed one of the other kernels on 32 x 32 x 16
 // instructions: S^T = K Q^T leaves query = lane % 32 and keys in registers,

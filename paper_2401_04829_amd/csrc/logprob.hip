@@ -21,8 +21,9 @@
 // wavefront's, or one workgroup's, or (few rows) several workgroups', whose
 // parts a second launch joins.  Bound by memory, and beside it by the vector
 // instructions of the alternatives: 10,000 x 32,768 bf16 (656 MB) without them
-// 125 us, 5.2 TB/s, with the top 5 152 us, 4.3 TB/s.  One row of 131,072 with the
-// top 20: 9 us, and 7 us to join its 16 parts.
+// 137 us, 4.8 TB/s (from 127 to 160, by the clocks), with the top 5 152 us, 4.3
+// TB/s.  One row of 131,072 with the top 20: 8.5 us, and 7.2 us to join its 16
+// parts.
 #include "tokens.h"
 
 namespace {
@@ -427,7 +428,8 @@ __global__ __launch_bounds__(64 * kWaves) void k_token_logprobs_join(LogprobArgs
 // Rows of up to LANES x N logits, LANES lanes per row: a row is in registers,
 // so its maximum comes first and the alternatives are taken off one by one.
 // Lanes of 16 are put together by moves within the vector unit: 100,000 x 41
-// fp32 with the top 3 16.2 us, 17.1 by way of LDS.
+// fp32 with the top 3 14.5 us, 0.9 less than by way of LDS; bf16 without
+// alternatives 8.4.
 template <class T, int LANES, int N>
 __global__ __launch_bounds__(256) void k_token_logprobs_short(LogprobArgs a) {
   const int lane = threadIdx.x % LANES, V = static_cast<int>(a.l.vocab);
@@ -491,8 +493,9 @@ constexpr int kGradPacks = 4;
 
 // blockDim.x threads take a row's elements in packs of 16 bytes, four in
 // flight, blockDim.y rows per workgroup; every element is read once and
-// written once.  2,000 x 50,021 bf16 (400 MB, rows at odd addresses): 90 us,
-// 4.4 TB/s; 115 us with one pack in flight.
+// written once.  2,000 x 50,021 bf16 (400 MB, rows at odd addresses): 88 us,
+// 4.5 TB/s (74 where other work runs between the calls); 115 us with one pack in
+// flight.
 template <class T>
 __global__ __launch_bounds__(256) void k_token_logprobs_grad(GradArgs a) {
   constexpr int kVec = 16 / sizeof(T);
