@@ -575,16 +575,68 @@ typedef struct {
   int64_t q_token_stride, q_head_stride;
   void* q_out;               /* [dev] may be q itself, with the same strides */
   int64_t q_out_token_stride, q_out_head_stride;
+  const void* q_norm;        /* [dev] head_dim weights of the queries' norm, in the cache's type; NULL: no norm */
+  const void* k_norm;        /* [dev] likewise of the keys */
+  double norm_eps;           /* added to the mean square; read with q_norm or k_norm, finite and >= 0 then */
 } gnnshap_new_tokens;
 
 /* Appends keys and values of new tokens to the cache, rotating the keys (and
  * the tokens' queries, if given) by their positions on the way: the pair
- * (x, y) becomes (x cos - y sin, y cos + x sin), in fp32, rounded once.
+ * (x, y) becomes (x cos - y sin, y cos + x sin), in fp32, rounded once.  With
+ * q_norm or k_norm each head of the queries (keys) is normed before: x_i becomes
+ * x_i w_i / sqrt(mean x^2 + norm_eps), in fp32 too and not rounded in between.
  * Tokens may be of any sequences in any order (a prompt's, one of every
  * row's); two tokens of one slot leave either one's vectors there.  The
  * cache must not overlap the inputs.  EINVAL: sizes, NULL arrays;
  * EUNSUPPORTED: head_dim, dtype. */
 int gnnshap_cache_append(const gnnshap_cache* cache, const gnnshap_new_tokens* tokens, int32_t* info, void* stream);
+
+/* Heads of one kind, queries or keys: element d of head h of token t is
+ * x[t token_stride + h head_stride + d]. */
+typedef struct {
+  int32_t heads;
+  int32_t reserved;
+  const void* x;             /* [dev] */
+  int64_t token_stride, head_stride;
+  void* out;                 /* [dev] what becomes of x; may be x itself, with the same strides */
+  int64_t out_token_stride, out_head_stride;
+} gnnshap_heads;
+
+/* Queries and keys whose heads are normed and rotated, for training. */
+typedef struct {
+  int32_t dtype;             /* gnnshap_dtype of all heads and weights */
+  int32_t head_dim;          /* a multiple of 8 up to GNNSHAP_MAX_HEAD_DIM */
+  int64_t num_tokens;
+  gnnshap_heads q, k;        /* either may have no heads */
+  const void* q_norm;        /* [dev] head_dim weights; NULL: all 1 */
+  const void* k_norm;
+  const int32_t* positions;  /* [dev] of each token; NULL: token t is at t.  Negative: not rotated */
+  const float* cos;          /* as in gnnshap_new_tokens */
+  const float* sin;
+  int64_t num_positions;
+  int32_t rot_dim, interleaved;
+  double eps;                /* finite, >= 0 */
+} gnnshap_normed;
+
+/* y = R(position) (x_i w_i r), r = 1 / sqrt(mean x^2 + eps), per head: the norm
+ * and the rotation of gnnshap_cache_append, in fp32 and rounded once, from x to
+ * out.  The mean square has to be finite in fp32.  EINVAL: sizes, NULL arrays;
+ * EUNSUPPORTED: head_dim, dtype. */
+int gnnshap_norm_rotate(const gnnshap_normed* n, int32_t* info, void* stream);
+
+/* Bytes of device workspace for gnnshap_norm_rotate_backward (parts of the
+ * weights' gradients). */
+int gnnshap_norm_rotate_backward_workspace(const gnnshap_normed* n, size_t* bytes);
+
+/* The gradients of gnnshap_norm_rotate.  grad_q and grad_k hold, as x, the
+ * gradient by the outputs and, as out, where that by n->q.x and n->k.x goes
+ * (which may be the same, with the same strides; n's own out is not read).  With
+ * z = R(-position) grad, per head
+ *     dx = r (z w - x r mean(z w x r)),  dw = sum over tokens and heads of z x r,
+ * in fp32, rounded once.  dq_norm and dk_norm [dev, head_dim each, in the
+ * heads' type] may be NULL.  The sums are taken in a fixed order. */
+int gnnshap_norm_rotate_backward(const gnnshap_normed* n, const gnnshap_heads* grad_q, const gnnshap_heads* grad_k,
+                                 void* dq_norm, void* dk_norm, int32_t* info, void* ws, size_t ws_bytes, void* stream);
 
 /* One new token's queries per row, and what each row sees.  The context of
  * row b is the shared part of its group, the max_shared or fewer tokens of

@@ -62,7 +62,19 @@ class gnnshap_new_tokens(ctypes.Structure):
                 ("positions", c_vp), ("table", c_vp), ("num_rows", c_i64), ("table_width", c_i64), ("cos", c_vp),
                 ("sin", c_vp), ("num_positions", c_i64), ("rot_dim", c_i32), ("interleaved", c_i32), ("heads", c_i32),
                 ("reserved", c_i32), ("q", c_vp), ("q_token_stride", c_i64), ("q_head_stride", c_i64),
-                ("q_out", c_vp), ("q_out_token_stride", c_i64), ("q_out_head_stride", c_i64)]
+                ("q_out", c_vp), ("q_out_token_stride", c_i64), ("q_out_head_stride", c_i64), ("q_norm", c_vp),
+                ("k_norm", c_vp), ("norm_eps", c_dbl)]
+
+
+class gnnshap_heads(ctypes.Structure):
+    _fields_ = [("heads", c_i32), ("reserved", c_i32), ("x", c_vp), ("token_stride", c_i64), ("head_stride", c_i64),
+                ("out", c_vp), ("out_token_stride", c_i64), ("out_head_stride", c_i64)]
+
+
+class gnnshap_normed(ctypes.Structure):
+    _fields_ = [("dtype", c_i32), ("head_dim", c_i32), ("num_tokens", c_i64), ("q", gnnshap_heads),
+                ("k", gnnshap_heads), ("q_norm", c_vp), ("k_norm", c_vp), ("positions", c_vp), ("cos", c_vp),
+                ("sin", c_vp), ("num_positions", c_i64), ("rot_dim", c_i32), ("interleaved", c_i32), ("eps", c_dbl)]
 
 
 class gnnshap_queries(ctypes.Structure):
@@ -141,6 +153,10 @@ _SIGNATURES = {
     "gnnshap_gat_eval_coalitions": (ctypes.c_int, [_P(gnnshap_subgraph), _P(gnnshap_gat), c_i32, c_vp, c_i64, c_i64,
                                                    c_vp, c_vp, c_vp, c_vp, ctypes.c_size_t, c_vp]),
     "gnnshap_cache_append": (ctypes.c_int, [_P(gnnshap_cache), _P(gnnshap_new_tokens), c_vp, c_vp]),
+    "gnnshap_norm_rotate": (ctypes.c_int, [_P(gnnshap_normed), c_vp, c_vp]),
+    "gnnshap_norm_rotate_backward_workspace": (ctypes.c_int, [_P(gnnshap_normed), _P(ctypes.c_size_t)]),
+    "gnnshap_norm_rotate_backward": (ctypes.c_int, [_P(gnnshap_normed), _P(gnnshap_heads), _P(gnnshap_heads), c_vp,
+                                                    c_vp, c_vp, c_vp, ctypes.c_size_t, c_vp]),
     "gnnshap_cache_attend_workspace": (ctypes.c_int, [_P(gnnshap_cache), _P(gnnshap_queries), _P(ctypes.c_size_t)]),
     "gnnshap_cache_attend": (ctypes.c_int, [_P(gnnshap_cache), _P(gnnshap_queries), c_vp, c_vp, ctypes.c_size_t,
                                             c_vp]),
@@ -437,6 +453,21 @@ def gnnshap_fidelity_average(terms_ptr, n, stride, avg_ptr, stream):
 
 def gnnshap_cache_append(cache, tokens, info_ptr, stream):
     check(load().gnnshap_cache_append(cache, tokens, info_ptr, stream), "cache_append")
+
+
+def gnnshap_norm_rotate(normed, info_ptr, stream):
+    check(load().gnnshap_norm_rotate(normed, info_ptr, stream), "norm_rotate")
+
+
+def gnnshap_norm_rotate_backward_workspace(normed):
+    n = ctypes.c_size_t()
+    check(load().gnnshap_norm_rotate_backward_workspace(normed, n), "norm_rotate_backward_workspace")
+    return n.value
+
+
+def gnnshap_norm_rotate_backward(normed, grad_q, grad_k, dq_norm_ptr, dk_norm_ptr, info_ptr, ws_ptr, ws_bytes, stream):
+    check(load().gnnshap_norm_rotate_backward(normed, grad_q, grad_k, dq_norm_ptr, dk_norm_ptr, info_ptr, ws_ptr,
+                                              ws_bytes, stream), "norm_rotate_backward")
 
 
 def gnnshap_cache_attend_workspace(cache, queries):

@@ -103,16 +103,18 @@ class PagedCache:
 
 
 def append_tokens(cache, k, v, table, index, rows=None, positions=None, q=None, cos=None, sin=None, interleaved=False,
-                  q_out=None, info=None):
+                  q_out=None, info=None, q_norm=None, k_norm=None, eps=1e-6):
     """gnnshap_cache_append: writes keys and values [tokens, kv heads, head
     dim] of new tokens into the cache, token t at place index[t] (int32;
     negative: not stored) of the sequence in row rows[t] (int32; None: t) of
     `table`.  With cos and sin (float32 [positions, rot dim / 2]) keys are
     rotated by positions[t] (int32; None: index), and so are the queries q
     [tokens, heads, head dim] of the same tokens, which are returned (in
-    q_out, which may be q).  info: int32 [1], set to 1 on an index out of
-    range."""
-    _no_derivative("append_tokens", k, v, q, cache.k, cache.v)
+    q_out, which may be q).  With q_norm or k_norm ([head dim] weights in the
+    cache's type) each head of the queries (the keys) is normed before it is
+    rotated: x w / sqrt(mean x^2 + eps).  info: int32 [1], set to 1 on an index
+    out of range."""
+    _no_derivative("append_tokens", k, v, q, cache.k, cache.v, q_norm, k_norm)
     dtype, dev, dim = cache.dtype, cache.device, cache.head_dim
     n = k.shape[0]
     kp = _heads(k, "k", cache.kv_heads, dim, dtype, dev)
@@ -134,9 +136,114 @@ def append_tokens(cache, k, v, table, index, rows=None, positions=None, q=None, 
         n, *kp, *vp, _vector(rows, "rows", torch.int32, (n,), dev), _vector(index, "index", torch.int32, (n,), dev),
         _vector(positions, "positions", torch.int32, (n,), dev), _vector(table, "table", torch.int32, None, dev),
         table.shape[0], table.shape[1], _vector(cos, "cos", torch.float32, angles, dev),
-        _vector(sin, "sin", torch.float32, angles, dev), angles[0], 2 * angles[1], int(interleaved), heads, 0, *qp, *op)
+        _vector(sin, "sin", torch.float32, angles, dev), angles[0], 2 * angles[1], int(interleaved), heads, 0, *qp, *op,
+        _vector(q_norm, "q_norm", dtype, (dim,), dev), _vector(k_norm, "k_norm", dtype, (dim,), dev), eps)
     _on(dev, L.gnnshap_cache_append, cache._c, t, _vector(info, "info", torch.int32, (1,), dev))
     return q_out
+
+
+def _normed(q, k, q_norm, k_norm, cos, sin, positions, interleaved, eps):
+    """The library's description of heads to norm and rotate, without outputs."""
+    if q.dim() != 3 or not q.is_cuda or q.dtype not in _DTYPES:
+        raise ValueError(f"q: a [tokens, heads, head dim] float32, float16 or bfloat16 tensor on a GPU is needed, got "
+                         f"{q.dtype} {tuple(q.shape)} on {q.device}")
+    n, heads, dim = q.shape
+    dtype, dev = q.dtype, q.device
+    kinds = [L.gnnshap_heads(heads, 0, *_heads(q, "q", heads, dim, dtype, dev)), L.gnnshap_heads()]
+    if k is not None:
+        kp = _heads(k, "k", None, dim, dtype, dev)
+        _need(k.shape[0] == n, "as many keys as queries are needed")
+        kinds[1] = L.gnnshap_heads(k.shape[1], 0, *kp)
+    else:
+        _need(k_norm is None, "k_norm without keys")
+    angles = (0, 0)
+    if cos is not None:
+        _need(sin is not None and cos.dim() == 2, "cos and sin: two [positions, rot dim / 2] tensors")
+        angles = tuple(cos.shape)
+    return L.gnnshap_normed(
+        _DTYPES[dtype], dim, n, *kinds, _vector(q_norm, "q_norm", dtype, (dim,), dev),
+        _vector(k_norm, "k_norm", dtype, (dim,), dev), _vector(positions, "positions", torch.int32, (n,), dev),
+        _vector(cos, "cos", torch.float32, angles, dev), _vector(sin, "sin", torch.float32, angles, dev), angles[0],
+        2 * angles[1], int(interleaved), eps)
+
+
+def norm_rotate(q, k=None, q_norm=None, k_norm=None, cos=None, sin=None, positions=None, interleaved=False, eps=1e-6,
+                info=None):
+    """gnnshap_norm_rotate: each head of the queries q [tokens, heads, head dim]
+    and of the keys k (other heads, or None) normed and, with cos and sin
+    (float32 [positions, rot dim / 2]), rotated by positions[t] (int32; None: t;
+    negative: not rotated), as append_tokens does on the way into a cache.
+    q_norm and k_norm: [head dim] weights in the heads' type; None: all 1.
+    Returns both, new and contiguous (None for no keys).  info: int32 [1], set
+    to 1 on a position out of range."""
+    _no_derivative("norm_rotate (but for differentiable_norm_rotate)", q, k, q_norm, k_norm, cos, sin)
+    a = _normed(q, k, q_norm, k_norm, cos, sin, positions, interleaved, eps)
+    out = [None if x is None else torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (q, k)]
+    for kind, x in zip((a.q, a.k), out):
+        if x is not None:
+            kind.out, kind.out_token_stride, kind.out_head_stride = x.data_ptr(), x.stride(0), x.stride(1)
+    _on(q.device, L.gnnshap_norm_rotate, a, _vector(info, "info", torch.int32, (1,), q.device))
+    return tuple(out)
+
+
+def norm_rotate_backward(grad_q, grad_k, q, k=None, q_norm=None, k_norm=None, cos=None, sin=None, positions=None,
+                         interleaved=False, eps=1e-6, weights=True, info=None):
+    """gnnshap_norm_rotate_backward: the gradients by q, k, q_norm and k_norm of
+    norm_rotate's outputs, whose gradients are grad_q and grad_k.  Returns the
+    four, None where the input is None (with weights=False for both weights)."""
+    _no_derivative("norm_rotate_backward", grad_q, grad_k, q, k, q_norm, k_norm, cos, sin)
+    a = _normed(q, k, q_norm, k_norm, cos, sin, positions, interleaved, eps)
+    dev, dtype, dim = q.device, q.dtype, q.shape[2]
+    out, kinds = [], []
+    for x, g, name in ((q, grad_q, "grad_q"), (k, grad_k, "grad_k")):
+        if x is None:
+            out.append(None)
+            kinds.append(L.gnnshap_heads())
+            continue
+        gp = _heads(g, name, x.shape[1], dim, dtype, dev)
+        _need(g.shape[0] == x.shape[0], f"{name} of as many tokens is needed")
+        out.append(torch.empty(x.shape, dtype=dtype, device=dev))
+        kinds.append(L.gnnshap_heads(x.shape[1], 0, *gp, out[-1].data_ptr(), out[-1].stride(0), out[-1].stride(1)))
+    out += [torch.empty(dim, dtype=dtype, device=dev) if weights and w is not None else None for w in (q_norm, k_norm)]
+    nbytes = L.gnnshap_norm_rotate_backward_workspace(a) if out[2] is not None or out[3] is not None else 0
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+    _on(dev, L.gnnshap_norm_rotate_backward, a, *kinds, _ptr(out[2]), _ptr(out[3]),
+        _vector(info, "info", torch.int32, (1,), dev), _ptr(ws), nbytes)
+    return tuple(out)
+
+
+class _NormRotate(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, q_norm, k_norm, cos, sin, positions, interleaved, eps):
+        ctx.save_for_backward(q, k, q_norm, k_norm, cos, sin, positions)
+        ctx.rest = interleaved, eps
+        return norm_rotate(q, k, q_norm, k_norm, cos, sin, positions, interleaved, eps)
+
+    @staticmethod
+    def backward(ctx, grad_q, grad_k):
+        return (*_NormRotateGradient.apply(grad_q, grad_k, *ctx.saved_tensors, *ctx.rest,
+                                           any(ctx.needs_input_grad[2:4])), None, None, None, None, None)
+
+
+class _NormRotateGradient(torch.autograd.Function):
+    """The gradient as a node of its own, so that differentiating it again raises."""
+    @staticmethod
+    def forward(ctx, grad_q, grad_k, *rest):
+        grads = (g if g is None or g.stride(2) == 1 else g.contiguous() for g in (grad_q, grad_k))
+        return norm_rotate_backward(*grads, *rest)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("differentiable_norm_rotate has a first derivative only")
+
+
+def differentiable_norm_rotate(q, k=None, q_norm=None, k_norm=None, cos=None, sin=None, positions=None,
+                               interleaved=False, eps=1e-6):
+    """norm_rotate with its gradient by q, k, q_norm and k_norm (autograd), for
+    training.  The gradient is of first order, and the angles have none: cos and
+    sin that require a gradient are refused."""
+    _no_derivative("differentiable_norm_rotate by cos and sin", cos, sin)
+    return _NormRotate.apply(q, k, q_norm, k_norm, cos, sin, positions, interleaved, eps)
 
 
 def attend(cache, q, table=None, lengths=None, max_length=None, shared_table=None, shared_lengths=None,

@@ -6,10 +6,11 @@
 // with the angle's cosine and sine read from tables (so that long positions
 // lose nothing to fp32 arguments), in fp32, rounded once to the element type.
 // Every element is read once and written once: the call is bound by the
-// copy, or by the launch when there are few tokens.  20,000 bf16 tokens of
+// copy, or by the launch when there are few tokens.  The norm of a head's
+// elements is a sum over the lanes that hold them (heads.h).  20,000 bf16 tokens of
 // 32 query and 2 x 8 key and value heads of 128: 89 us in the kernel, 5.6 TB/s
 // (a large copy reaches 4.7); one token: 3 us.
-#include "tokens.h"
+#include "heads.h"
 
 namespace {
 
@@ -31,7 +32,7 @@ struct AppendArgs {
 // other where the pairs are N apart or more, each in itself where they are
 // interleaved, and else are copied.  So the two halves of a pair meet in one
 // thread's registers, and a head's threads read and write on end.
-template <class T, int N>
+template <class T, int N, bool NORM>
 __global__ __launch_bounds__(256) void k_cache_append(AppendArgs a) {
   const int64_t t = blockIdx.x;
   const int head = blockIdx.y * blockDim.y + threadIdx.y;
@@ -81,6 +82,15 @@ __global__ __launch_bounds__(256) void k_cache_append(AppendArgs a) {
   const float* cs = turn ? a.t.cos + pos * half : nullptr;
   const float* sn = turn ? a.t.sin + pos * half : nullptr;
 
+  const void* const weight = is_v ? nullptr : is_q ? a.t.q_norm : a.t.k_norm;
+  if (NORM && weight) {
+    gnnshap::HeadUnits<T, N> x(D, rot, a.t.interleaved);
+    x.load(src);
+    x.norm(static_cast<const T*>(weight), static_cast<float>(a.t.norm_eps));
+    if (turn) x.turn(cs, sn, rot, a.t.interleaved, 1.f);
+    x.store(dst);
+    return;
+  }
   for (int u = threadIdx.x; u < D / (2 * N); u += blockDim.x) {
     if (turn && !a.t.interleaved && u < half / N) {
       const int i = u * N;
@@ -117,14 +127,16 @@ __global__ __launch_bounds__(256) void k_cache_append(AppendArgs a) {
 template <class T, int N>
 int launch(const AppendArgs& a, hipStream_t s) {
   const int units = a.c.head_dim / (2 * N);
-  int x = 1;
-  while (x < units && x < 64) x *= 2;
+  const int x = gnnshap::head_lanes(units);
   if (const int st = gnnshap::check_launch(a.t.num_tokens, x)) return st;
   const int heads = a.q_heads + 2 * a.c.kv_heads, y = std::min(256 / x, heads);
   dim3 grid(static_cast<unsigned>(a.t.num_tokens), static_cast<unsigned>(gnnshap::ceil_div(heads, y)));
   {
     GS_TIMED("k_cache_append", s);
-    k_cache_append<T, N><<<grid, dim3(x, y), 0, s>>>(a);
+    if (a.t.q_norm || a.t.k_norm)
+      k_cache_append<T, N, true><<<grid, dim3(x, y), 0, s>>>(a);
+    else
+      k_cache_append<T, N, false><<<grid, dim3(x, y), 0, s>>>(a);
   }
   GS_LAUNCHED();
   return GNNSHAP_OK;
@@ -147,6 +159,8 @@ extern "C" int gnnshap_cache_append(const gnnshap_cache* cache, const gnnshap_ne
       return fail(GNNSHAP_EINVAL, "rot_dim %d of head_dim %d", static_cast<int>(t->rot_dim),
                   static_cast<int>(cache->head_dim));
   }
+  if ((t->q_norm || t->k_norm) && !(t->norm_eps >= 0.0 && std::isfinite(static_cast<float>(t->norm_eps))))
+    return fail(GNNSHAP_EINVAL, "norm_eps %g is negative or not finite in fp32", t->norm_eps);
   if (t->q && (!t->q_out || t->heads < 1)) return fail(GNNSHAP_EINVAL, "queries without heads or q_out");
   if (t->num_rows < 1 || t->table_width < 1) return fail(GNNSHAP_EINVAL, "page table without rows or pages");
   if (t->num_tokens == 0) return GNNSHAP_OK;
@@ -163,12 +177,7 @@ extern "C" int gnnshap_cache_append(const gnnshap_cache* cache, const gnnshap_ne
   // 16-byte packs where the rotated half is whole packs, else the widest that fit
   return gnnshap::with_dtype(cache->dtype, [&](auto* p) {
     using T = std::remove_pointer_t<decltype(p)>;
-    constexpr int kWide = 16 / sizeof(T);
-    const auto fits = [&](int n) { return cache->head_dim % (2 * n) == 0 && (rot / 2) % n == 0; };
-    if (fits(kWide)) return launch<T, kWide>(a, s);
-    if (fits(4)) return launch<T, 4>(a, s);
-    if (fits(2)) return launch<T, 2>(a, s);
-    return launch<T, 1>(a, s);
+    return gnnshap::with_pack<T>(cache->head_dim, rot, [&](auto n) { return launch<T, decltype(n)::value>(a, s); });
   });
   GS_TRY_END
 }

@@ -1,0 +1,259 @@
+"""Norm and rotation of heads, into the cache and for training, against plain
+implementations in float64.
+
+Tolerances, with u the element type's half unit (2^-24, 2^-11, 2^-8; fp16 also
+2^-25 absolute, below its normal numbers) and D the head dim.  A mean square is
+off by D + 2 roundings relative at most, one over its root by half of that and
+three more, a normed element by three more: k = (D + 16) 2^-24 relative covers
+each with room, and a turned one is a sum of two.  A gradient's mean has D + 8
+roundings of its terms' absolute sum.
+"""
+import math
+
+import pytest
+import torch
+
+from paper_2401_04829_amd import answers as A
+from tests.gpu_util import require_gpu
+
+pytestmark = pytest.mark.gpu
+
+HALF = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+EPS = 1e-5
+
+
+@pytest.fixture(scope="module")
+def dev():
+    return require_gpu()
+
+
+def _gen(dev, seed):
+    return torch.Generator(device=dev).manual_seed(seed)
+
+
+def _angles(dev, positions, rot):
+    angle = torch.arange(positions, device=dev, dtype=torch.float64)[:, None] * 100.0 ** (
+        -torch.arange(0, rot, 2, device=dev, dtype=torch.float64) / max(rot, 1))
+    return angle.cos().float().contiguous(), angle.sin().float().contiguous()
+
+
+def _turn(x, cos, sin, positions, interleaved, absolute=False):
+    """Heads [n, h, D] in float64 turned by their positions; those of a negative one are not."""
+    if cos is None or cos.shape[1] == 0:
+        return x
+    rot = 2 * cos.shape[1]
+    there = (positions >= 0)[:, None, None]
+    c, s = (y.double()[positions.clamp(min=0).long()][:, None] for y in (cos, sin))
+    a, b = (x[..., 0:rot:2], x[..., 1:rot:2]) if interleaved else (x[..., :rot // 2], x[..., rot // 2:rot])
+    p, q = (a * c.abs() + b * s.abs(), b * c.abs() + a * s.abs()) if absolute else (a * c - b * s, b * c + a * s)
+    y = torch.stack([p, q], -1).flatten(-2) if interleaved else torch.cat([p, q], -1)
+    return torch.where(there, torch.cat([y, x[..., rot:]], -1), x)
+
+
+def _reference(x, w, cos, sin, positions, interleaved):
+    """Result and the sum of its terms' sizes."""
+    x = x.double()
+    unit = x / torch.sqrt(x.square().mean(-1, keepdim=True) + EPS)
+    z = unit if w is None else unit * w.double()
+    return _turn(z, cos, sin, positions, interleaved), _turn(z.abs(), cos, sin, positions, interleaved, True)
+
+
+def _close(got, want, size, dtype, dim, what=""):
+    tol = HALF[dtype] * want.abs() + (dim + 16) * 2.0 ** -24 * size + 2.0 ** -25 * (dtype == torch.float16)
+    d = (got.double() - want).abs()
+    assert bool((d <= tol).all()), (what, float((d / tol).max()))
+
+
+SHAPES = [  # tokens, heads, kv heads, head dim, rotated, interleaved
+    (1, 1, 1, 8, 8, False), (3, 4, 2, 64, 64, False), (37, 32, 8, 128, 128, False), (5, 3, 1, 80, 40, True),
+    (9, 7, 7, 256, 128, False), (2, 5, 2, 200, 22, True), (130, 2, 1, 104, 0, False), (6, 2, 2, 248, 246, False),
+    (17, 40, 1, 128, 64, True),
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,heads,kv,dim,rot,interleaved", SHAPES)
+def test_norm_and_gradient(dev, dtype, n, heads, kv, dim, rot, interleaved):
+    """Heads that are slices of a projection, some of them 0 and some far from
+    1, positions in no order and one that is not rotated."""
+    print("norm", dtype, n, heads, kv, dim, rot, interleaved, flush=True)
+    gen = _gen(dev, n + dim)
+    qkv = torch.randn((n, heads + 2 * kv, dim), generator=gen, device=dev)
+    qkv = (qkv * torch.exp(2 * torch.randn((n, heads + 2 * kv, 1), generator=gen, device=dev))).to(dtype)
+    qkv[0, 0] = 0
+    q, k, _ = qkv.split([heads, kv, kv], 1)
+    wq, wk = ((1 + 0.3 * torch.randn(dim, generator=gen, device=dev)).to(dtype) for _ in range(2))
+    cos, sin = _angles(dev, 50, rot) if rot else (None, None)
+    positions = torch.randint(0, 50, (n,), generator=gen, device=dev, dtype=torch.int32)
+    positions[n // 2] = -1
+    gq, gk = (torch.randn((n, h, dim), generator=gen, device=dev).to(dtype) for h in (heads, kv))
+    leaves = [x.detach().requires_grad_() for x in (q, k, wq, wk)]
+    out = A.differentiable_norm_rotate(*leaves, cos=cos, sin=sin, positions=positions, interleaved=interleaved, eps=EPS)
+    grads = torch.autograd.grad(out, leaves, (gq, gk))
+    again = torch.autograd.grad(A.differentiable_norm_rotate(*leaves, cos, sin, positions, interleaved, EPS), leaves,
+                                (gq, gk))
+    assert all(torch.equal(a, b) for a, b in zip(grads, again))
+    for x, w, g, y, dx, dw in ((q, wq, gq, out[0], grads[0], grads[2]), (k, wk, gk, out[1], grads[1], grads[3])):
+        want, size = _reference(x, w, cos, sin, positions, interleaved)
+        assert y.dtype == dx.dtype == dw.dtype == dtype and y.shape == dx.shape == x.shape
+        _close(y.detach(), want, size, dtype, dim, "y")
+        x64, w64 = (t.detach().double().requires_grad_() for t in (x, w))
+        want_dx, want_dw = torch.autograd.grad(_reference(x64, w64, cos, sin, positions, interleaved)[0], (x64, w64),
+                                               g.double())
+        z = _turn(g.double().abs(), cos, sin, positions, interleaved, True)
+        r = 1 / torch.sqrt(x.double().square().mean(-1, keepdim=True) + EPS)
+        unit, wd = (x.double() * r).abs(), w.double().abs()
+        _close(dx, want_dx, r * (z * wd + 3 * unit * (z * wd * unit).mean(-1, keepdim=True)), dtype, dim, "dx")
+        d, tol = (dw.double() - want_dw).abs(), HALF[dtype] * want_dw.abs() + (
+            n * x.shape[1] + dim + 16) * 2.0 ** -24 * (z * unit).sum((0, 1)) + 2.0 ** -25 * (dtype == torch.float16)
+        assert bool((d <= tol).all()), ("dw", float((d / tol).max()))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,heads,kv,dim,rot,interleaved", SHAPES)
+def test_norm_on_the_way_into_the_cache(dev, dtype, n, heads, kv, dim, rot, interleaved):
+    """As norm_rotate, bit for bit; values and what no token goes to stay as
+    they are; either norm alone, in place.  Queries without a norm beside keys
+    with one: as without both, but for what of a c - b s is fused, at most one
+    rounding of each product and of the sum on either side, 2 x 2 2^-24 (|a c| +
+    |b s|), and one to the type on either side."""
+    print("append", dtype, n, heads, kv, dim, rot, interleaved, flush=True)
+    gen = _gen(dev, n + dim)
+    page = 7
+    qkv = torch.randn((n, heads + 2 * kv, dim), generator=gen, device=dev).to(dtype)
+    q, k, v = qkv.split([heads, kv, kv], 1)
+    wq, wk = ((1 + 0.3 * torch.randn(dim, generator=gen, device=dev)).to(dtype) for _ in range(2))
+    cos, sin = _angles(dev, 200, rot) if rot else (None, None)
+    table = torch.randperm(-(-(n + 3) // page), generator=gen, device=dev).to(torch.int32)[None]
+    index = torch.arange(2, n + 2, device=dev, dtype=torch.int32)
+    rows = torch.zeros_like(index)
+    plain = A.norm_rotate(q, k, wq, wk, cos, sin, index, interleaved, EPS)
+    bare = A.append_tokens(A.PagedCache.empty(table.numel(), page, kv, dim, dtype, dev), k, v, table, index, rows, q=q,
+                           cos=cos, sin=sin, interleaved=interleaved)
+    page_of, slot = table[0][(index // page).long()].long(), (index % page).long()
+    for norms in (dict(q_norm=wq, k_norm=wk), dict(q_norm=wq), dict(k_norm=wk)):
+        cache = A.PagedCache(*torch.full((2, table.numel(), page, kv, dim), 7.0, dtype=dtype, device=dev).unbind(0))
+        mine = q.clone()
+        A.append_tokens(cache, k, v, table, index, rows, q=mine, cos=cos, sin=sin, interleaved=interleaved, q_out=mine,
+                        eps=EPS, **norms)
+        if "q_norm" in norms:
+            assert torch.equal(mine, plain[0])
+        else:
+            size = _turn(q.double().abs(), cos, sin, index, interleaved, True)
+            assert bool(((mine.double() - bare.double()).abs() <= 2 * HALF[dtype] * size * (1 + 2.0 ** -7)
+                         + 2.0 ** -22 * size + 2.0 ** -24 * (dtype == torch.float16)).all())
+        assert torch.equal(cache.v[page_of, slot], v)
+        if "k_norm" in norms:
+            assert torch.equal(cache.k[page_of, slot], plain[1])
+        rest = torch.ones((table.numel(), page), dtype=torch.bool, device=dev)
+        rest[page_of, slot] = False
+        assert bool((cache.k[rest] == 7).all()) and bool((cache.v[rest] == 7).all())
+
+
+def test_gradient_against_differences(dev):
+    """Central differences of the kernel's own results along random directions:
+    off by the outputs' rounding over the step, and by what float64's own
+    differences are off the derivative."""
+    gen = _gen(dev, 3)
+    n, heads, dim, h = 3, 2, 64, 2.0 ** -5
+    x, g, vx = (torch.randn((n, heads, dim), generator=gen, device=dev) for _ in range(3))
+    w, vw = (torch.randn(dim, generator=gen, device=dev) for _ in range(2))
+    cos, sin = _angles(dev, n, dim)
+    at = torch.arange(n, device=dev)
+    dx, _, dw, _ = A.norm_rotate_backward(g, None, x, None, w, None, cos, sin, eps=EPS)
+    for a, b in ((1.0, 0.0), (0.0, 1.0), (1.0, -1.0)):
+        ends = [((x + s * a * vx), (w + s * b * vw)) for s in (h, -h)]
+        slope = [float((A.norm_rotate(p, None, o, None, cos, sin, eps=EPS)[0].double() * g.double()).sum()) for p, o in ends]
+        slope64 = [float((_reference(p, o, cos, sin, at, False)[0] * g.double()).sum()) for p, o in ends]
+        got = a * float((dx.double() * vx.double()).sum()) + b * float((dw.double() * vw.double()).sum())
+        x64, w64 = x.double().requires_grad_(), w.double().requires_grad_()
+        d = torch.autograd.grad((_reference(x64, w64, cos, sin, at, False)[0] * g.double()).sum(), (x64, w64))
+        true = a * float((d[0] * vx).sum()) + b * float((d[1] * vw).sum())
+        size = float((_reference(x, w, cos, sin, at, False)[1] * g.abs()).sum())
+        tol = abs((slope64[0] - slope64[1]) / (2 * h) - true) + (dim + 17) * 2.0 ** -24 * 2 * size / h
+        assert abs(got - (slope[0] - slope[1]) / (2 * h)) <= tol
+
+
+def test_parts_of_the_call(dev):
+    """No keys, no tokens, no weights, unit weights; only weights or only heads want a gradient; outputs that are not used."""
+    gen = _gen(dev, 1)
+    q, k = (torch.randn((5, h, 64), generator=gen, device=dev, dtype=torch.float32) for h in (3, 2))
+    one = torch.ones(64, device=dev)
+    assert A.norm_rotate(q)[1] is None
+    assert torch.equal(A.norm_rotate(q, k)[1], A.norm_rotate(q, k, one, one)[1])
+    assert torch.equal(A.norm_rotate(q, k)[0], A.norm_rotate(q)[0])
+    empty = A.norm_rotate(q[:0], k[:0], one, one)
+    assert empty[0].shape == (0, 3, 64) and empty[1].shape == (0, 2, 64)
+    d = A.norm_rotate_backward(q[:0], k[:0], q[:0], k[:0], one, one)
+    assert d[0].shape == (0, 3, 64) and bool((d[2] == 0).all()) and bool((d[3] == 0).all())
+    w = one.clone().requires_grad_()
+    y, z = A.differentiable_norm_rotate(q, k, w, one)
+    y.sum().backward()
+    both = A.norm_rotate_backward(torch.ones_like(q), torch.zeros_like(k), q, k, one, one)
+    assert torch.equal(w.grad, both[2]) and bool((both[3] == 0).all()) and bool((both[1] == 0).all())
+    x = q.clone().requires_grad_()
+    A.differentiable_norm_rotate(x, None, one)[0].sum().backward()      # an expanded gradient
+    assert torch.equal(x.grad, both[0])
+    lone = torch.randn((1, 1, 64), generator=gen, device=dev, requires_grad=True)
+    A.differentiable_norm_rotate(lone.expand(5, 3, 64), None, one)[0].sum().backward()
+    u = lone.detach().expand(5, 3, 64)
+    want = A.norm_rotate_backward(torch.ones_like(q), None, u, None, one)[0].sum((0, 1))
+    assert torch.allclose(lone.grad[0, 0], want, rtol=0, atol=15 * 2.0 ** -24 * 15 * float(want.abs().max() + 1))
+
+
+def test_a_second_derivative_raises(dev):
+    x = torch.randn((3, 2, 64), device=dev, requires_grad=True)
+    y = A.differentiable_norm_rotate(x)[0]
+    first, = torch.autograd.grad((y * y).sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="first derivative only"):
+        first.sum().backward()
+    cos = torch.ones((3, 32), device=dev, requires_grad=True)
+    with pytest.raises(ValueError, match="has no derivative"):
+        A.differentiable_norm_rotate(x, cos=cos, sin=torch.zeros((3, 32), device=dev))
+
+
+def test_positions_out_of_range_and_not_finite_heads(dev):
+    """A position behind the angles sets info and leaves the other tokens as
+    they are; a NaN or an infinity stays in its own head."""
+    gen = _gen(dev, 2)
+    x = torch.randn((6, 4, 128), generator=gen, device=dev).bfloat16()
+    cos, sin = _angles(dev, 6, 128)
+    want = A.norm_rotate(x, cos=cos, sin=sin)[0]
+    info = torch.zeros(1, dtype=torch.int32, device=dev)
+    at = torch.arange(6, dtype=torch.int32, device=dev)
+    at[3] = 6
+    got = A.norm_rotate(x, cos=cos, sin=sin, positions=at, info=info)[0]
+    keep = torch.arange(6, device=dev) != 3
+    assert int(info) == 1 and torch.equal(got[keep], want[keep])
+    x[1, 2, 5], x[4, 0, 0] = math.nan, math.inf
+    got = A.norm_rotate(x, cos=cos, sin=sin)[0]
+    bad = torch.zeros((6, 4), dtype=torch.bool, device=dev)
+    bad[1, 2] = bad[4, 0] = True
+    assert bool(got[1, 2].isnan().all()) and bool(got[4, 0].isnan().any()) and torch.equal(got[~bad], want[~bad])
+
+
+def test_graph_and_stream(dev):
+    """A captured forward and backward, replayed on new values with eager work
+    between, and calls on another stream than the default."""
+    gen = _gen(dev, 4)
+    q, k, gq, gk = (torch.randn((33, h, 128), generator=gen, device=dev).bfloat16() for h in (8, 2, 8, 2))
+    w = torch.ones(128, device=dev, dtype=torch.bfloat16)
+    cos, sin = _angles(dev, 33, 128)
+
+    def step():
+        return (*A.norm_rotate(q, k, w, w, cos, sin), *A.norm_rotate_backward(gq, gk, q, k, w, w, cos, sin))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = step()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(other, step()))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for seed in range(3):
+        q.copy_(torch.randn(q.shape, generator=_gen(dev, seed), device=dev))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, step()))
