@@ -726,6 +726,55 @@ int gnnshap_token_logprobs(const gnnshap_logits* logits, int32_t* info, void* ws
 int gnnshap_token_logprobs_backward(const gnnshap_logits* logits, const float* g_logprob, const float* g_entropy,
                                     void* grad, int64_t grad_stride, int32_t* info, void* stream);
 
+/* Rows of hidden states, a vocabulary's weights, and what is read off their
+ * products, the logits x = hidden weight^T, of which none is kept.  Outputs may
+ * be NULL, each; they are those of gnnshap_logits. */
+typedef struct {
+  int32_t dtype;            /* gnnshap_dtype of hidden states and weights */
+  int32_t reserved;
+  int64_t num_rows, vocab, width;
+  const void* hidden;       /* [dev] num_rows x width, row b at hidden + b hidden_stride */
+  int64_t hidden_stride;
+  const void* weight;       /* [dev] vocab x width, token j's row at weight + j weight_stride */
+  int64_t weight_stride;
+  const int64_t* targets;   /* [dev] as in gnnshap_logits */
+  float* logprob;           /* [dev] num_rows, as all that follow */
+  float* entropy;
+  float* lse;
+  float* maximum;
+  float* log_sum;
+} gnnshap_linear;
+
+int gnnshap_linear_logprobs_workspace(const gnnshap_linear* linear, size_t* bytes);
+
+/* Log probabilities of given tokens and entropies from hidden states: logits
+ * are sums of products in fp32 (of 16-bit elements exact products) and not
+ * rounded to the elements' type; of each tile of logits the rows' statistics
+ * are kept.  Rows with infinite or NaN logits as in gnnshap_token_logprobs.
+ * EINVAL: sizes, NULL arrays; EUNSUPPORTED: dtype, a vocabulary over 2^30, a
+ * width over 2^24; ECAPACITY: workspace. */
+int gnnshap_linear_logprobs(const gnnshap_linear* linear, int32_t* info, void* ws, size_t ws_bytes, void* stream);
+
+/* Bytes of device workspace for gnnshap_linear_logprobs_backward: the gradient
+ * by the logits of a piece of the vocabulary, and parts of the hidden states'
+ * gradient. */
+int gnnshap_linear_logprobs_backward_workspace(const gnnshap_linear* linear, size_t* bytes);
+
+/* Gradients by hidden states and weights of sum_b g_logprob[b] logprob[b] +
+ * g_entropy[b] entropy[b], in their type: with d as in
+ * gnnshap_token_logprobs_backward, whose logits are computed again piece by
+ * piece of the vocabulary,
+ *     grad_hidden = d weight,  grad_weight = d^T hidden,
+ * summed in fp32 in a fixed order.  d enters these products in the elements'
+ * type; of up to 128 rows in two parts, the second what the first's rounding
+ * left.  Reads maximum, log_sum and entropy (with g_entropy) as
+ * gnnshap_linear_logprobs wrote them.  grad_hidden, grad_weight, g_logprob and
+ * g_entropy may be NULL.  With no rows grad_weight is 0. */
+int gnnshap_linear_logprobs_backward(const gnnshap_linear* linear, const float* g_logprob, const float* g_entropy,
+                                     void* grad_hidden, int64_t grad_hidden_stride, void* grad_weight,
+                                     int64_t grad_weight_stride, int32_t* info, void* ws, size_t ws_bytes,
+                                     void* stream);
+
 /* ------------------------------------------------------------------------ */
 /* Diagnostics: HIP-event timing of one kernel.                             */
 /* ------------------------------------------------------------------------ */

@@ -92,6 +92,13 @@ class gnnshap_logits(ctypes.Structure):
                 ("rank", c_vp), ("top_logprob", c_vp), ("top_id", c_vp), ("maximum", c_vp), ("log_sum", c_vp)]
 
 
+class gnnshap_linear(ctypes.Structure):
+    _fields_ = [("dtype", c_i32), ("reserved", c_i32), ("num_rows", c_i64), ("vocab", c_i64), ("width", c_i64),
+                ("hidden", c_vp), ("hidden_stride", c_i64), ("weight", c_vp), ("weight_stride", c_i64),
+                ("targets", c_vp), ("logprob", c_vp), ("entropy", c_vp), ("lse", c_vp), ("maximum", c_vp),
+                ("log_sum", c_vp)]
+
+
 _P = ctypes.POINTER
 _SIGNATURES = {
     "gnnshap_status_str": (ctypes.c_char_p, [ctypes.c_int]),
@@ -163,6 +170,11 @@ _SIGNATURES = {
     "gnnshap_token_logprobs_workspace": (ctypes.c_int, [_P(gnnshap_logits), _P(ctypes.c_size_t)]),
     "gnnshap_token_logprobs": (ctypes.c_int, [_P(gnnshap_logits), c_vp, c_vp, ctypes.c_size_t, c_vp]),
     "gnnshap_token_logprobs_backward": (ctypes.c_int, [_P(gnnshap_logits), c_vp, c_vp, c_vp, c_i64, c_vp, c_vp]),
+    "gnnshap_linear_logprobs_workspace": (ctypes.c_int, [_P(gnnshap_linear), _P(ctypes.c_size_t)]),
+    "gnnshap_linear_logprobs": (ctypes.c_int, [_P(gnnshap_linear), c_vp, c_vp, ctypes.c_size_t, c_vp]),
+    "gnnshap_linear_logprobs_backward_workspace": (ctypes.c_int, [_P(gnnshap_linear), _P(ctypes.c_size_t)]),
+    "gnnshap_linear_logprobs_backward": (ctypes.c_int, [_P(gnnshap_linear), c_vp, c_vp, c_vp, c_i64, c_vp, c_i64,
+                                                        c_vp, c_vp, ctypes.c_size_t, c_vp]),
     "gnnshap_timing_begin": (ctypes.c_int, [ctypes.c_char_p]),
     "gnnshap_timing_end": (ctypes.c_int, [_P(ctypes.c_double), _P(c_i64)]),
     "gnnshap_timing_solves": (ctypes.c_int, [_P(c_i64), c_i64, _P(c_i64)]),
@@ -493,3 +505,26 @@ def gnnshap_token_logprobs(logits, info_ptr, ws_ptr, ws_bytes, stream):
 def gnnshap_token_logprobs_backward(logits, g_logprob_ptr, g_entropy_ptr, grad_ptr, grad_stride, info_ptr, stream):
     check(load().gnnshap_token_logprobs_backward(logits, g_logprob_ptr, g_entropy_ptr, grad_ptr, grad_stride,
                                                  info_ptr, stream), "token_logprobs_backward")
+
+
+def gnnshap_linear_logprobs_workspace(linear):
+    n = ctypes.c_size_t()
+    check(load().gnnshap_linear_logprobs_workspace(linear, n), "linear_logprobs_workspace")
+    return n.value
+
+
+def gnnshap_linear_logprobs(linear, info_ptr, ws_ptr, ws_bytes, stream):
+    check(load().gnnshap_linear_logprobs(linear, info_ptr, ws_ptr, ws_bytes, stream), "linear_logprobs")
+
+
+def gnnshap_linear_logprobs_backward_workspace(linear):
+    n = ctypes.c_size_t()
+    check(load().gnnshap_linear_logprobs_backward_workspace(linear, n), "linear_logprobs_backward_workspace")
+    return n.value
+
+
+def gnnshap_linear_logprobs_backward(linear, g_logprob_ptr, g_entropy_ptr, grad_hidden_ptr, grad_hidden_stride,
+                                     grad_weight_ptr, grad_weight_stride, info_ptr, ws_ptr, ws_bytes, stream):
+    check(load().gnnshap_linear_logprobs_backward(linear, g_logprob_ptr, g_entropy_ptr, grad_hidden_ptr,
+                                                  grad_hidden_stride, grad_weight_ptr, grad_weight_stride, info_ptr,
+                                                  ws_ptr, ws_bytes, stream), "linear_logprobs_backward")

@@ -409,6 +409,105 @@ def differentiable_logprobs(logits, targets):
     return _Logprob.apply(logits, targets)
 
 
+class LinearLogprobs(NamedTuple):
+    logprob: torch.Tensor       # float32 [rows]: log probability of the given token
+    entropy: torch.Tensor       # float32 [rows]
+    lse: torch.Tensor           # float32 [rows]: log of the sum of exponentials
+    maximum: torch.Tensor       # float32 [rows]: the largest logit
+    log_sum: torch.Tensor       # float32 [rows]: log of the sum of exp(x - maximum)
+
+
+def _linear(hidden, weight, targets, **outputs):
+    """The library's description of hidden states [rows, width] and weights [vocabulary, width]."""
+    if (hidden.dim() != 2 or not hidden.is_cuda or hidden.dtype not in _DTYPES
+            or (hidden.stride(1) != 1 and hidden.shape[1] > 1)):
+        raise ValueError(f"hidden: a [rows, width] float32, float16 or bfloat16 tensor on a GPU with a contiguous last "
+                         f"axis is needed, got {hidden.dtype} {tuple(hidden.shape)} with strides {hidden.stride()} on "
+                         f"{hidden.device}")
+    (rows, width), dev = hidden.shape, hidden.device
+    if (weight.dim() != 2 or weight.dtype != hidden.dtype or weight.device != dev or weight.shape[1] != width
+            or (weight.stride(1) != 1 and width > 1)):
+        raise ValueError(f"weight: a [vocabulary, {width}] {hidden.dtype} tensor on {dev} with a contiguous last axis "
+                         f"is needed, got {weight.dtype} {tuple(weight.shape)} with strides {weight.stride()} on "
+                         f"{weight.device}")
+    return L.gnnshap_linear(_DTYPES[hidden.dtype], 0, rows, weight.shape[0], width, hidden.data_ptr(), hidden.stride(0),
+                            weight.data_ptr(), weight.stride(0), _vector(targets, "targets", torch.int64, (rows,), dev),
+                            **outputs)
+
+
+def linear_logprobs(hidden, weight, targets=None, info=None):
+    """gnnshap_linear_logprobs: what token_logprobs gives of the logits hidden
+    [rows, width] @ weight [vocabulary, width]^T, without keeping them: log
+    probabilities of the tokens `targets` (int64 [rows]; negative or None: no
+    token, 0), entropies and lse, and its two parts for the gradient.  The logits
+    are in fp32 and not rounded to the weights' type.  Returns a LinearLogprobs."""
+    _no_derivative("linear_logprobs (but for differentiable_linear_logprobs)", hidden, weight)
+    a = _linear(hidden, weight, targets)
+    rows, dev = hidden.shape[0], hidden.device
+    r = LinearLogprobs(*torch.empty((5, rows), dtype=torch.float32, device=dev).unbind(0))
+    a.logprob, a.entropy, a.lse, a.maximum, a.log_sum = (x.data_ptr() for x in r)
+    nbytes = L.gnnshap_linear_logprobs_workspace(a)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+    _on(dev, L.gnnshap_linear_logprobs, a, _vector(info, "info", torch.int32, (1,), dev), _ptr(ws), nbytes)
+    return r
+
+
+def linear_logprobs_backward(hidden, weight, targets, maximum, log_sum, entropy=None, grad_logprob=None,
+                             grad_entropy=None, of_hidden=True, of_weight=True, info=None):
+    """gnnshap_linear_logprobs_backward: the gradients by hidden and by weight
+    (None for one that is not wanted) of sum(grad_logprob * logprob) +
+    sum(grad_entropy * entropy), in their type; maximum, log_sum and entropy as
+    linear_logprobs gave them.  The logits are computed again, a piece of the
+    vocabulary at a time."""
+    _no_derivative("linear_logprobs_backward", hidden, weight, maximum, log_sum, entropy, grad_logprob, grad_entropy)
+    a = _linear(hidden, weight, targets)
+    size, dev = (hidden.shape[0],), hidden.device
+    _give_parts(a, maximum, log_sum, size, dev)
+    a.entropy = _vector(entropy, "entropy", torch.float32, size, dev)
+    out = [torch.empty(x.shape, dtype=x.dtype, device=dev) if wanted else None
+           for x, wanted in ((hidden, of_hidden), (weight, of_weight))]
+    nbytes = L.gnnshap_linear_logprobs_backward_workspace(a)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+    _on(dev, L.gnnshap_linear_logprobs_backward, a,
+        _vector(grad_logprob, "grad_logprob", torch.float32, size, dev),
+        _vector(grad_entropy, "grad_entropy", torch.float32, size, dev), _ptr(out[0]), hidden.shape[1], _ptr(out[1]),
+        hidden.shape[1], _vector(info, "info", torch.int32, (1,), dev), _ptr(ws), nbytes)
+    return tuple(out)
+
+
+class _LinearLogprob(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, hidden, weight, targets):
+        r = linear_logprobs(hidden, weight, targets)
+        ctx.save_for_backward(hidden, weight, targets, r.maximum, r.log_sum, r.entropy)
+        return r.logprob, r.entropy
+
+    @staticmethod
+    def backward(ctx, grad_logprob, grad_entropy):
+        return (*_LinearLogprobGradient.apply(*ctx.saved_tensors, grad_logprob, grad_entropy,
+                                              *ctx.needs_input_grad[:2]), None)
+
+
+class _LinearLogprobGradient(torch.autograd.Function):
+    """The gradient as a node of its own, so that differentiating it again raises."""
+    @staticmethod
+    def forward(ctx, hidden, weight, targets, maximum, log_sum, entropy, grad_logprob, grad_entropy, *wanted):
+        grads = (None if g is None else g.float().contiguous() for g in (grad_logprob, grad_entropy))
+        return linear_logprobs_backward(hidden, weight, targets, maximum, log_sum, entropy, *grads, *wanted)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("differentiable_linear_logprobs has a first derivative only")
+
+
+def differentiable_linear_logprobs(hidden, weight, targets):
+    """Log probabilities of `targets` (int64 [rows]) and entropies of the logits
+    hidden @ weight^T with their gradient by hidden and weight (autograd), for
+    training and attributions: neither pass keeps the logits.  The gradient is
+    of first order: differentiating it again raises."""
+    return _LinearLogprob.apply(hidden, weight, targets)
+
+
 def _batches(rows, batch):
     """Bounds of batches of at most `batch` rows, of which the last has two at
     least: one row alone would be the full coalition, so the batch before it

@@ -1,0 +1,436 @@
+// Gradients of the log probabilities from hidden states, by these and by the
+// vocabulary's weights.
+//
+// With p = e^{x - lse} of the logits x = h w^T, H the entropy and g, g_H the
+// incoming gradients of a row,
+//     d_j = g (1[j = t] - p_j) - g_H p_j (log p_j + H),
+//     dh = d w,  dw = d^T h.
+// The logits are not kept by the forward pass: they are computed again (the
+// same product, bit for bit), for a piece of the vocabulary at a time, whose d
+// is written in the elements' type and read by the two other products; w and h
+// are turned over on the way from LDS to the matrix instructions.  So are three
+// products of 2 rows vocabulary width operations each, where many rows make
+// them bound by the matrix instructions; few rows are bound by reading the
+// weights twice and writing their gradient once.
+//
+// dh sums over the vocabulary, of which several workgroups take parts where the
+// tiles are few: each keeps its part of the sum in fp32 over all pieces, and a
+// last launch adds the parts up in order.
+//
+// In fp16 d is carried 2^k larger, k from the largest incoming gradient, so that
+// its largest elements are below 2^15 and those down to 2^-28 of them keep 11
+// bits; of bf16 and fp32 the exponent's range needs none of it.
+#include "linear.h"
+
+namespace {
+
+using namespace gnnshap;
+
+constexpr int64_t kPieceBytes = int64_t(192) << 20;  // of d
+
+template <class P>
+__global__ __launch_bounds__(P::kThreads) void k_linear_d(LinearArgs a) {
+  using T = typename P::T;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const TileAt tile = tile_at(blockIdx.x, a.tiles_m, a.tiles_n);
+  const int64_t v0 = static_cast<int64_t>(tile.m) * P::TM, b0 = static_cast<int64_t>(tile.n) * P::TN;
+  P p;
+  p.run(lds, Operand{static_cast<const T*>(a.l.weight) + a.v0 * a.l.weight_stride, a.l.weight_stride, a.piece},
+        Operand{a.l.hidden, a.l.hidden_stride, a.l.num_rows}, v0, b0, a.l.width);
+  const float scale = a.scale ? a.scale[0] : 1.f;
+#pragma unroll
+  for (int t = 0; t < P::NT; ++t) {
+    const int64_t row = b0 + p.col_of(t);
+    if (row >= a.l.num_rows) continue;
+    int64_t given = a.l.targets ? a.l.targets[row] : -1;
+    if (given >= a.l.vocab) {
+      if (a.info) *a.info = 1;
+      given = -1;
+    }
+    const float top = a.l.maximum[row], logs = a.l.log_sum[row];
+    const float gl = a.gl && given >= 0 ? a.gl[row] : 0.f;
+    const float ge = a.ge ? a.ge[row] : 0.f, ent = a.ge ? a.l.entropy[row] : 0.f;
+    const bool none = top == -INFINITY && logs == 0.f;
+    given -= a.v0 + v0;
+    T* const out = static_cast<T*>(a.d) + row * a.pitch + v0;
+#pragma unroll
+    for (int j = 0; j < P::kRuns; ++j) {
+      constexpr int kPack = P::kRun < 16 / static_cast<int>(sizeof(T)) ? P::kRun : 16 / static_cast<int>(sizeof(T));
+#pragma unroll
+      for (int i0 = 0; i0 < P::kRun; i0 += kPack) {
+        Pack<T, kPack> hi, lo;
+#pragma unroll
+        for (int i = 0; i < kPack; ++i) {
+          const int at = p.run_of(j) + i0 + i;
+          const float logp = (p.at(j, i0 + i, t) - top) - logs, e = __builtin_amdgcn_exp2f(logp * kLog2e);
+          const float own = at == given ? gl : 0.f;
+          float d = own - e * (gl + ge * ((e == 0.f ? 0.f : logp) + ent));
+          if (none || v0 + at >= a.piece) d = 0.f;  // behind the piece: the products read it
+          d *= scale;
+          hi.v[i] = static_cast<T>(d);
+          lo.v[i] = static_cast<T>(d - static_cast<float>(hi.v[i]));
+        }
+        store_pack(out + p.run_of(j) + i0, hi);
+        if (a.two) store_pack(out + a.l.num_rows * a.pitch + p.run_of(j) + i0, lo);
+      }
+    }
+  }
+}
+
+struct HiddenArgs {
+  const void* weight;   // of the piece
+  int64_t weight_stride;
+  const void* d;
+  int64_t pitch;
+  int64_t piece, rows, width;  // rows of d
+  unsigned tiles_m, tiles_n;
+  int64_t split;        // of the vocabulary, a workgroup
+  float* sums;          // [split][row][width]
+  bool first;           // piece
+};
+
+// dh's parts: a tile's rows are elements of the width, its columns rows of d.
+template <class P>
+__global__ __launch_bounds__(P::kThreads) void k_linear_dh(HiddenArgs a) {
+  using T = typename P::T;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const unsigned tiles = a.tiles_m * a.tiles_n, part = blockIdx.x / tiles;
+  const TileAt tile = tile_at(blockIdx.x - part * tiles, a.tiles_m, a.tiles_n);
+  const int64_t m0 = static_cast<int64_t>(tile.m) * P::TM, n0 = static_cast<int64_t>(tile.n) * P::TN;
+  const int64_t k0 = part * a.split, K = a.piece - k0 < a.split ? a.piece - k0 : a.split;
+  P p;
+  p.run(lds, Operand{static_cast<const T*>(a.weight) + k0 * a.weight_stride, a.weight_stride, a.width},
+        Operand{static_cast<const T*>(a.d) + k0, a.pitch, a.rows}, m0, n0, K > 0 ? K : 0);
+#pragma unroll
+  for (int t = 0; t < P::NT; ++t) {
+    const int64_t row = n0 + p.col_of(t);
+    if (row >= a.rows) continue;
+#pragma unroll
+    for (int j = 0; j < P::kRuns; ++j) {
+      const int64_t m = m0 + p.run_of(j);
+      float* const out = a.sums + (part * a.rows + row) * a.width + m;
+#pragma unroll
+      for (int i = 0; i < P::kRun; i += 4) {
+        Pack<float, 4> x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x.v[e] = p.at(j, i + e, t);
+        if (m + i + 4 <= a.width) {
+          if (!a.first) {
+            const Pack<float, 4> y = load_pack<float, 4>(out + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x.v[e] += y.v[e];
+          }
+          store_pack(out + i, x);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (m + i + e < a.width) out[i + e] = a.first ? x.v[e] : x.v[e] + out[i + e];
+        }
+      }
+    }
+  }
+}
+
+struct JoinArgs {
+  const float* sums;
+  int64_t parts, rows, width;
+  bool two;             // row b's second part is row rows / 2 + b
+  const float* scale;
+  void* out;
+  int64_t stride;
+};
+
+// Adds up dh's parts, four elements to a thread.
+template <class T>
+__global__ __launch_bounds__(256) void k_linear_dh_join(JoinArgs a) {
+  const int64_t packs = (a.width + 3) / 4, rows = a.two ? a.rows / 2 : a.rows;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= rows * packs) return;
+  const int64_t row = i / packs, m = (i - row * packs) * 4;
+  const int n = a.width - m < 4 ? static_cast<int>(a.width - m) : 4;
+  const float over = a.scale ? a.scale[1] : 1.f;
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  const auto add_row = [&](const float* p) {
+    if (n == 4) {
+      const Pack<float, 4> x = load_pack<float, 4>(p);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] += x.v[e];
+    } else {
+      for (int e = 0; e < n; ++e) s[e] += p[e];
+    }
+  };
+#pragma unroll 4
+  for (int64_t part = 0; part < a.parts; ++part) add_row(a.sums + (part * a.rows + row) * a.width + m);
+  if (a.two)
+#pragma unroll 4
+    for (int64_t part = 0; part < a.parts; ++part) add_row(a.sums + (part * a.rows + rows + row) * a.width + m);
+  T* const out = static_cast<T*>(a.out) + row * a.stride + m;
+  if (n == 4) {
+    Pack<T, 4> x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x.v[e] = static_cast<T>(s[e] * over);
+    store_pack(out, x);
+  } else {
+    for (int e = 0; e < n; ++e) out[e] = static_cast<T>(s[e] * over);
+  }
+}
+
+struct WeightArgs {
+  const void* hidden;
+  int64_t hidden_stride;
+  const void* d;
+  int64_t pitch;
+  int64_t piece, rows, width;  // rows of the hidden states
+  bool two;
+  unsigned tiles_m, tiles_n;
+  const float* scale;
+  void* out;            // of the piece
+  int64_t stride;
+};
+
+// dw: a tile's rows are elements of the width, its columns tokens.
+template <class P>
+__global__ __launch_bounds__(P::kThreads) void k_linear_dw(WeightArgs a) {
+  using T = typename P::T;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const TileAt tile = tile_at(blockIdx.x, a.tiles_m, a.tiles_n);
+  const int64_t m0 = static_cast<int64_t>(tile.m) * P::TM, n0 = static_cast<int64_t>(tile.n) * P::TN;
+  P p;
+  p.run(lds, Operand{a.hidden, a.hidden_stride, a.width}, Operand{a.d, a.pitch, a.piece}, m0, n0, a.rows, a.two ? 2 : 1,
+        0, a.rows * a.pitch * static_cast<int64_t>(sizeof(T)));
+  const float over = a.scale ? a.scale[1] : 1.f;
+  constexpr int kPack = 16 / sizeof(T);
+#pragma unroll
+  for (int t = 0; t < P::NT; ++t) {
+    const int64_t token = n0 + p.col_of(t);
+    if (token >= a.piece) continue;
+#pragma unroll
+    for (int j = 0; j < P::kRuns; ++j) {
+      const int64_t m = m0 + p.run_of(j);
+      T* const out = static_cast<T*>(a.out) + token * a.stride + m;
+#pragma unroll
+      for (int i = 0; i < P::kRun; i += kPack) {
+        Pack<T, kPack> x;
+#pragma unroll
+        for (int e = 0; e < kPack; ++e) x.v[e] = static_cast<T>(p.at(j, i + e, t) * over);
+        if (m + i + kPack <= a.width) {
+          store_pack(out + i, x);
+        } else {
+#pragma unroll
+          for (int e = 0; e < kPack; ++e)
+            if (m + i + e < a.width) out[i + e] = x.v[e];
+        }
+      }
+    }
+  }
+}
+
+// The power of two that d is carried larger by, and one over it: |d| is at most
+// 2 |g| + |g_H| (H + 1), of which the largest comes to 2^14 .. 2^15.
+__global__ __launch_bounds__(1024) void k_linear_scale(LinearArgs a, float* scale) {
+  __shared__ float most[16];
+  float m = 0.f;
+  for (int64_t b = threadIdx.x; b < a.l.num_rows; b += 1024) {
+    float x = a.gl ? 2.f * fabsf(a.gl[b]) : 0.f;
+    if (a.ge) x += fabsf(a.ge[b]) * (fabsf(a.l.entropy[b]) + 1.f);
+    if (x < INFINITY) m = fmaxf(m, x);
+  }
+  for (int off = 1; off < 64; off *= 2) m = fmaxf(m, __shfl_xor(m, off));
+  if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = m;
+  __syncthreads();
+  if (threadIdx.x > 0) return;
+  for (int i = 1; i < 16; ++i) m = fmaxf(m, most[i]);
+  int e = 0;
+  if (m > 0.f) frexpf(m, &e);
+  const int k = m > 0.f ? max(-100, min(100, 15 - e)) : 0;
+  scale[0] = ldexpf(1.f, k);
+  scale[1] = ldexpf(1.f, -k);
+}
+
+template <class T, bool DIRECT>
+using HiddenMany = Product<T, 8, 4, 2, 4, 64, 4, true, false, DIRECT>;
+template <class T, bool DIRECT>
+using HiddenSome = Product<T, 4, 4, 4, 1, 64, 4, true, false, DIRECT>;
+template <class T, bool DIRECT>
+using HiddenFew = Product<T, 4, 2, 4, 1, 64, 4, true, false, DIRECT>;
+template <class T, bool DIRECT>
+using Weights = Product<T, 8, 4, 2, 4, 64, 4, true, true, DIRECT>;
+
+template <class T, class F>
+int with_hidden(int64_t rows, bool direct, F f) {
+  const auto pick = [&](auto d) {
+    constexpr bool D = decltype(d)::value;
+    if (rows <= 32) return f(static_cast<HiddenFew<T, D>*>(nullptr));
+    if (rows <= 256) return f(static_cast<HiddenSome<T, D>*>(nullptr));
+    return f(static_cast<HiddenMany<T, D>*>(nullptr));
+  };
+  return direct ? pick(std::true_type()) : pick(std::false_type());
+}
+template <class T, class F>
+int with_weights(bool direct, F f) {
+  return direct ? f(static_cast<Weights<T, true>*>(nullptr)) : f(static_cast<Weights<T, false>*>(nullptr));
+}
+
+// How the backward pass is laid out; all of it goes by the sizes alone.
+struct Layout {
+  bool two;
+  int64_t d_rows, piece, pitch, split, parts;
+  float* scale;
+  void* d;
+  float* sums;
+};
+
+template <class T>
+Layout lay_out(const gnnshap_linear& l) {
+  Layout y{};
+  y.two = sizeof(T) == 2 && l.num_rows <= kTwoParts;
+  y.d_rows = y.two ? 2 * l.num_rows : l.num_rows;
+  // pieces of like size, whole tiles of 256
+  const int64_t most = std::max<int64_t>(kPieceBytes / (std::max<int64_t>(y.d_rows, 1) * sizeof(T)) / 256 * 256, 256);
+  const int64_t pieces = ceil_div(l.vocab, most);
+  y.piece = ceil_div(ceil_div(l.vocab, pieces), 256) * 256;
+  y.pitch = y.piece;
+  // enough workgroups for the chip, each with 512 tokens at least
+  with_hidden<T>(y.d_rows, true, [&](auto* p) {
+    using P = std::remove_pointer_t<decltype(p)>;
+    const int64_t tiles = ceil_div(l.width, P::TM) * ceil_div(std::max<int64_t>(y.d_rows, 1), P::TN);
+    const int64_t want = std::max<int64_t>(1, (P::TN >= 256 ? 256 : 512) / tiles);
+    y.split = std::max<int64_t>(ceil_div(ceil_div(y.piece, want), 64) * 64, 512);
+    y.parts = ceil_div(y.piece, y.split);
+    return 0;
+  });
+  return y;
+}
+
+size_t carve(Layout& y, const gnnshap_linear& l, void* ws) {
+  Carver c(ws);
+  y.scale = c.take<float>(2);
+  y.d = c.take<char>(static_cast<size_t>(y.d_rows) * y.pitch * (l.dtype == GNNSHAP_F32 ? 4 : 2));
+  y.sums = c.take<float>(static_cast<size_t>(y.parts) * y.d_rows * l.width);
+  return c.bytes();
+}
+
+template <class P, class A>
+int launch(void (*kernel)(A), const char* name, const A& a, int64_t workgroups, hipStream_t s) {
+  if (const int st = check_launch(workgroups, P::kThreads)) return st;
+  GS_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, P::kLds));
+  {
+    GS_TIMED(name, s);
+    kernel<<<static_cast<unsigned>(workgroups), P::kThreads, P::kLds, s>>>(a);
+  }
+  GS_LAUNCHED();
+  return GNNSHAP_OK;
+}
+
+template <class T>
+int run(const LinearArgs& given, void* grad_hidden, int64_t gh_stride, void* grad_weight, int64_t gw_stride,
+        Layout y, hipStream_t s) {
+  const gnnshap_linear& l = given.l;
+  LinearArgs a = given;
+  if (l.dtype == GNNSHAP_F16 && l.num_rows > 0) {
+    {
+      GS_TIMED("k_linear_scale", s);
+      k_linear_scale<<<1, 1024, 0, s>>>(a, y.scale);
+    }
+    GS_LAUNCHED();
+    a.scale = y.scale;
+  }
+  a.d = y.d;
+  a.pitch = y.pitch;
+  a.two = y.two;
+  const bool direct_logits_too = direct_logits<T>(l);
+  // turned over, packs lie along the width
+  const bool direct_w = direct_operand<T>(l.weight, l.weight_stride, l.width, 256);
+  const bool direct_h = direct_operand<T>(l.hidden, l.hidden_stride, l.width, 256);
+  for (int64_t v0 = 0; v0 < l.vocab; v0 += y.piece) {
+    const int64_t piece = std::min(y.piece, l.vocab - v0);
+    int st = GNNSHAP_OK;
+    if (l.num_rows > 0) {
+      st = with_logits<T>(l.num_rows, direct_logits_too, [&](auto* p) {
+        using P = std::remove_pointer_t<decltype(p)>;
+        a.v0 = v0;
+        a.piece = piece;
+        a.tiles_m = static_cast<unsigned>(ceil_div(piece, P::TM));
+        a.tiles_n = static_cast<unsigned>(ceil_div(l.num_rows, P::TN));
+        return launch<P>(k_linear_d<P>, "k_linear_d", a, static_cast<int64_t>(a.tiles_m) * a.tiles_n, s);
+      });
+      if (st) return st;
+    }
+    if (grad_hidden && l.num_rows > 0) {
+      st = with_hidden<T>(y.d_rows, direct_w, [&](auto* p) {
+        using P = std::remove_pointer_t<decltype(p)>;
+        HiddenArgs h{static_cast<const T*>(l.weight) + v0 * l.weight_stride, l.weight_stride, y.d, y.pitch, piece, y.d_rows,
+                     l.width, static_cast<unsigned>(ceil_div(l.width, P::TM)),
+                     static_cast<unsigned>(ceil_div(y.d_rows, P::TN)), y.split, y.sums, v0 == 0};
+        return launch<P>(k_linear_dh<P>, "k_linear_dh", h, y.parts * h.tiles_m * h.tiles_n, s);
+      });
+      if (st) return st;
+    }
+    if (grad_weight) {
+      st = with_weights<T>(direct_h, [&](auto* p) {
+        using P = std::remove_pointer_t<decltype(p)>;
+        WeightArgs w{l.hidden, l.hidden_stride, y.d, y.pitch, piece, l.num_rows, l.width, y.two,
+                     static_cast<unsigned>(ceil_div(l.width, P::TM)), static_cast<unsigned>(ceil_div(piece, P::TN)),
+                     a.scale, static_cast<T*>(grad_weight) + v0 * gw_stride, gw_stride};
+        return launch<P>(k_linear_dw<P>, "k_linear_dw", w, static_cast<int64_t>(w.tiles_m) * w.tiles_n, s);
+      });
+      if (st) return st;
+    }
+  }
+  if (grad_hidden && l.num_rows > 0) {
+    JoinArgs j{y.sums, y.parts, y.d_rows, l.width, y.two, a.scale, grad_hidden, gh_stride};
+    const int64_t groups = ceil_div(l.num_rows * ceil_div(l.width, 4), 256);
+    if (const int st = check_launch(groups, 256)) return st;
+    {
+      GS_TIMED("k_linear_dh_join", s);
+      k_linear_dh_join<T><<<static_cast<unsigned>(groups), 256, 0, s>>>(j);
+    }
+    GS_LAUNCHED();
+  }
+  return GNNSHAP_OK;
+}
+
+}  // namespace
+
+extern "C" int gnnshap_linear_logprobs_backward_workspace(const gnnshap_linear* l, size_t* bytes) {
+  GS_TRY_BEGIN
+  clear_error();
+  if (!bytes) return fail(GNNSHAP_EINVAL, "bytes is NULL");
+  if (const int st = check_linear(l)) return st;
+  return with_dtype(l->dtype, [&](auto* x) {
+    Layout y = lay_out<std::remove_pointer_t<decltype(x)>>(*l);
+    *bytes = carve(y, *l, nullptr);
+    return static_cast<int>(GNNSHAP_OK);
+  });
+  GS_TRY_END
+}
+
+extern "C" int gnnshap_linear_logprobs_backward(const gnnshap_linear* l, const float* g_logprob, const float* g_entropy,
+                                                void* grad_hidden, int64_t grad_hidden_stride, void* grad_weight,
+                                                int64_t grad_weight_stride, int32_t* info, void* ws, size_t ws_bytes,
+                                                void* stream) {
+  GS_TRY_BEGIN
+  clear_error();
+  if (const int st = check_linear(l)) return st;
+  if (grad_hidden_stride < 0 || grad_weight_stride < 0) return fail(GNNSHAP_EINVAL, "negative stride of a gradient");
+  if (l->num_rows > 0 &&
+      (!l->hidden || !l->weight || !l->maximum || !l->log_sum || (g_entropy && !l->entropy)))
+    return fail(GNNSHAP_EINVAL, "NULL hidden, weight, maximum, log_sum or (with g_entropy) entropy");
+  if (!grad_hidden && !grad_weight) return GNNSHAP_OK;
+  LinearArgs a{};
+  a.l = *l;
+  a.gl = g_logprob;
+  a.ge = g_entropy;
+  a.info = info;
+  return with_dtype(l->dtype, [&](auto* x) {
+    using T = std::remove_pointer_t<decltype(x)>;
+    Layout y = lay_out<T>(*l);
+    const size_t need = carve(y, *l, ws);
+    if (!ws || ws_bytes < need)
+      return fail(GNNSHAP_ECAPACITY, "linear_logprobs_backward workspace needs %zu bytes, has %zu", need,
+                  ws ? ws_bytes : 0);
+    return run<T>(a, grad_hidden, grad_hidden_stride, grad_weight, grad_weight_stride, y,
+                  static_cast<hipStream_t>(stream));
+  });
+  GS_TRY_END
+}

@@ -24,7 +24,7 @@
 // 137 us, 4.8 TB/s (from 127 to 160, by the clocks), with the top 5 152 us, 4.3
 // TB/s.  One row of 131,072 with the top 20: 8.5 us, and 7.2 us to join its 16
 // parts.
-#include "tokens.h"
+#include "stats.h"
 
 namespace {
 
@@ -34,18 +34,18 @@ using gnnshap::load_pack;
 using gnnshap::Pack;
 using gnnshap::store_pack;
 
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
+using gnnshap::add;
+using gnnshap::finite_max;
+using gnnshap::kLn2;
+using gnnshap::kLog2e;
+using gnnshap::move_to;
+using gnnshap::no_stats;
+using gnnshap::Stats;
+using gnnshap::wave_sum;
+
 constexpr int kWaves = 4;      // wavefronts of a workgroup
 constexpr int kMaxParts = 64;        // workgroups of a row
 constexpr int kMaxPartKeys = 1024;  // of their alternatives
-
-struct Stats {
-  float m, s, w;  // w = sum e_j log2(e_j)
-};
-__device__ __forceinline__ Stats no_stats() { return Stats{-INFINITY, 0.f, 0.f}; }
-
-__device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.f : m; }
 
 // The value of a lane of the same 16, `Turn` lanes on, moved within the vector unit.
 template <int Turn>
@@ -73,36 +73,6 @@ __device__ __forceinline__ X together(X x, F f) {
     x = f(x, static_cast<X>(__shfl_xor(x, 32)));
   }
   return x;
-}
-
-// Moves a to the maximum m >= a.m.  Far below it f is 0, and what it multiplies
-// has to stay finite: up to 2^30 logits times 1e4.
-__device__ __forceinline__ void move_to(Stats& a, float m) {
-  if (a.s != 0.f) {  // NaN too
-    const float d = (a.m - finite_max(m)) * kLog2e, f = __builtin_amdgcn_exp2f(d);
-    a.w = f * (a.w + a.s * fmaxf(d, -1e4f));
-    a.s *= f;
-  }
-  a.m = m;
-}
-
-__device__ __forceinline__ void add(Stats& a, Stats b) {
-  const float m = fmaxf(a.m, b.m);
-  move_to(a, m);
-  move_to(b, m);
-  a.s += b.s;
-  a.w += b.w;
-}
-
-__device__ __forceinline__ void wave_sum(Stats& a) {
-#pragma unroll
-  for (int off = 1; off < 64; off *= 2) {
-    Stats b;
-    b.m = __shfl_xor(a.m, off);
-    b.s = __shfl_xor(a.s, off);
-    b.w = __shfl_xor(a.w, off);
-    add(a, b);
-  }
 }
 
 // Whole numbers in the order of the floats (-0 and 0 alike, NaN above all; none
