@@ -682,6 +682,75 @@ int gnnshap_cache_attend_workspace(const gnnshap_cache* cache, const gnnshap_que
 int gnnshap_cache_attend(const gnnshap_cache* cache, const gnnshap_queries* queries, int32_t* info, void* ws,
                          size_t ws_bytes, void* stream);
 
+/* What attention looked at.  Row b is one of rows_per_seq rows on end whose
+ * queries see the tokens of one sequence, row b / rows_per_seq of table: its
+ * first lengths[b] tokens (a new token's row all of them, a prompt's row those
+ * up to its own), and of these, as in gnnshap_queries, the positions that are no
+ * player (outside first_player .. first_player + num_players - 1) or whose bit of
+ * row b of `masks` is set. */
+typedef struct {
+  int64_t num_rows;
+  int32_t heads;                 /* as in gnnshap_queries */
+  int32_t reserved;
+  const void* q;                 /* [dev] */
+  int64_t q_row_stride, q_head_stride;
+  const float* lse;              /* [dev] num_rows x heads, as gnnshap_cache_attend wrote it */
+  const int32_t* table;          /* [dev] sequences x table_width */
+  const int32_t* lengths;        /* [dev] num_rows */
+  int64_t rows_per_seq;          /* divides num_rows */
+  int64_t table_width, max_length;  /* max_length: no length is larger; at most table_width pages' tokens */
+  const uint64_t* masks;         /* [dev] num_rows x mask_words, or NULL (num_players is then 0) */
+  int64_t mask_words, num_players, first_player;
+  double scale;                  /* scores are scale q.k, as for gnnshap_cache_attend */
+  float* weights;                /* [dev] sequence s's at weights + s weights_stride, max_length of them */
+  int64_t weights_stride;
+} gnnshap_observed;
+
+/* Bytes of device workspace for gnnshap_cache_weights (the parts of many
+ * queries' sums). */
+int gnnshap_cache_weights_workspace(const gnnshap_cache* cache, const gnnshap_observed* observed, size_t* bytes);
+
+/* Adds to weights[s][j] the weight that sequence s's rows gave its token j,
+ *     sum over rows b of s that see j and heads of exp(scale q.k_j - lse_b),
+ * in fp32 and in a fixed order.  Where lse is of a longer context (other parts
+ * too), so are the weights.  A row of lse -inf gives nothing; tokens that no row
+ * sees keep what they have, whatever their keys hold.  EINVAL: sizes, NULL
+ * arrays; EUNSUPPORTED: head_dim, dtype, more than 2^30 tokens; ECAPACITY:
+ * workspace. */
+int gnnshap_cache_weights(const gnnshap_cache* cache, const gnnshap_observed* observed, int32_t* info, void* ws,
+                          size_t ws_bytes, void* stream);
+
+/* Sequences that give up tokens.  Their pages must be theirs alone: no page is
+ * in two rows of the table, or twice in one. */
+typedef struct {
+  int64_t num_seqs;
+  const int32_t* table;          /* [dev] num_seqs x table_width */
+  int64_t table_width, max_length;
+  const int32_t* lengths;        /* [dev] num_seqs */
+  const float* weights;          /* [dev] sequence s's at weights + s weights_stride, max_length of them */
+  int64_t weights_stride;
+  int64_t keep;                  /* tokens that a sequence keeps at most, >= 1 */
+  int64_t first, recent;         /* of these, its first and its last ones; first + recent <= keep */
+  int32_t* kept;                 /* [dev] num_seqs x keep: the former places of the kept tokens, rising; then -1 */
+  int32_t* new_lengths;          /* [dev] num_seqs; may be lengths */
+  float* new_weights;            /* [dev] likewise; may be weights, with their stride: the kept tokens', then 0 */
+  int64_t new_weights_stride;
+} gnnshap_eviction;
+
+/* Bytes of device workspace for gnnshap_cache_evict. */
+int gnnshap_cache_evict_workspace(const gnnshap_cache* cache, const gnnshap_eviction* eviction, size_t* bytes);
+
+/* Sequences of more than `keep` tokens keep their first and their last ones and,
+ * of those between, the ones of the largest weights (of equal weights the lower
+ * place; NaN counts as the largest); the others' keys and values are dropped, and
+ * the kept ones moved up in the pages, in their order, bit for bit.  Slots behind
+ * a sequence's new length hold what they held before or a dropped token's.
+ * Sequences of `keep` tokens or fewer stay as they are.  EINVAL: sizes, NULL
+ * arrays; EUNSUPPORTED: head_dim, dtype, more than 2^30 tokens; ECAPACITY:
+ * workspace. */
+int gnnshap_cache_evict(const gnnshap_cache* cache, const gnnshap_eviction* eviction, int32_t* info, void* ws,
+                        size_t ws_bytes, void* stream);
+
 /* Rows of logits and what is read off them.  Outputs may be NULL, each. */
 typedef struct {
   int32_t dtype;            /* gnnshap_dtype of the logits */

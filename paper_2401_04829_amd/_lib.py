@@ -86,6 +86,20 @@ class gnnshap_queries(ctypes.Structure):
                 ("first_player", c_i64), ("scale", c_dbl)]
 
 
+class gnnshap_observed(ctypes.Structure):
+    _fields_ = [("num_rows", c_i64), ("heads", c_i32), ("reserved", c_i32), ("q", c_vp), ("q_row_stride", c_i64),
+                ("q_head_stride", c_i64), ("lse", c_vp), ("table", c_vp), ("lengths", c_vp), ("rows_per_seq", c_i64),
+                ("table_width", c_i64), ("max_length", c_i64), ("masks", c_vp), ("mask_words", c_i64),
+                ("num_players", c_i64), ("first_player", c_i64), ("scale", c_dbl), ("weights", c_vp),
+                ("weights_stride", c_i64)]
+
+
+class gnnshap_eviction(ctypes.Structure):
+    _fields_ = [("num_seqs", c_i64), ("table", c_vp), ("table_width", c_i64), ("max_length", c_i64), ("lengths", c_vp),
+                ("weights", c_vp), ("weights_stride", c_i64), ("keep", c_i64), ("first", c_i64), ("recent", c_i64),
+                ("kept", c_vp), ("new_lengths", c_vp), ("new_weights", c_vp), ("new_weights_stride", c_i64)]
+
+
 class gnnshap_logits(ctypes.Structure):
     _fields_ = [("dtype", c_i32), ("top", c_i32), ("num_rows", c_i64), ("vocab", c_i64), ("logits", c_vp),
                 ("row_stride", c_i64), ("targets", c_vp), ("logprob", c_vp), ("entropy", c_vp), ("lse", c_vp),
@@ -167,6 +181,12 @@ _SIGNATURES = {
     "gnnshap_cache_attend_workspace": (ctypes.c_int, [_P(gnnshap_cache), _P(gnnshap_queries), _P(ctypes.c_size_t)]),
     "gnnshap_cache_attend": (ctypes.c_int, [_P(gnnshap_cache), _P(gnnshap_queries), c_vp, c_vp, ctypes.c_size_t,
                                             c_vp]),
+    "gnnshap_cache_weights_workspace": (ctypes.c_int, [_P(gnnshap_cache), _P(gnnshap_observed), _P(ctypes.c_size_t)]),
+    "gnnshap_cache_weights": (ctypes.c_int, [_P(gnnshap_cache), _P(gnnshap_observed), c_vp, c_vp, ctypes.c_size_t,
+                                             c_vp]),
+    "gnnshap_cache_evict_workspace": (ctypes.c_int, [_P(gnnshap_cache), _P(gnnshap_eviction), _P(ctypes.c_size_t)]),
+    "gnnshap_cache_evict": (ctypes.c_int, [_P(gnnshap_cache), _P(gnnshap_eviction), c_vp, c_vp, ctypes.c_size_t,
+                                           c_vp]),
     "gnnshap_token_logprobs_workspace": (ctypes.c_int, [_P(gnnshap_logits), _P(ctypes.c_size_t)]),
     "gnnshap_token_logprobs": (ctypes.c_int, [_P(gnnshap_logits), c_vp, c_vp, ctypes.c_size_t, c_vp]),
     "gnnshap_token_logprobs_backward": (ctypes.c_int, [_P(gnnshap_logits), c_vp, c_vp, c_vp, c_i64, c_vp, c_vp]),
@@ -490,6 +510,26 @@ def gnnshap_cache_attend_workspace(cache, queries):
 
 def gnnshap_cache_attend(cache, queries, info_ptr, ws_ptr, ws_bytes, stream):
     check(load().gnnshap_cache_attend(cache, queries, info_ptr, ws_ptr, ws_bytes, stream), "cache_attend")
+
+
+def gnnshap_cache_weights_workspace(cache, observed):
+    n = ctypes.c_size_t()
+    check(load().gnnshap_cache_weights_workspace(cache, observed, n), "cache_weights_workspace")
+    return n.value
+
+
+def gnnshap_cache_weights(cache, observed, info_ptr, ws_ptr, ws_bytes, stream):
+    check(load().gnnshap_cache_weights(cache, observed, info_ptr, ws_ptr, ws_bytes, stream), "cache_weights")
+
+
+def gnnshap_cache_evict_workspace(cache, eviction):
+    n = ctypes.c_size_t()
+    check(load().gnnshap_cache_evict_workspace(cache, eviction, n), "cache_evict_workspace")
+    return n.value
+
+
+def gnnshap_cache_evict(cache, eviction, info_ptr, ws_ptr, ws_bytes, stream):
+    check(load().gnnshap_cache_evict(cache, eviction, info_ptr, ws_ptr, ws_bytes, stream), "cache_evict")
 
 
 def gnnshap_token_logprobs_workspace(logits):

@@ -300,6 +300,90 @@ def attend(cache, q, table=None, lengths=None, max_length=None, shared_table=Non
     return (out, lse) if return_lse else out
 
 
+def _weights_of(t, name, rows, columns, device):
+    """Checks float32 [rows, columns or more] with a contiguous last axis; its address and stride."""
+    if (t.dim() != 2 or t.dtype != torch.float32 or t.device != device or t.shape[0] != rows or t.shape[1] < columns
+            or (t.stride(1) != 1 and t.shape[1] > 1)):
+        raise ValueError(f"{name}: a float32 [{rows}, {columns} or more] tensor on {device} with a contiguous last axis "
+                         f"is needed, got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
+    return t.data_ptr(), t.stride(0)
+
+
+def attention_weights(cache, q, lse, table, lengths, weights, max_length=None, masks=None, num_players=None,
+                      first_player=0, scale=None, info=None):
+    """gnnshap_cache_weights: adds to weights [sequences, tokens] (float32) what
+    the queries q [rows, heads, head dim], whose attention left lse (float32
+    [rows, heads]), gave each token of their sequence, summed over rows and heads.
+    The rows of q are, rows / sequences at a time, those of a row of `table`; row
+    b sees its first lengths[b] (int32 [rows]) tokens: a new token's row all of
+    them, a prompt's rows each those up to its own, coalitions all the prompt's
+    through their masks (as for attend, position first_player + j of the sequence
+    is player j).  max_length bounds the lengths (None: what the table's pages and
+    the weights hold).  Returns weights."""
+    _no_derivative("attention_weights", q, lse, cache.k, weights)
+    dtype, dev, dim = cache.dtype, cache.device, cache.head_dim
+    qp = _heads(q, "q", None, dim, dtype, dev)
+    rows, heads = q.shape[0], q.shape[1]
+    _need(table.dim() == 2 and (rows % table.shape[0] == 0 if table.shape[0] else rows == 0),
+          "table: [sequences, pages], the rows a multiple of the sequences")
+    seqs, width = table.shape
+    max_length = min(width * cache.page_size, weights.shape[-1]) if max_length is None else max_length
+    wp = _weights_of(weights, "weights", seqs, max_length, dev)
+    words = 0
+    if masks is not None:
+        _need(num_players is not None, "masks without num_players")
+        words = masks.shape[-1]
+    else:
+        _need(not num_players, "players without masks")
+        num_players = first_player = 0
+    a = L.gnnshap_observed(
+        rows, heads, 0, *qp, _vector(lse, "lse", torch.float32, (rows, heads), dev),
+        _vector(table, "table", torch.int32, None, dev), _vector(lengths, "lengths", torch.int32, (rows,), dev),
+        max(rows // max(seqs, 1), 1), width, max_length, _vector(masks, "masks", torch.int64, (rows, words), dev), words,
+        num_players, first_player, 1.0 / math.sqrt(dim) if scale is None else scale, *wp)
+    nbytes = L.gnnshap_cache_weights_workspace(cache._c, a)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+    _on(dev, L.gnnshap_cache_weights, cache._c, a, _vector(info, "info", torch.int32, (1,), dev), _ptr(ws), nbytes)
+    return weights
+
+
+class Evicted(NamedTuple):
+    kept: torch.Tensor          # int32 [sequences, keep]: former places of the kept tokens, rising; then -1
+    lengths: torch.Tensor       # int32 [sequences]
+    weights: torch.Tensor       # float32 [sequences, tokens]: the kept tokens', then 0
+
+
+def evict_tokens(cache, table, lengths, weights, keep, first=0, recent=0, max_length=None, lengths_out=None,
+                 weights_out=None, info=None):
+    """gnnshap_cache_evict: cuts each sequence (a row of `table`, whose pages are
+    its own, lengths int32 [sequences]) to `keep` tokens: its `first` and `recent`
+    last ones and, of the others, those of the largest weights (float32
+    [sequences, tokens], as attention_weights adds them up; of equal ones the
+    lower place).  The kept tokens' keys and values move up in the cache, in their
+    order.  max_length bounds the lengths (None: what the table's pages and the
+    weights hold).  Returns an Evicted; lengths_out and weights_out may be given,
+    and be lengths and weights themselves.  Columns of weights_out from
+    max_length on are left as they are."""
+    _no_derivative("evict_tokens", cache.k, cache.v, weights)
+    dev = cache.device
+    _need(table.dim() == 2, "table: [sequences, pages]")
+    seqs, width = table.shape
+    max_length = min(width * cache.page_size, weights.shape[-1]) if max_length is None else max_length
+    wp = _weights_of(weights, "weights", seqs, max_length, dev)
+    lengths_out = torch.empty(seqs, dtype=torch.int32, device=dev) if lengths_out is None else lengths_out
+    weights_out = torch.empty((seqs, max_length), dtype=torch.float32, device=dev) if weights_out is None else weights_out
+    op = _weights_of(weights_out, "weights_out", seqs, max_length, dev)
+    _need(keep >= 1, "at least one token is kept")
+    kept = torch.empty((seqs, keep), dtype=torch.int32, device=dev)
+    a = L.gnnshap_eviction(seqs, _vector(table, "table", torch.int32, None, dev), width, max_length,
+                           _vector(lengths, "lengths", torch.int32, (seqs,), dev), *wp, keep, first, recent,
+                           kept.data_ptr(), _vector(lengths_out, "lengths_out", torch.int32, (seqs,), dev), *op)
+    nbytes = L.gnnshap_cache_evict_workspace(cache._c, a)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+    _on(dev, L.gnnshap_cache_evict, cache._c, a, _vector(info, "info", torch.int32, (1,), dev), _ptr(ws), nbytes)
+    return Evicted(kept, lengths_out, weights_out)
+
+
 class TokenLogprobs(NamedTuple):
     logprob: torch.Tensor       # float32 [rows]: log probability of the given token
     entropy: torch.Tensor       # float32 [rows]

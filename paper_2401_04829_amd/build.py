@@ -19,7 +19,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libgnnshap.so")
 
 HIP_SOURCES = ["extract.hip", "sample.hip", "eval.hip", "eval_wide.hip", "solve.hip", "cg.hip", "fidelity.hip", "gat.hip", "batch.hip", "append.hip",
-               "norm.hip", "attend.hip", "attend_wide.hip", "logprob.hip", "linear.hip",
+               "norm.hip", "attend.hip", "attend_wide.hip", "weights.hip", "evict.hip", "logprob.hip", "linear.hip",
                "linear_grad.hip", "timing.hip"]
 HOST_SOURCES = ["plan.cpp", "status.cpp"]
 ARCH = "gfx950"

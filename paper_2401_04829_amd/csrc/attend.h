@@ -6,9 +6,6 @@
 
 namespace gnnshap {
 
-typedef float f4_t __attribute__((ext_vector_type(4)));
-typedef unsigned u4_t __attribute__((ext_vector_type(4)));
-
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kWaves = 4;
 constexpr int kChunk = 32;  // keys of a wavefront's step

@@ -40,6 +40,7 @@ using gnnshap::kLn2;
 using gnnshap::kLog2e;
 using gnnshap::move_to;
 using gnnshap::no_stats;
+using gnnshap::ordered;
 using gnnshap::Stats;
 using gnnshap::wave_sum;
 
@@ -75,13 +76,7 @@ __device__ __forceinline__ X together(X x, F f) {
   return x;
 }
 
-// Whole numbers in the order of the floats (-0 and 0 alike, NaN above all; none
-// is all ones, so that every key is below the one that a search starts from).
-__device__ __forceinline__ uint32_t ordered(float x) {
-  const uint32_t b = __float_as_uint(x + 0.f);
-  if (x != x) return 0xFFFFFFFEu;
-  return b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u);
-}
+// The float whose image is o.
 __device__ __forceinline__ float unordered(uint32_t o) {
   return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
 }

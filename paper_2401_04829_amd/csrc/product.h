@@ -21,9 +21,6 @@
 
 namespace gnnshap {
 
-typedef float f4_t __attribute__((ext_vector_type(4)));
-typedef unsigned u4_t __attribute__((ext_vector_type(4)));
-
 // How a product's operand lies in memory.
 struct Operand {
   const void* p;

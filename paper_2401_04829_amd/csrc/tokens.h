@@ -11,6 +11,8 @@ namespace gnnshap {
 
 typedef __bf16 bf16_t;
 typedef _Float16 f16_t;
+typedef float f4_t __attribute__((ext_vector_type(4)));
+typedef unsigned u4_t __attribute__((ext_vector_type(4)));
 
 // N elements that are loaded and stored at any element's address (gfx950
 // takes wide accesses at any address).

@@ -1,0 +1,367 @@
+// What attention's queries looked at: each cached token's weight, summed over
+// rows and heads.
+//
+// With a row's lse known, a weight is e^{scale q.k - lse} by itself: no maximum
+// runs along, nothing is scaled again, values are not read.  A wavefront keeps 32
+// keys of a kv head in registers as the left operand of the matrix
+// instructions and takes the queries 16 at a time; the weights that come out (query in
+// the lane's column, keys in its registers) are added up in the lane, and over
+// the 16 columns at the end.
+//
+// Few queries (a new token of each sequence) are bound by reading the keys
+// once; the kv heads' sums meet in LDS.  Many (coalitions, a prompt's rows) are
+// bound by an exponential per query and key; their range is split so that the
+// chip is full, and a second launch adds up the parts in order.
+#include "attend.h"
+
+namespace {
+
+using namespace gnnshap;
+
+constexpr float kLog2eF = 1.4426950408889634f;
+
+struct WeightsArgs {
+  gnnshap_cache c;
+  gnnshap_observed o;
+  int share, page_shift;
+  int64_t queries;   // of a sequence and kv head
+  float scale;
+  int splits;        // of the queries; 0: the kernel of few
+  int64_t split;     // tiles of 16 queries of a split
+  float* part;       // [sequence][kv head][split][max_length]
+  int32_t* info;
+};
+
+// 16 keys or queries, this lane's quarter of their elements.
+template <class T, int DP>
+struct Vectors {
+  static constexpr int kVec = 16 / sizeof(T), kSteps = DP / (4 * kVec);
+  u4_t s[kSteps];
+  __device__ __forceinline__ void load(const T* p, int D) {
+    const int g = (threadIdx.x >> 4) & 3;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const int d = (4 * i + g) * kVec;
+      s[i] = u4_t{0u, 0u, 0u, 0u};
+      if (d < D) __builtin_memcpy(&s[i], p + d, 16);
+    }
+  }
+  typedef T vec8 __attribute__((ext_vector_type(8)));
+  static __device__ __forceinline__ f4_t products(const Vectors& k, const Vectors& q) {
+    f4_t c = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      if constexpr (std::is_same_v<T, bf16_t>) {
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(vec8, k.s[i]), __builtin_bit_cast(vec8, q.s[i]), c,
+                                                    0, 0, 0);
+      } else if constexpr (std::is_same_v<T, f16_t>) {
+        c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(vec8, k.s[i]), __builtin_bit_cast(vec8, q.s[i]), c,
+                                                   0, 0, 0);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k.s[i][e]), __uint_as_float(q.s[i][e]), c, 0, 0, 0);
+      }
+    }
+    return c;
+  }
+};
+
+// A wavefront's 32 keys: where they are, and their part of the sums.
+template <class T, int DP>
+struct KeyTile {
+  using V = Vectors<T, DP>;
+  int64_t where;   // lane i % 32: of key i
+  uint32_t lost;   // keys whose page is out of range
+  V key[2];
+  float sum[8];    // of keys 16 (i / 4) + 4 g + i % 4, this lane's queries
+
+  __device__ __forceinline__ void find(const WeightsArgs& a, int64_t seq, int64_t k0) {
+    const int64_t k = k0 + (threadIdx.x & 31);
+    int slot = 0, page = -1;
+    if (k < a.o.max_length) {
+      int pg;
+      if (a.page_shift >= 0) {
+        pg = static_cast<int>(k >> a.page_shift);
+        slot = static_cast<int>(k) & ((1 << a.page_shift) - 1);
+      } else {
+        pg = static_cast<int>(k) / a.c.page_size;
+        slot = static_cast<int>(k) - pg * a.c.page_size;
+      }
+      page = a.o.table[seq * a.o.table_width + pg];
+    }
+    const bool bad = page < 0 || page >= a.c.num_pages;
+    lost = static_cast<uint32_t>(__ballot(bad));
+    where = bad ? 0 : page * a.c.page_stride + slot * a.c.slot_stride;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = 0.f;
+  }
+  __device__ __forceinline__ void load(const WeightsArgs& a, int kv_head) {
+    const T* const k = static_cast<const T*>(a.c.k) + kv_head * a.c.head_stride;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) key[i].load(k + __shfl(where, 16 * i + (threadIdx.x & 15)), a.c.head_dim);
+  }
+};
+
+// 16 queries of a sequence and kv head: this lane's is number `at`.
+template <class T, int DP>
+struct QueryTile {
+  Vectors<T, DP> q;
+  float lse;
+  uint32_t bits;   // of the 32 keys from k0 on, those it sees
+  __device__ __forceinline__ void load(const WeightsArgs& a, int64_t seq, int kv_head, int64_t at, int64_t k0) {
+    const bool in = at < a.queries;
+    const int64_t n = in ? at : 0, row = seq * a.o.rows_per_seq + n / a.share;
+    const int head = kv_head * a.share + static_cast<int>(n % a.share);
+    q.load(static_cast<const T*>(a.o.q) + row * a.o.q_row_stride + head * a.o.q_head_stride, a.c.head_dim);
+    lse = a.o.lse[row * a.o.heads + head];
+    int64_t len = a.o.lengths[row];
+    if (len < 0 || len > a.o.max_length) {
+      if (a.info) *a.info = 1;
+      len = len < 0 ? 0 : a.o.max_length;
+    }
+    const int64_t left = len - k0;
+    bits = left <= 0 || !in || lse == -INFINITY ? 0u : left >= 32 ? ~0u : (1u << left) - 1u;
+    if (a.o.num_players > 0 && bits)
+      bits &= seen(a.o.masks + row * a.o.mask_words, k0 - a.o.first_player, a.o.num_players);
+  }
+};
+
+template <class T, int DP>
+__device__ __forceinline__ void add(const WeightsArgs& a, KeyTile<T, DP>& t, const QueryTile<T, DP>& q) {
+  if (q.bits & t.lost && a.info) *a.info = 1;
+  const uint32_t bits = (q.bits & ~t.lost) >> (4 * ((threadIdx.x >> 4) & 3));
+  if (!__ballot(bits)) return;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const f4_t c = Vectors<T, DP>::products(t.key[i], q.q);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      // the difference first: its rounding is that of a small number
+      const float p = __builtin_amdgcn_exp2f(fmaf(c[e], a.scale, -q.lse) * kLog2eF);
+      t.sum[4 * i + e] += bits >> (16 * i + e) & 1u ? p : 0.f;
+    }
+  }
+}
+
+// Adds up the 16 columns; all lanes get the sums of their keys.
+__device__ __forceinline__ void columns(float (&sum)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int off = 1; off < 16; off *= 2) sum[i] += __shfl_xor(sum[i], off);
+}
+
+// Few queries: a workgroup's wavefronts share 32 keys, each with its kv heads
+// (or, where there are fewer kv heads, have 32 keys of their own).
+template <class T, int DP>
+__global__ __launch_bounds__(256) void k_cache_weights(WeightsArgs a, int by_heads, unsigned tiles) {
+  __shared__ float sums[4][32];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  const int64_t seq = blockIdx.x / tiles;
+  const int own = wave % by_heads, tile = wave / by_heads;   // wavefront of the keys, which keys
+  const int64_t k0 = (static_cast<int64_t>(blockIdx.x % tiles) * (4 / by_heads) + tile) * 32;
+  KeyTile<T, DP> t;
+  t.find(a, seq, k0);
+  // a wavefront whose keys no row sees has nothing to read
+  bool any = false;
+  for (int64_t b = lane; b < a.o.rows_per_seq && !any; b += 64) any = a.o.lengths[seq * a.o.rows_per_seq + b] > k0;
+  if (__ballot(any)) {
+    for (int h = own; h < a.c.kv_heads; h += by_heads) {
+      t.load(a, h);
+      for (int64_t q0 = 0; q0 < a.queries; q0 += 16) {
+        QueryTile<T, DP> q;
+        q.load(a, seq, h, q0 + r, k0);
+        add(a, t, q);
+      }
+    }
+  }
+  columns(t.sum);
+  if (r == 0)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sums[wave][16 * (i / 4) + 4 * g + i % 4] = t.sum[i];
+  __syncthreads();
+  if (own == 0 && lane < 32 && k0 + lane < a.o.max_length) {
+    float s = 0.f;
+    for (int i = 0; i < by_heads; ++i) s += sums[wave + i][lane];
+    float* const w = a.o.weights + seq * a.o.weights_stride + k0 + lane;
+    if (s != 0.f) *w += s;
+  }
+}
+
+// Many queries: each wavefront of a workgroup has 32 keys of its own, all the same queries.
+template <class T, int DP>
+__global__ __launch_bounds__(256) void k_cache_weights_many(WeightsArgs a, unsigned tiles) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  unsigned b = blockIdx.x;
+  const int split = b % a.splits;
+  b /= a.splits;
+  const int kv_head = b % a.c.kv_heads;
+  b /= a.c.kv_heads;
+  const int64_t k0 = (static_cast<int64_t>(b % tiles) * 4 + wave) * 32, seq = b / tiles;
+  KeyTile<T, DP> t;
+  t.find(a, seq, k0);
+  t.load(a, kv_head);
+  const int64_t q0 = split * a.split * 16, q1 = q0 + a.split * 16 < a.queries ? q0 + a.split * 16 : a.queries;
+  if (q0 < q1) {
+    QueryTile<T, DP> now, next;
+    now.load(a, seq, kv_head, q0 + r, k0);
+#pragma unroll 1
+    for (int64_t q = q0; q < q1; q += 32) {
+      if (q + 16 < q1) next.load(a, seq, kv_head, q + 16 + r, k0);
+      add(a, t, now);
+      if (q + 32 < q1) now.load(a, seq, kv_head, q + 32 + r, k0);
+      if (q + 16 < q1) add(a, t, next);
+    }
+  }
+  columns(t.sum);
+  float* const part = a.part + ((seq * a.c.kv_heads + kv_head) * a.splits + split) * a.o.max_length;
+  if (r == 0)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t k = k0 + 16 * (i / 4) + 4 * g + i % 4;
+      if (k < a.o.max_length) part[k] = t.sum[i];
+    }
+}
+
+// Adds the parts up, a thread per token of a sequence.
+__global__ __launch_bounds__(256) void k_cache_weights_join(WeightsArgs a) {
+  __shared__ float sums[4][64];
+  const int64_t tiles = (a.o.max_length + 63) / 64, seq = blockIdx.x / tiles, k = blockIdx.x % tiles * 64 + (threadIdx.x & 63);
+  const int64_t parts = static_cast<int64_t>(a.c.kv_heads) * a.splits;
+  const int way = threadIdx.x >> 6;
+  float s = 0.f;
+  if (k < a.o.max_length) {
+    const float* const p = a.part + seq * parts * a.o.max_length + k;
+#pragma unroll 8
+    for (int64_t i = way; i < parts; i += 4) s += p[i * a.o.max_length];
+  }
+  sums[way][threadIdx.x & 63] = s;
+  __syncthreads();
+  if (way > 0 || k >= a.o.max_length) return;
+  for (int i = 1; i < 4; ++i) s += sums[i][threadIdx.x];
+  if (s != 0.f) a.o.weights[seq * a.o.weights_stride + k] += s;
+}
+
+int check_observed(const gnnshap_cache* c, const gnnshap_observed* o) {
+  if (const int st = check_cache(c)) return st;
+  if (!o || o->num_rows < 0) return fail(GNNSHAP_EINVAL, "observed queries: NULL or a negative number of rows");
+  if (o->heads < 1 || o->heads % c->kv_heads != 0)
+    return fail(GNNSHAP_EINVAL, "%d query heads over %d kv heads", static_cast<int>(o->heads),
+                static_cast<int>(c->kv_heads));
+  if (!(o->scale != 0.0) || !std::isfinite(static_cast<float>(o->scale * 1.4426950408889634074)))
+    return fail(GNNSHAP_EINVAL, "scale %g is 0 or not finite in fp32", o->scale);
+  if (o->num_rows > INT32_MAX || o->num_rows * o->heads > INT32_MAX)
+    return fail(GNNSHAP_EUNSUPPORTED, "%lld rows in one call", static_cast<long long>(o->num_rows));
+  if (o->rows_per_seq < 1 || o->num_rows % o->rows_per_seq != 0)
+    return fail(GNNSHAP_EINVAL, "sequences of %lld of %lld rows", static_cast<long long>(o->rows_per_seq),
+                static_cast<long long>(o->num_rows));
+  if (o->table_width < 0 || o->max_length < 0) return fail(GNNSHAP_EINVAL, "negative width or length");
+  if (o->max_length > (int64_t(1) << 30))
+    return fail(GNNSHAP_EUNSUPPORTED, "up to %lld tokens", static_cast<long long>(o->max_length));
+  if (ceil_div(o->max_length, c->page_size) > o->table_width)
+    return fail(GNNSHAP_EINVAL, "%lld tokens do not fit %lld pages of %d", static_cast<long long>(o->max_length),
+                static_cast<long long>(o->table_width), static_cast<int>(c->page_size));
+  if (o->num_players < 0 || o->num_players > INT32_MAX || o->first_player < 0 || o->first_player > INT32_MAX)
+    return fail(GNNSHAP_EINVAL, "%lld players from position %lld", static_cast<long long>(o->num_players),
+                static_cast<long long>(o->first_player));
+  if (o->num_players > 0 && (!o->masks || o->mask_words < ceil_div(o->num_players, 64)))
+    return fail(GNNSHAP_EINVAL, "%lld players without masks, or with %lld words", static_cast<long long>(o->num_players),
+                static_cast<long long>(o->mask_words));
+  if (o->weights_stride < 0) return fail(GNNSHAP_EINVAL, "negative stride of the weights");
+  return GNNSHAP_OK;
+}
+
+int64_t sequences(const WeightsArgs& a) { return a.o.num_rows / a.o.rows_per_seq; }
+int64_t key_tiles(const WeightsArgs& a, int keys) { return ceil_div(std::max<int64_t>(a.o.max_length, 1), keys); }
+
+int by_heads(const WeightsArgs& a) { return a.c.kv_heads >= 4 ? 4 : a.c.kv_heads >= 2 ? 2 : 1; }
+
+int lay_out(WeightsArgs& a, const gnnshap_cache* c, const gnnshap_observed* o) {
+  a.c = *c;
+  a.o = *o;
+  a.share = o->heads / c->kv_heads;
+  a.queries = o->rows_per_seq * a.share;
+  a.scale = static_cast<float>(o->scale);
+  a.page_shift = -1;
+  for (int i = 0; i < 31; ++i)
+    if (c->page_size == 1 << i) a.page_shift = i;
+  const int64_t seqs = sequences(a), tiles = ceil_div(a.queries, 16);
+  if (a.queries <= 64) return check_launch(seqs * key_tiles(a, 128 / by_heads(a)), 256);
+  const int64_t base = seqs * c->kv_heads * key_tiles(a, 128);
+  const int64_t want = std::max<int64_t>(1, std::min(1024 / std::max<int64_t>(base, 1), ceil_div(tiles, 8)));
+  a.split = ceil_div(tiles, want);
+  a.splits = static_cast<int>(ceil_div(tiles, a.split));
+  if (const int st = check_launch(base * a.splits, 256)) return st;
+  return check_launch(seqs * key_tiles(a, 64), 256);
+}
+
+size_t carve(WeightsArgs& a, void* ws) {
+  if (a.splits == 0) return 0;
+  Carver c(ws);
+  a.part = c.take<float>(static_cast<size_t>(sequences(a)) * a.c.kv_heads * a.splits * a.o.max_length);
+  return c.bytes();
+}
+
+template <class T, int DP>
+int launch(const WeightsArgs& a, hipStream_t s) {
+  if (a.splits == 0) {
+    const int64_t tiles = key_tiles(a, 128 / by_heads(a));
+    GS_TIMED("k_cache_weights", s);
+    k_cache_weights<T, DP><<<static_cast<unsigned>(sequences(a) * tiles), 256, 0, s>>>(a, by_heads(a),
+                                                                                       static_cast<unsigned>(tiles));
+    GS_LAUNCHED();
+    return GNNSHAP_OK;
+  }
+  const int64_t tiles = key_tiles(a, 128);
+  {
+    GS_TIMED("k_cache_weights_many", s);
+    k_cache_weights_many<T, DP><<<static_cast<unsigned>(sequences(a) * a.c.kv_heads * tiles * a.splits), 256, 0, s>>>(
+        a, static_cast<unsigned>(tiles));
+  }
+  GS_LAUNCHED();
+  {
+    GS_TIMED("k_cache_weights_join", s);
+    k_cache_weights_join<<<static_cast<unsigned>(sequences(a) * key_tiles(a, 64)), 256, 0, s>>>(a);
+  }
+  GS_LAUNCHED();
+  return GNNSHAP_OK;
+}
+
+}  // namespace
+
+extern "C" int gnnshap_cache_weights_workspace(const gnnshap_cache* cache, const gnnshap_observed* o, size_t* bytes) {
+  GS_TRY_BEGIN
+  clear_error();
+  if (!bytes) return fail(GNNSHAP_EINVAL, "bytes is NULL");
+  if (const int st = check_observed(cache, o)) return st;
+  WeightsArgs a{};
+  if (const int st = lay_out(a, cache, o)) return st;
+  *bytes = carve(a, nullptr);
+  return GNNSHAP_OK;
+  GS_TRY_END
+}
+
+extern "C" int gnnshap_cache_weights(const gnnshap_cache* cache, const gnnshap_observed* o, int32_t* info, void* ws,
+                                     size_t ws_bytes, void* stream) {
+  GS_TRY_BEGIN
+  clear_error();
+  if (const int st = check_observed(cache, o)) return st;
+  if (o->num_rows == 0 || o->max_length == 0) return GNNSHAP_OK;
+  if (!o->q || !o->lse || !o->table || !o->lengths || !o->weights)
+    return fail(GNNSHAP_EINVAL, "NULL q, lse, table, lengths or weights");
+  WeightsArgs a{};
+  if (const int st = lay_out(a, cache, o)) return st;
+  a.info = info;
+  const size_t need = carve(a, ws);
+  if (need > 0 && (!ws || ws_bytes < need))
+    return fail(GNNSHAP_ECAPACITY, "cache_weights workspace needs %zu bytes, has %zu", need, ws ? ws_bytes : 0);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return with_dtype(cache->dtype, [&](auto* p) {
+    using T = std::remove_pointer_t<decltype(p)>;
+    if (cache->head_dim <= 64) return launch<T, 64>(a, s);
+    if (cache->head_dim <= 128) return launch<T, 128>(a, s);
+    return launch<T, 256>(a, s);
+  });
+  GS_TRY_END
+}
