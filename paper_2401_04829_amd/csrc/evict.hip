@@ -18,6 +18,7 @@ using namespace gnnshap;
 constexpr int kSelect = 1024;  // threads that select
 constexpr int kSlots = 4;      // elements of a thread at a time, 64 apart
 constexpr int kBins = 2048;
+constexpr int kCopies = 4;     // of the bins, by lanes: what adds to one place waits for each other
 
 struct EvictArgs {
   gnnshap_cache c;
@@ -50,18 +51,44 @@ __device__ __forceinline__ int before(int x, int* room, int& all) {
   return base + up - x;
 }
 
+// A token's image, by which it stays or goes: the first and the last ones' above
+// all others, those behind the sequence below all (ordered() gives neither).
+struct Images {
+  int first, last, len;   // first <= place < last: the weight decides
+  __device__ __forceinline__ uint32_t operator()(float w, int at) const {
+    return at >= len ? 0u : at >= first && at < last ? ordered(w) : 0xFFFFFFFFu;
+  }
+};
+
+// The images of up to 4,096 HELD tokens stay in registers, so that memory is
+// waited for twice; HELD = 0: of any number, read for each digit and once more.
+// One workgroup's instructions bound it: 30,000 tokens, of which 4,000 stay,
+// 38 us when an image was found anew each time; 2,001 tokens 8.5 us.
+template <int HELD>
 __global__ __launch_bounds__(kSelect) void k_evict_select(EvictArgs a) {
-  __shared__ int bins[kBins], room[kSelect / 64], found[2], first_gap;
+  constexpr int kWaves = kSelect / 64, kBlocks = kWaves * (HELD ? HELD : 1);
+  constexpr int kTurn = kSelect * kSlots;   // tokens of a turn: a wavefront has kSlots times 64 on end
+  __shared__ int bins[kBins * kCopies], room[kWaves], found[2], first_gap;
+  __shared__ int block_sure[kBlocks], block_ties[kBlocks];
   const int64_t seq = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int keep = static_cast<int>(a.e.keep), first = static_cast<int>(a.e.first);
+  const int keep = static_cast<int>(a.e.keep);
+  const float* const w = a.e.weights + seq * a.e.weights_stride;
+  const auto place_in = [&](int turn, int s) { return turn * kTurn + (wave * kSlots + s) * 64 + lane; };
+  uint32_t held[HELD ? HELD : 1][kSlots];
+  if constexpr (HELD > 0) {  // before the length is known
+#pragma unroll
+    for (int j = 0; j < HELD; ++j)
+#pragma unroll
+      for (int s = 0; s < kSlots; ++s)
+        held[j][s] = place_in(j, s) < a.e.max_length ? __float_as_uint(w[place_in(j, s)]) : 0u;
+  }
   int len = a.e.lengths[seq];
   if (len < 0 || len > a.e.max_length) {
     if (tid == 0 && a.info) *a.info = 1;
     len = len < 0 ? 0 : static_cast<int>(a.e.max_length);
   }
   __syncthreads();  // (new_lengths may be lengths)
-  const float* const w = a.e.weights + seq * a.e.weights_stride;
   float* const out = a.e.new_weights + seq * a.e.new_weights_stride;
   int32_t* const kept = a.e.kept + seq * a.e.keep;
   const int now = len < keep ? len : keep;
@@ -72,91 +99,181 @@ __global__ __launch_bounds__(kSelect) void k_evict_select(EvictArgs a) {
     }
     if (tid == 0) a.begin[seq] = now;
   } else {
-    const int last = len - static_cast<int>(a.e.recent);   // first <= place < last: the weights decide
-    int want = keep - first - static_cast<int>(a.e.recent);
-    uint32_t low = 0xFFFFFFFFu;  // image of the last one that enters (none does if it stays so: images are below)
-    int ties = 0;                // of those with this image, so many enter
+    const Images image{static_cast<int>(a.e.first), len - static_cast<int>(a.e.recent), len};
+    if constexpr (HELD > 0) {
+#pragma unroll
+      for (int j = 0; j < HELD; ++j)
+#pragma unroll
+        for (int s = 0; s < kSlots; ++s) held[j][s] = image(__uint_as_float(held[j][s]), place_in(j, s));
+    }
+    // the lowest image that stays; of those with it, so many do as are not above it
+    uint32_t low = 0xFFFFFFFFu, mask = 0;
+    int ties = keep;
+    const int want = keep - static_cast<int>(a.e.first) - static_cast<int>(a.e.recent);
     if (want > 0) {
-      uint32_t prefix = 0, mask = 0;
+      low = 0;
+      ties = want;   // (the first and the last ones are not counted: many of one image wait for each other)
+    }
 #pragma unroll 1
-      for (int digit = 0; digit < 3; ++digit) {
-        const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bits = digit == 2 ? 10 : 11;
-        for (int i = tid; i < kBins; i += kSelect) bins[i] = 0;
-        __syncthreads();
+    for (int digit = 0; digit < 3 && want > 0; ++digit) {
+      const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bits = digit == 2 ? 10 : 11;
+      for (int i = tid; i < kBins * kCopies; i += kSelect) bins[i] = 0;
+      __syncthreads();
+      const auto count = [&](uint32_t x) {
+        if ((x & mask) == low && x - 1u < 0xFFFFFFFEu)
+          atomicAdd(&bins[__builtin_amdgcn_ubfe(x, shift, bits) * kCopies + lane % kCopies], 1);
+      };
+      if constexpr (HELD > 0) {
+#pragma unroll
+        for (int j = 0; j < HELD; ++j)
+          if (j * kTurn < len)
+#pragma unroll
+            for (int s = 0; s < kSlots; ++s) count(held[j][s]);
+      } else {
 #pragma unroll 4
-        for (int i = first + tid; i < last; i += kSelect) {
-          const uint32_t x = ordered(w[i]);
-          if ((x & mask) == prefix) atomicAdd(&bins[x >> shift & ((1u << bits) - 1u)], 1);
-        }
-        __syncthreads();
-        // from the highest bin down: two of a thread
-        const int hi = bins[kBins - 1 - 2 * tid], lo = bins[kBins - 2 - 2 * tid];
-        int all;
-        const int above = before(hi + lo, room, all);
-        if (above < want && want <= above + hi + lo) {
-          const bool in_hi = want <= above + hi;
-          found[0] = kBins - 1 - 2 * tid - (in_hi ? 0 : 1);
-          found[1] = in_hi ? above : above + hi;
-        }
-        __syncthreads();
-        prefix |= static_cast<uint32_t>(found[0]) << shift;
-        mask |= ((1u << bits) - 1u) << shift;
-        want -= found[1];
-        __syncthreads();
+        for (int i = tid; i < len; i += kSelect) count(image(w[i], i));
       }
-      low = prefix;
-      ties = want;
+      __syncthreads();
+      // from the highest bin down: two of a thread
+      int hi = 0, lo = 0, all;
+#pragma unroll
+      for (int i = 0; i < kCopies; ++i) {
+        hi += bins[(kBins - 1 - 2 * tid) * kCopies + i];
+        lo += bins[(kBins - 2 - 2 * tid) * kCopies + i];
+      }
+      const int above = before(hi + lo, room, all);
+      if (above < ties && ties <= above + hi + lo) {
+        const bool in_hi = ties <= above + hi;
+        found[0] = kBins - 1 - 2 * tid - (in_hi ? 0 : 1);
+        found[1] = in_hi ? above : above + hi;
+      }
+      __syncthreads();
+      low |= static_cast<uint32_t>(found[0]) << shift;
+      mask |= ((1u << bits) - 1u) << shift;
+      ties -= found[1];
+      __syncthreads();
     }
     if (tid == 0) first_gap = len;
-    __syncthreads();
-    int placed = 0, tied = 0;
-#pragma unroll 1
-    for (int base = 0; base < len; base += kSelect * kSlots) {
-      float x[kSlots];
-      bool sure[kSlots], tie[kSlots];
-      int at[kSlots], n_tie = 0, all;
+    const uint64_t under = (1ull << lane) - 1ull;
+    // Which of a turn's tokens stay (a bit per slot), behind `tied` ties, and their
+    // places in `kept` from `placed` on.
+    const auto choose = [&](const uint32_t (&x)[kSlots], int turn, int placed, int tied) {
+      uint32_t stays = 0;
 #pragma unroll
       for (int s = 0; s < kSlots; ++s) {
-        at[s] = base + (wave * kSlots + s) * 64 + lane;
-        x[s] = at[s] < len ? w[at[s]] : 0.f;
-        const uint32_t image = ordered(x[s]);
-        const bool middle = at[s] >= first && at[s] < last;
-        sure[s] = at[s] < len && (!middle || image > low);
-        tie[s] = middle && image == low;
-        n_tie += tie[s];
-      }
-      // ties in the order of their places: the wavefront's first, then by slots
-      const uint64_t under = (1ull << lane) - 1ull;
-      int ties_before = 0, mine = 0;
-      {
-        int total = 0;
-#pragma unroll
-        for (int s = 0; s < kSlots; ++s) total += __popcll(__ballot(tie[s]));
-        const int b = before(lane == 0 ? total : 0, room, all);
-        ties_before = tied + __shfl(b, 0);
-        tied += all;
-      }
-      uint64_t in[kSlots];
-#pragma unroll
-      for (int s = 0; s < kSlots; ++s) {
-        const uint64_t t = __ballot(tie[s]);
-        const bool enters = sure[s] || (tie[s] && ties_before + __popcll(t & under) < ties);
-        ties_before += __popcll(t);
-        in[s] = __ballot(enters);
-        mine += __popcll(in[s]);
-      }
-      int place = placed + __shfl(before(lane == 0 ? mine : 0, room, all), 0);
-      placed += all;
-#pragma unroll
-      for (int s = 0; s < kSlots; ++s) {
-        const int to = place + __popcll(in[s] & under);
-        if (in[s] >> lane & 1ull) {
-          kept[to] = at[s];
-          out[to] = x[s];   // (all of these places have been read)
-        } else if (at[s] < len && to == at[s]) {
+        const int at = place_in(turn, s);
+        const uint64_t tie = __ballot(x[s] == low);
+        const bool enters = x[s] > low || (x[s] == low && tied + __popcll(tie & under) < ties);
+        const uint64_t in = __ballot(enters);
+        const int to = placed + __popcll(in & under);
+        stays |= enters ? 1u << s : 0u;
+        if (enters)
+          kept[to] = at;
+        else if (to == at)   // (not behind the sequence, where there are fewer kept)
           atomicMin(&first_gap, to);
+        placed += __popcll(in);
+        tied += __popcll(tie);
+      }
+      return stays;
+    };
+    // Writes their weights, which have been read.
+    const auto write = [&](const uint32_t (&x)[kSlots], uint32_t stays, int placed) {
+#pragma unroll
+      for (int s = 0; s < kSlots; ++s) {
+        const uint64_t in = __ballot(stays >> s & 1u);
+        if (stays >> s & 1u) out[placed + __popcll(in & under)] = __uint_as_float(x[s]);
+        placed += __popcll(in);
+      }
+    };
+    const auto totals = [&](const uint32_t (&x)[kSlots], int& sure, int& tied) {
+      sure = tied = 0;
+#pragma unroll
+      for (int s = 0; s < kSlots; ++s) {
+        sure += __popcll(__ballot(x[s] > low));
+        tied += __popcll(__ballot(x[s] == low));
+      }
+    };
+    if constexpr (HELD > 0) {
+#pragma unroll
+      for (int j = 0; j < HELD; ++j) {
+        int sure, tied;
+        totals(held[j], sure, tied);
+        if (lane == 0) {
+          block_sure[j * kWaves + wave] = sure;
+          block_ties[j * kWaves + wave] = tied;
         }
-        place += __popcll(in[s]);
+      }
+      __syncthreads();
+      if (wave == 0) {  // of the blocks before each
+        constexpr int kEach = (kBlocks + 63) / 64;
+        int n_sure[kEach], n_ties[kEach], s = 0, t = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+          const int b = lane * kEach + i;
+          n_sure[i] = b < kBlocks ? block_sure[b] : 0;
+          n_ties[i] = b < kBlocks ? block_ties[b] : 0;
+          s += n_sure[i];
+          t += n_ties[i];
+        }
+        int up_s = s, up_t = t;
+#pragma unroll
+        for (int off = 1; off < 64; off *= 2) {
+          const int x = __shfl_up(up_s, off), y = __shfl_up(up_t, off);
+          if (lane >= off) {
+            up_s += x;
+            up_t += y;
+          }
+        }
+        s = up_s - s;
+        t = up_t - t;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+          const int b = lane * kEach + i;
+          if (b < kBlocks) {
+            block_sure[b] = s + min(t, ties);
+            block_ties[b] = t;
+          }
+          s += n_sure[i];
+          t += n_ties[i];
+        }
+      }
+      __syncthreads();
+      uint32_t stays[HELD];
+#pragma unroll
+      for (int j = 0; j < HELD; ++j) {
+        stays[j] = 0;
+        if (j * kTurn < len) {
+          stays[j] = choose(held[j], j, block_sure[j * kWaves + wave], block_ties[j * kWaves + wave]);
+#pragma unroll
+          for (int s = 0; s < kSlots; ++s)
+            if (stays[j] >> s & 1u) held[j][s] = __float_as_uint(w[place_in(j, s)]);
+        }
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();  // all are read: new_weights may be weights
+#pragma unroll
+      for (int j = 0; j < HELD; ++j)
+        if (j * kTurn < len) write(held[j], stays[j], block_sure[j * kWaves + wave]);
+    } else {
+      __syncthreads();
+      int placed = 0, tied = 0;   // in the turns before, `placed` without ties
+#pragma unroll 1
+      for (int turn = 0; turn * kTurn < len; ++turn) {
+        uint32_t x[kSlots], weight[kSlots];
+#pragma unroll
+        for (int s = 0; s < kSlots; ++s) {
+          weight[s] = place_in(turn, s) < len ? __float_as_uint(w[place_in(turn, s)]) : 0u;
+          x[s] = image(__uint_as_float(weight[s]), place_in(turn, s));
+        }
+        int n_sure, n_ties, all_sure, all_ties;
+        totals(x, n_sure, n_ties);
+        // (barriers: the turn is read before any of its places is written)
+        const int s = __shfl(before(lane == 0 ? n_sure : 0, room, all_sure), 0);
+        const int t = __shfl(before(lane == 0 ? n_ties : 0, room, all_ties), 0);
+        const int from = placed + s + min(tied + t, ties);
+        write(weight, choose(x, turn, from, tied + t), from);
+        placed += all_sure;
+        tied += all_ties;
       }
     }
     __syncthreads();
@@ -167,8 +284,8 @@ __global__ __launch_bounds__(kSelect) void k_evict_select(EvictArgs a) {
   for (int64_t i = now + tid; i < a.e.max_length; i += kSelect) out[i] = 0.f;
 }
 
-constexpr int kMove = 512;     // threads that move
-constexpr int kInFlight = 8;   // tokens of a thread
+constexpr int kMove = 1024;    // threads that move
+constexpr int kInFlight = 4;   // tokens of a thread
 
 // Where token i of a sequence is; -1 if its page is out of range.
 __device__ __forceinline__ int64_t place_of(const EvictArgs& a, int64_t seq, int i) {
@@ -192,8 +309,10 @@ __device__ __forceinline__ int64_t place_of(const EvictArgs& a, int64_t seq, int
 template <class T>
 __global__ __launch_bounds__(kMove) void k_evict_move(EvictArgs a) {
   unsigned b = blockIdx.x;
-  const int piece = b % a.pieces;
-  b /= a.pieces;
+  // slices of the same head mostly meet in one XCD, whose cache holds the lines that they share
+  const unsigned heads = gridDim.x / a.pieces;
+  const int piece = b / heads;
+  b -= piece * heads;
   const int head = b % a.c.kv_heads;
   b /= a.c.kv_heads;
   T* const pages = static_cast<T*>(b & 1 ? a.c.v : a.c.k);
@@ -303,7 +422,13 @@ extern "C" int gnnshap_cache_evict(const gnnshap_cache* cache, const gnnshap_evi
   hipStream_t s = static_cast<hipStream_t>(stream);
   {
     GS_TIMED("k_evict_select", s);
-    k_evict_select<<<static_cast<unsigned>(e->num_seqs), kSelect, 0, s>>>(a);
+    const unsigned grid = static_cast<unsigned>(e->num_seqs);
+    if (e->max_length <= 4096)
+      k_evict_select<1><<<grid, kSelect, 0, s>>>(a);
+    else if (e->max_length <= 8 * 4096)
+      k_evict_select<8><<<grid, kSelect, 0, s>>>(a);
+    else
+      k_evict_select<0><<<grid, kSelect, 0, s>>>(a);
   }
   GS_LAUNCHED();
   return with_dtype(cache->dtype, [&](auto* p) {

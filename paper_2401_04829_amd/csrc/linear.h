@@ -28,27 +28,95 @@ struct LinearArgs {
   int64_t v0, piece;          // the piece of the vocabulary
 };
 
-// The product of logits: a tile's rows are tokens, its columns hidden states'
-// rows, so that a lane has tokens on end.  256 x 256 for many rows; where they
-// are fewer the weights' rows are read once, and a workgroup takes fewer of
-// them so that all compute units have some.
-template <class T, bool DIRECT>
-using LogitsMany = Product<T, 8, 4, 2, 4, 64, 4, false, false, DIRECT>;
-template <class T, bool DIRECT>
-using LogitsSome = Product<T, 4, 2, 2, 2, 128, 3, false, false, DIRECT>;
-template <class T, bool DIRECT>
-using LogitsFew = Product<T, 1, 1, 4, 1, 128, 4, false, false, DIRECT>;
-
-// Calls f with the product for `rows` rows.
-template <class T, class F>
-inline int with_logits(int64_t rows, bool direct, F f) {
-  const auto pick = [&](auto d) {
-    constexpr bool D = decltype(d)::value;
-    if (rows <= 16) return f(static_cast<LogitsFew<T, D>*>(nullptr));
-    if (rows <= 128) return f(static_cast<LogitsSome<T, D>*>(nullptr));
-    return f(static_cast<LogitsMany<T, D>*>(nullptr));
+// The shapes of a product's tiles, from the largest on.  A large one reads less
+// per product, a small one gives more compute units work.
+template <class T, int SHAPE, bool A_TURNED, bool B_TURNED, bool DIRECT>
+struct ShapeOf;
+#define GS_SHAPE(N, ...)                                              \
+  template <class T, bool A_TURNED, bool B_TURNED, bool DIRECT>       \
+  struct ShapeOf<T, N, A_TURNED, B_TURNED, DIRECT> {                  \
+    using P = Product<T, __VA_ARGS__, A_TURNED, B_TURNED, DIRECT>;    \
   };
-  return direct ? pick(std::true_type()) : pick(std::false_type());
+GS_SHAPE(0, 8, 4, 2, 4, 128, 2)  // 256 x 256
+GS_SHAPE(1, 4, 4, 2, 2, 128, 2)  // 128 x 128
+GS_SHAPE(2, 4, 2, 2, 2, 128, 3)  // 128 x 64
+GS_SHAPE(3, 2, 2, 2, 2, 128, 4)  // 64 x 64
+GS_SHAPE(4, 2, 1, 2, 2, 128, 4)  // 64 x 32
+GS_SHAPE(5, 1, 1, 4, 1, 128, 4)  // 64 x 16
+#undef GS_SHAPE
+constexpr int kShapes = 6;
+constexpr int kTileM[kShapes] = {256, 128, 128, 64, 64, 64}, kTileN[kShapes] = {256, 128, 64, 64, 32, 16};
+
+// The time of a tile's chunk (128 bytes of K) in us: of one workgroup alone,
+// and of one of very many times a 256th (the chip's), in 16 and in 32 bits.
+// Measured with the logits' kernel: bf16, 10,000 x 32,768 x 2,048: 1,162 us at
+// 256 x 256, 1,331 at 128 x 128; 300 x 5,000 x 2,048: 65, 31, 25 (128 x 64), 21
+// (64 x 64); 1,534 x 3 x 1,304: 46, 24, 20, 15, 12.5 (64 x 16); fp32, 2,000 x
+// 32,768 x 1,024: 999 and 1,055; 1,534 x 3 x 1,304: 325, 97, 59, 37, 22.
+struct Pace {
+  float alone, full;
+};
+constexpr Pace kPace[2][kShapes] = {{{1.7f, 1.8f}, {.71f, .53f}, {.53f, .42f}, {.34f, .33f}, {.28f, .29f}, {.21f, .26f}},
+                                    {{7.7f, 8.0f}, {2.2f, 2.1f}, {1.25f, 1.3f}, {.65f, .68f}, {.48f, .42f}, {.34f, .24f}}};
+// Time of a chunk of `tiles` tiles that read `rows` rows of A.
+inline float pace(int shape, bool wide, int64_t tiles, int64_t rows) {
+  const Pace& p = kPace[wide][shape];
+  // one workgroup of the largest shape fills a compute unit: rounds are whole
+  const float rounds = shape == 0 ? static_cast<float>(ceil_div(tiles, 256)) : static_cast<float>(tiles) / 256.f;
+  // A, the larger operand, comes from memory at 5.2 TB/s at most
+  return std::max({p.alone, p.full * rounds, static_cast<float>(rows) * 128.f / 5.2e6f});
+}
+
+// The fastest of the shapes in `which` (bits) for M x N; of equally fast ones
+// (bound by memory) the smallest, of which more are resident (one row of 131,072
+// x 2,048 in bf16: 64 x 16 102 us, 128 x 64 117).
+inline int shape_for(int64_t M, int64_t N, bool wide, unsigned which) {
+  int best = -1;
+  float least = 0.f;
+  for (int i = 0; i < kShapes; ++i) {
+    if (!(which >> i & 1u)) continue;
+    const float t = pace(i, wide, ceil_div(M, kTileM[i]) * ceil_div(std::max<int64_t>(N, 1), kTileN[i]), M);
+    if (best < 0 || t <= least) {
+      best = i;
+      least = t;
+    }
+  }
+  return best;
+}
+
+// Calls f with a null pointer of the product of a shape; of operands that have
+// to go through registers there are fewer shapes.
+constexpr unsigned kThroughRegisters = 1u << 1 | 1u << 3 | 1u << 5;
+template <class T, bool A_TURNED, bool B_TURNED, unsigned WHICH, class F>
+inline int with_shape(int shape, bool direct, F f) {
+#define GS_CASE(N, D) f(static_cast<typename ShapeOf<T, N, A_TURNED, B_TURNED, D>::P*>(nullptr))
+#define GS_SHAPE(N)                                                     \
+  case N:                                                               \
+    if constexpr ((WHICH >> N & 1u) != 0) {                             \
+      if (direct) return GS_CASE(N, true);                              \
+      if constexpr ((kThroughRegisters >> N & 1u) != 0) return GS_CASE(N, false); \
+    }                                                                   \
+    break;
+  switch (shape) {
+    GS_SHAPE(0)
+    GS_SHAPE(1)
+    GS_SHAPE(2)
+    GS_SHAPE(3)
+    GS_SHAPE(4)
+    GS_SHAPE(5)
+  }
+#undef GS_SHAPE
+#undef GS_CASE
+  return fail(GNNSHAP_EUNSUPPORTED, "no product of shape %d", shape);
+}
+
+// The logits' product: a tile's rows are tokens, its columns hidden states'
+// rows, so that a lane has tokens on end.
+constexpr unsigned kLogitShapes = 0x2F;  // (64 x 32 is no faster than its neighbours)
+template <class T, class F>
+inline int with_logits(int64_t tokens, int64_t rows, bool direct, F f) {
+  const int shape = shape_for(tokens, rows, sizeof(T) == 4, direct ? kLogitShapes : kLogitShapes & kThroughRegisters);
+  return with_shape<T, false, false, kLogitShapes>(shape, direct, f);
 }
 
 template <class T>

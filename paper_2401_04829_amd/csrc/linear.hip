@@ -163,13 +163,18 @@ extern "C" int gnnshap_linear_logprobs_workspace(const gnnshap_linear* l, size_t
   if (l->num_rows == 0) return GNNSHAP_OK;
   return with_dtype(l->dtype, [&](auto* x) {
     using T = std::remove_pointer_t<decltype(x)>;
-    return with_logits<T>(l->num_rows, true, [&](auto* p) {
-      LinearArgs a{};
-      a.l = *l;
-      if (const int st = lay_out<std::remove_pointer_t<decltype(p)>>(a)) return st;
-      *bytes = carve(a, nullptr);
-      return static_cast<int>(GNNSHAP_OK);
-    });
+    int st = GNNSHAP_OK;
+    for (const bool direct : {true, false}) {  // as the call's addresses will have it
+      if (st) break;
+      st = with_logits<T>(l->vocab, l->num_rows, direct, [&](auto* p) {
+        LinearArgs a{};
+        a.l = *l;
+        if (const int refused = lay_out<std::remove_pointer_t<decltype(p)>>(a)) return refused;
+        *bytes = std::max(*bytes, carve(a, nullptr));
+        return static_cast<int>(GNNSHAP_OK);
+      });
+    }
+    return st;
   });
   GS_TRY_END
 }
@@ -183,7 +188,7 @@ extern "C" int gnnshap_linear_logprobs(const gnnshap_linear* l, int32_t* info, v
   if (!l->hidden || !l->weight) return fail(GNNSHAP_EINVAL, "NULL hidden states or weights");
   return with_dtype(l->dtype, [&](auto* x) {
     using T = std::remove_pointer_t<decltype(x)>;
-    return with_logits<T>(l->num_rows, direct_logits<T>(*l), [&](auto* p) {
+    return with_logits<T>(l->vocab, l->num_rows, direct_logits<T>(*l), [&](auto* p) {
       using P = std::remove_pointer_t<decltype(p)>;
       LinearArgs a{};
       a.l = *l;

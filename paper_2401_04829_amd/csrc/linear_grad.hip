@@ -40,40 +40,39 @@ __global__ __launch_bounds__(P::kThreads) void k_linear_d(LinearArgs a) {
   const float scale = a.scale ? a.scale[0] : 1.f;
 #pragma unroll
   for (int t = 0; t < P::NT; ++t) {
-    const int64_t row = b0 + p.col_of(t);
-    if (row >= a.l.num_rows) continue;
-    int64_t given = a.l.targets ? a.l.targets[row] : -1;
+    const int64_t row = b0 + p.col_of(t), b = row < a.l.num_rows ? row : 0;
+    int64_t given = a.l.targets ? a.l.targets[b] : -1;
     if (given >= a.l.vocab) {
       if (a.info) *a.info = 1;
       given = -1;
     }
-    const float top = a.l.maximum[row], logs = a.l.log_sum[row];
-    const float gl = a.gl && given >= 0 ? a.gl[row] : 0.f;
-    const float ge = a.ge ? a.ge[row] : 0.f, ent = a.ge ? a.l.entropy[row] : 0.f;
+    const float top = a.l.maximum[b], logs = a.l.log_sum[b];
+    const float gl = a.gl && given >= 0 ? a.gl[b] : 0.f;
+    const float ge = a.ge ? a.ge[b] : 0.f, ent = a.ge ? a.l.entropy[b] : 0.f;
     const bool none = top == -INFINITY && logs == 0.f;
     given -= a.v0 + v0;
-    T* const out = static_cast<T*>(a.d) + row * a.pitch + v0;
+    float d[P::kRuns][P::kRun];
 #pragma unroll
-    for (int j = 0; j < P::kRuns; ++j) {
-      constexpr int kPack = P::kRun < 16 / static_cast<int>(sizeof(T)) ? P::kRun : 16 / static_cast<int>(sizeof(T));
+    for (int j = 0; j < P::kRuns; ++j)
 #pragma unroll
-      for (int i0 = 0; i0 < P::kRun; i0 += kPack) {
-        Pack<T, kPack> hi, lo;
-#pragma unroll
-        for (int i = 0; i < kPack; ++i) {
-          const int at = p.run_of(j) + i0 + i;
-          const float logp = (p.at(j, i0 + i, t) - top) - logs, e = __builtin_amdgcn_exp2f(logp * kLog2e);
-          const float own = at == given ? gl : 0.f;
-          float d = own - e * (gl + ge * ((e == 0.f ? 0.f : logp) + ent));
-          if (none || v0 + at >= a.piece) d = 0.f;  // behind the piece: the products read it
-          d *= scale;
-          hi.v[i] = static_cast<T>(d);
-          lo.v[i] = static_cast<T>(d - static_cast<float>(hi.v[i]));
-        }
-        store_pack(out + p.run_of(j) + i0, hi);
-        if (a.two) store_pack(out + a.l.num_rows * a.pitch + p.run_of(j) + i0, lo);
+      for (int i = 0; i < P::kRun; ++i) {
+        const int at = p.run_of(j) + i;
+        const float logp = (p.at(j, i, t) - top) - logs, e = __builtin_amdgcn_exp2f(logp * kLog2e);
+        const float own = at == given ? gl : 0.f;
+        d[j][i] = own - e * (gl + ge * ((e == 0.f ? 0.f : logp) + ent));
+        if (none || v0 + at >= a.piece) d[j][i] = 0.f;  // behind the piece: the products read it
+        d[j][i] *= scale;
       }
-    }
+    T* const out = static_cast<T*>(a.d) + v0;
+    p.template rows_out<T>(lds, t, [&](int j, int i) { return static_cast<T>(d[j][i]); }, [&](int n, int m, const auto& x) {
+      if (b0 + n < a.l.num_rows) store_pack(out + (b0 + n) * a.pitch + m, x);
+    });
+    if (a.two)
+      p.template rows_out<T>(
+          lds, t, [&](int j, int i) { return static_cast<T>(d[j][i] - static_cast<float>(static_cast<T>(d[j][i]))); },
+          [&](int n, int m, const auto& x) {
+            if (b0 + n < a.l.num_rows) store_pack(out + (a.l.num_rows + b0 + n) * a.pitch + m, x);
+          });
   }
 }
 
@@ -102,33 +101,26 @@ __global__ __launch_bounds__(P::kThreads) void k_linear_dh(HiddenArgs a) {
   p.run(lds, Operand{static_cast<const T*>(a.weight) + k0 * a.weight_stride, a.weight_stride, a.width},
         Operand{static_cast<const T*>(a.d) + k0, a.pitch, a.rows}, m0, n0, K > 0 ? K : 0);
 #pragma unroll
-  for (int t = 0; t < P::NT; ++t) {
-    const int64_t row = n0 + p.col_of(t);
-    if (row >= a.rows) continue;
+  for (int t = 0; t < P::NT; ++t)
+    p.template rows_out<float>(lds, t, [&](int j, int i) { return p.at(j, i, t); }, [&](int n, int m, const auto& x) {
+      const int64_t row = n0 + n, at = m0 + m;
+      if (row >= a.rows || at >= a.width) return;
+      float* const out = a.sums + (part * a.rows + row) * a.width + at;
+      const int there = a.width - at < 4 ? static_cast<int>(a.width - at) : 4;
+      if (there == 4) {
+        Pack<float, 4> y = x;
+        if (!a.first) {
+          const Pack<float, 4> z = load_pack<float, 4>(out);
 #pragma unroll
-    for (int j = 0; j < P::kRuns; ++j) {
-      const int64_t m = m0 + p.run_of(j);
-      float* const out = a.sums + (part * a.rows + row) * a.width + m;
-#pragma unroll
-      for (int i = 0; i < P::kRun; i += 4) {
-        Pack<float, 4> x;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x.v[e] = p.at(j, i + e, t);
-        if (m + i + 4 <= a.width) {
-          if (!a.first) {
-            const Pack<float, 4> y = load_pack<float, 4>(out + i);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x.v[e] += y.v[e];
-          }
-          store_pack(out + i, x);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (m + i + e < a.width) out[i + e] = a.first ? x.v[e] : x.v[e] + out[i + e];
+          for (int e = 0; e < 4; ++e) y.v[e] += z.v[e];
         }
+        store_pack(out, y);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e < there) out[e] = a.first ? x.v[e] : x.v[e] + out[e];
       }
-    }
-  }
+    });
 }
 
 struct JoinArgs {
@@ -200,29 +192,22 @@ __global__ __launch_bounds__(P::kThreads) void k_linear_dw(WeightArgs a) {
         0, a.rows * a.pitch * static_cast<int64_t>(sizeof(T)));
   const float over = a.scale ? a.scale[1] : 1.f;
   constexpr int kPack = 16 / sizeof(T);
+  static_assert(P::kRun >= kPack, "a lane's run is whole packs");
 #pragma unroll
-  for (int t = 0; t < P::NT; ++t) {
-    const int64_t token = n0 + p.col_of(t);
-    if (token >= a.piece) continue;
+  for (int t = 0; t < P::NT; ++t)
+    p.template rows_out<T>(lds, t, [&](int j, int i) { return static_cast<T>(p.at(j, i, t) * over); },
+                           [&](int n, int m, const auto& x) {
+                             const int64_t token = n0 + n, at = m0 + m;
+                             if (token >= a.piece || at >= a.width) return;
+                             T* const out = static_cast<T*>(a.out) + token * a.stride + at;
+                             if (at + kPack <= a.width) {
+                               store_pack(out, x);
+                             } else {
 #pragma unroll
-    for (int j = 0; j < P::kRuns; ++j) {
-      const int64_t m = m0 + p.run_of(j);
-      T* const out = static_cast<T*>(a.out) + token * a.stride + m;
-#pragma unroll
-      for (int i = 0; i < P::kRun; i += kPack) {
-        Pack<T, kPack> x;
-#pragma unroll
-        for (int e = 0; e < kPack; ++e) x.v[e] = static_cast<T>(p.at(j, i + e, t) * over);
-        if (m + i + kPack <= a.width) {
-          store_pack(out + i, x);
-        } else {
-#pragma unroll
-          for (int e = 0; e < kPack; ++e)
-            if (m + i + e < a.width) out[i + e] = x.v[e];
-        }
-      }
-    }
-  }
+                               for (int e = 0; e < kPack; ++e)
+                                 if (at + e < a.width) out[e] = x.v[e];
+                             }
+                           });
 }
 
 // The power of two that d is carried larger by, and one over it: |d| is at most
@@ -247,33 +232,49 @@ __global__ __launch_bounds__(1024) void k_linear_scale(LinearArgs a, float* scal
   scale[1] = ldexpf(1.f, -k);
 }
 
-template <class T, bool DIRECT>
-using HiddenMany = Product<T, 8, 4, 2, 4, 64, 4, true, false, DIRECT>;
-template <class T, bool DIRECT>
-using HiddenSome = Product<T, 4, 4, 4, 1, 64, 4, true, false, DIRECT>;
-template <class T, bool DIRECT>
-using HiddenFew = Product<T, 4, 2, 4, 1, 64, 4, true, false, DIRECT>;
-template <class T, bool DIRECT>
-using Weights = Product<T, 8, 4, 2, 4, 64, 4, true, true, DIRECT>;
+// dh's product: a tile's rows are elements of the width, its columns rows of d.
+constexpr unsigned kHiddenShapes = 0x1B;   // all but 128 x 64 and those whose A would be read element by element
+// dw's: the width by tokens.
+constexpr unsigned kWeightShapes = 0x0F;
 
-template <class T, class F>
-int with_hidden(int64_t rows, bool direct, F f) {
-  const auto pick = [&](auto d) {
-    constexpr bool D = decltype(d)::value;
-    if (rows <= 32) return f(static_cast<HiddenFew<T, D>*>(nullptr));
-    if (rows <= 256) return f(static_cast<HiddenSome<T, D>*>(nullptr));
-    return f(static_cast<HiddenMany<T, D>*>(nullptr));
-  };
-  return direct ? pick(std::true_type()) : pick(std::false_type());
-}
-template <class T, class F>
-int with_weights(bool direct, F f) {
-  return direct ? f(static_cast<Weights<T, true>*>(nullptr)) : f(static_cast<Weights<T, false>*>(nullptr));
+// How dh's product is laid out: its shape and how many workgroups take parts of
+// the vocabulary.  Each part is a sum more to write and to read.
+struct Split {
+  int shape;
+  int64_t parts;
+};
+Split hidden_split(const gnnshap_linear& l, int64_t rows, int64_t piece, unsigned shapes) {
+  const bool wide = l.dtype == GNNSHAP_F32;
+  Split best{-1, 1};
+  float least = 0.f;
+  for (int i = 0; i < kShapes; ++i) {
+    if (!(shapes >> i & 1u)) continue;
+    const int64_t tiles = ceil_div(l.width, kTileM[i]) * ceil_div(rows, kTileN[i]);
+    for (int64_t parts = 1; parts <= 64; parts *= 2) {
+      if (parts > 1 && piece / parts < 256) break;
+      const int64_t chunks = ceil_div(ceil_div(piece, parts), wide ? 32 : 64);
+      // a part's sum: written and read, 8 bytes an element, at 3 TB/s
+      const float t = pace(i, wide, tiles * parts, l.width * parts) * static_cast<float>(chunks) +
+                      static_cast<float>(parts * rows * l.width) * 8.f / 3e6f;
+      if (best.shape < 0 || t < least) {
+        best = Split{i, parts};
+        least = t;
+      }
+    }
+  }
+  return best;
 }
 
-// How the backward pass is laid out; all of it goes by the sizes alone.
+// The weights turned over: their packs lie along the width.
+template <class T>
+bool direct_weight(const gnnshap_linear& l) {
+  return direct_operand<T>(l.weight, l.weight_stride, l.width, 256);
+}
+
+// How the backward pass is laid out.
 struct Layout {
   bool two;
+  int hidden_shape;
   int64_t d_rows, piece, pitch, split, parts;
   float* scale;
   void* d;
@@ -281,7 +282,7 @@ struct Layout {
 };
 
 template <class T>
-Layout lay_out(const gnnshap_linear& l) {
+Layout lay_out(const gnnshap_linear& l, bool direct) {
   Layout y{};
   y.two = sizeof(T) == 2 && l.num_rows <= kTwoParts;
   y.d_rows = y.two ? 2 * l.num_rows : l.num_rows;
@@ -290,15 +291,11 @@ Layout lay_out(const gnnshap_linear& l) {
   const int64_t pieces = ceil_div(l.vocab, most);
   y.piece = ceil_div(ceil_div(l.vocab, pieces), 256) * 256;
   y.pitch = y.piece;
-  // enough workgroups for the chip, each with 512 tokens at least
-  with_hidden<T>(y.d_rows, true, [&](auto* p) {
-    using P = std::remove_pointer_t<decltype(p)>;
-    const int64_t tiles = ceil_div(l.width, P::TM) * ceil_div(std::max<int64_t>(y.d_rows, 1), P::TN);
-    const int64_t want = std::max<int64_t>(1, (P::TN >= 256 ? 256 : 512) / tiles);
-    y.split = std::max<int64_t>(ceil_div(ceil_div(y.piece, want), 64) * 64, 512);
-    y.parts = ceil_div(y.piece, y.split);
-    return 0;
-  });
+  const Split h = hidden_split(l, std::max<int64_t>(y.d_rows, 1), std::min(y.piece, l.vocab),
+                               direct ? kHiddenShapes : kHiddenShapes & kThroughRegisters);
+  y.hidden_shape = h.shape;
+  y.split = ceil_div(ceil_div(y.piece, h.parts), 64) * 64;
+  y.parts = ceil_div(y.piece, y.split);
   return y;
 }
 
@@ -340,13 +337,13 @@ int run(const LinearArgs& given, void* grad_hidden, int64_t gh_stride, void* gra
   a.two = y.two;
   const bool direct_logits_too = direct_logits<T>(l);
   // turned over, packs lie along the width
-  const bool direct_w = direct_operand<T>(l.weight, l.weight_stride, l.width, 256);
+  const bool direct_w = direct_weight<T>(l);
   const bool direct_h = direct_operand<T>(l.hidden, l.hidden_stride, l.width, 256);
   for (int64_t v0 = 0; v0 < l.vocab; v0 += y.piece) {
     const int64_t piece = std::min(y.piece, l.vocab - v0);
     int st = GNNSHAP_OK;
     if (l.num_rows > 0) {
-      st = with_logits<T>(l.num_rows, direct_logits_too, [&](auto* p) {
+      st = with_logits<T>(piece, l.num_rows, direct_logits_too, [&](auto* p) {
         using P = std::remove_pointer_t<decltype(p)>;
         a.v0 = v0;
         a.piece = piece;
@@ -357,7 +354,7 @@ int run(const LinearArgs& given, void* grad_hidden, int64_t gh_stride, void* gra
       if (st) return st;
     }
     if (grad_hidden && l.num_rows > 0) {
-      st = with_hidden<T>(y.d_rows, direct_w, [&](auto* p) {
+      st = with_shape<T, true, false, kHiddenShapes>(y.hidden_shape, direct_w, [&](auto* p) {
         using P = std::remove_pointer_t<decltype(p)>;
         HiddenArgs h{static_cast<const T*>(l.weight) + v0 * l.weight_stride, l.weight_stride, y.d, y.pitch, piece, y.d_rows,
                      l.width, static_cast<unsigned>(ceil_div(l.width, P::TM)),
@@ -367,7 +364,9 @@ int run(const LinearArgs& given, void* grad_hidden, int64_t gh_stride, void* gra
       if (st) return st;
     }
     if (grad_weight) {
-      st = with_weights<T>(direct_h, [&](auto* p) {
+      const int shape = shape_for(l.width, piece, sizeof(T) == 4,
+                                  direct_h ? kWeightShapes : kWeightShapes & kThroughRegisters);
+      st = with_shape<T, true, true, kWeightShapes>(shape, direct_h, [&](auto* p) {
         using P = std::remove_pointer_t<decltype(p)>;
         WeightArgs w{l.hidden, l.hidden_stride, y.d, y.pitch, piece, l.num_rows, l.width, y.two,
                      static_cast<unsigned>(ceil_div(l.width, P::TM)), static_cast<unsigned>(ceil_div(piece, P::TN)),
@@ -398,8 +397,11 @@ extern "C" int gnnshap_linear_logprobs_backward_workspace(const gnnshap_linear* 
   if (!bytes) return fail(GNNSHAP_EINVAL, "bytes is NULL");
   if (const int st = check_linear(l)) return st;
   return with_dtype(l->dtype, [&](auto* x) {
-    Layout y = lay_out<std::remove_pointer_t<decltype(x)>>(*l);
-    *bytes = carve(y, *l, nullptr);
+    *bytes = 0;
+    for (const bool direct : {true, false}) {  // as the call's addresses will have it
+      Layout y = lay_out<std::remove_pointer_t<decltype(x)>>(*l, direct);
+      *bytes = std::max(*bytes, carve(y, *l, nullptr));
+    }
     return static_cast<int>(GNNSHAP_OK);
   });
   GS_TRY_END
@@ -424,7 +426,7 @@ extern "C" int gnnshap_linear_logprobs_backward(const gnnshap_linear* l, const f
   a.info = info;
   return with_dtype(l->dtype, [&](auto* x) {
     using T = std::remove_pointer_t<decltype(x)>;
-    Layout y = lay_out<T>(*l);
+    Layout y = lay_out<T>(*l, direct_weight<T>(*l));
     const size_t need = carve(y, *l, ws);
     if (!ws || ws_bytes < need)
       return fail(GNNSHAP_ECAPACITY, "linear_logprobs_backward workspace needs %zu bytes, has %zu", need,

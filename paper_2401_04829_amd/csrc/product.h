@@ -268,6 +268,7 @@ struct Product {
         x[i] = *reinterpret_cast<const u4_t*>(part + row * KB + (((4 * step + g) ^ swapped(row)) << 4));
       }
     } else if constexpr (sizeof(T) == 2) {
+      static_assert(OWN % 2 == 0, "elements are swapped in pairs");
 #pragma unroll
       for (int j = 0; j < TILES / OWN; ++j) {
         unsigned v[8][OWN / 2];
@@ -321,6 +322,43 @@ struct Product {
     return wave_n() + 16 * kOwnB * (t / kOwnB) + kOwnB * (threadIdx.x & 15) + t % kOwnB;
   }
   __device__ __forceinline__ float at(int j, int i, int t) const { return acc[j * kOwnA + i % kOwnA][t][i / kOwnA]; }
+
+  // The tile's columns t of the wavefront, 16 rows of C^T of 16 MT elements of
+  // type O each, by way of LDS so that 16 bytes a lane lie on end in memory
+  // (straight from the registers they would be 64 or more apart): value(j, i)
+  // gives the element, store(n, m, pack) takes 16 / sizeof(O) of them from row m
+  // of A on for row n of B.  Call it behind run(); lds as there.
+  template <class O, class V, class F>
+  __device__ __forceinline__ void rows_out(char* lds, int t, V value, F store) const {
+    constexpr int kPack = kRun * static_cast<int>(sizeof(O)) < 16 ? kRun : 16 / static_cast<int>(sizeof(O));
+    constexpr int kPieces = 16 * MT / kPack, kBytes = kPack * static_cast<int>(sizeof(O));
+    static_assert(kWaves * 16 * 16 * MT * static_cast<int>(sizeof(O)) <= kLds, "a wavefront's rows fit");
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    char* const room = lds + wave * (16 * kPieces * kBytes);
+    const auto at_piece = [&](int row, int piece) {
+      return room + (row * kPieces + (piece ^ (kPieces >= 16 ? row & 15 : row & (kPieces - 1)))) * kBytes;
+    };
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int j = 0; j < kRuns; ++j)
+#pragma unroll
+      for (int i = 0; i < kRun; i += kPack) {
+        Pack<O, kPack> x;
+#pragma unroll
+        for (int e = 0; e < kPack; ++e) x.v[e] = value(j, i + e);
+        __builtin_memcpy(__builtin_assume_aligned(at_piece(r, (16 * kOwnA * j + 4 * kOwnA * g + i) / kPack), kBytes), &x,
+                         kBytes);
+      }
+    __builtin_amdgcn_wave_barrier();
+    const int first = wave_n() + 16 * kOwnB * (t / kOwnB) + t % kOwnB;
+#pragma unroll
+    for (int at = 0; at < 16 * kPieces; at += 64) {
+      const int row = (at + lane) / kPieces, piece = (at + lane) % kPieces;
+      Pack<O, kPack> x;
+      __builtin_memcpy(&x, __builtin_assume_aligned(at_piece(row, piece), kBytes), kBytes);
+      store(first + kOwnB * row, wave_m() + piece * kPack, x);
+    }
+  }
 };
 
 // Whether a product's direct loads can take an operand: whole aligned packs, offsets within 2^31 bytes.
