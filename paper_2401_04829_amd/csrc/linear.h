@@ -15,8 +15,9 @@ constexpr int64_t kTwoParts = 128;
 struct LinearArgs {
   gnnshap_linear l;
   int32_t* info;
-  unsigned tiles_m, tiles_n;  // of the vocabulary (or piece), of the rows
+  unsigned tiles_m, tiles_n;  // of the segment of the vocabulary, of the rows
   Stats* parts;               // [row][tile of the vocabulary]
+  unsigned part0, row_parts;  // the segment's first part of a row's, and all of them
   float* given;               // [row] logit of the given token
   // the gradient's
   const float* gl;
@@ -25,7 +26,8 @@ struct LinearArgs {
   void* d;                    // [row, then what rounding left of row][pitch]
   int64_t pitch;
   bool two;                   // d in two parts
-  int64_t v0, piece;          // the piece of the vocabulary
+  int64_t v0, tokens;         // the segment: its first token and how many
+  int64_t d0;                 // the segment's first column of d
 };
 
 // The shapes of a product's tiles, from the largest on.  A large one reads less
@@ -84,6 +86,35 @@ inline int shape_for(int64_t M, int64_t N, bool wide, unsigned which) {
   return best;
 }
 
+// Part of the tokens, and the shape that takes them.
+struct Segment {
+  int shape;
+  int64_t begin, tokens;
+};
+// The tokens' segments, one or two: the largest shape's last round of
+// workgroups may have little to do, which smaller tiles then do faster (2,000
+// rows x 50,021 tokens of 2,048 are 6.1 rounds: 445 us, 403 and 24 as two).  The tokens are A's rows of the
+// logits' product (ROWS) or B's of dw's, `across` the other operand's, K in bytes.
+template <bool ROWS>
+inline int segments_for(int64_t tokens, int64_t across, int64_t k_bytes, bool wide, unsigned which, Segment (&s)[2]) {
+  const auto best = [&](int64_t n) { return ROWS ? shape_for(n, across, wide, which) : shape_for(across, n, wide, which); };
+  const auto time = [&](int shape, int64_t n) {
+    const int64_t m_rows = ROWS ? n : across, n_rows = ROWS ? across : n;
+    return pace(shape, wide, ceil_div(m_rows, kTileM[shape]) * ceil_div(std::max<int64_t>(n_rows, 1), kTileN[shape]), m_rows);
+  };
+  s[0] = Segment{best(tokens), 0, tokens};
+  if (s[0].shape != 0) return 1;
+  const int64_t side = ceil_div(std::max<int64_t>(across, 1), 256), tiles = ceil_div(tokens, 256);
+  const int64_t whole = tiles * side / 256 * 256 / side * 256;   // tokens of whole rounds
+  if (whole == 0 || whole >= tokens) return 1;
+  const int rest = best(tokens - whole);
+  const float launch = 4.f * 128.f / static_cast<float>(k_bytes);  // us, a chunk's share
+  if (time(0, whole) + time(rest, tokens - whole) + launch >= time(0, tokens)) return 1;
+  s[0].tokens = whole;
+  s[1] = Segment{rest, whole, tokens - whole};
+  return 2;
+}
+
 // Calls f with a null pointer of the product of a shape; of operands that have
 // to go through registers there are fewer shapes.
 constexpr unsigned kThroughRegisters = 1u << 1 | 1u << 3 | 1u << 5;
@@ -113,9 +144,13 @@ inline int with_shape(int shape, bool direct, F f) {
 // The logits' product: a tile's rows are tokens, its columns hidden states'
 // rows, so that a lane has tokens on end.
 constexpr unsigned kLogitShapes = 0x2F;  // (64 x 32 is no faster than its neighbours)
+template <class T>
+inline int logit_segments(int64_t tokens, const gnnshap_linear& l, bool direct, Segment (&s)[2]) {
+  return segments_for<true>(tokens, l.num_rows, l.width * static_cast<int64_t>(sizeof(T)), sizeof(T) == 4,
+                            direct ? kLogitShapes : kLogitShapes & kThroughRegisters, s);
+}
 template <class T, class F>
-inline int with_logits(int64_t tokens, int64_t rows, bool direct, F f) {
-  const int shape = shape_for(tokens, rows, sizeof(T) == 4, direct ? kLogitShapes : kLogitShapes & kThroughRegisters);
+inline int with_logits(int shape, bool direct, F f) {
   return with_shape<T, false, false, kLogitShapes>(shape, direct, f);
 }
 

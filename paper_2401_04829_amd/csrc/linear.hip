@@ -19,10 +19,10 @@ __global__ __launch_bounds__(P::kThreads) void k_linear_stats(LinearArgs a) {
   const TileAt tile = tile_at(blockIdx.x, a.tiles_m, a.tiles_n);
   const int64_t v0 = static_cast<int64_t>(tile.m) * P::TM, b0 = static_cast<int64_t>(tile.n) * P::TN;
   P p;
-  p.run(lds, Operand{a.l.weight, a.l.weight_stride, a.l.vocab}, Operand{a.l.hidden, a.l.hidden_stride, a.l.num_rows},
-        v0, b0, a.l.width);
+  p.run(lds, Operand{static_cast<const typename P::T*>(a.l.weight) + a.v0 * a.l.weight_stride, a.l.weight_stride, a.tokens},
+        Operand{a.l.hidden, a.l.hidden_stride, a.l.num_rows}, v0, b0, a.l.width);
   const int lane = threadIdx.x & 63;
-  const int64_t left = a.l.vocab - v0;
+  const int64_t left = a.tokens - v0;
   Stats* const mine = reinterpret_cast<Stats*>(lds) + p.wave_m() / (16 * P::MT) * P::TN;
 #pragma unroll
   for (int t = 0; t < P::NT; ++t) {
@@ -53,7 +53,7 @@ __global__ __launch_bounds__(P::kThreads) void k_linear_stats(LinearArgs a) {
     s += __shfl_xor(s, 32);
     w += __shfl_xor(w, 32);
     if (lane < 16) mine[p.col_of(t)] = Stats{most, s, w};
-    const int64_t given = a.l.targets && row < a.l.num_rows ? a.l.targets[row] - v0 : -1;
+    const int64_t given = a.l.targets && row < a.l.num_rows ? a.l.targets[row] - a.v0 - v0 : -1;
     if (__ballot(given >= p.wave_m() && given < p.wave_m() + 16 * P::MT)) {
 #pragma unroll
       for (int j = 0; j < P::kRuns; ++j)
@@ -68,7 +68,7 @@ __global__ __launch_bounds__(P::kThreads) void k_linear_stats(LinearArgs a) {
     const Stats* const s = reinterpret_cast<const Stats*>(lds) + n;
     Stats st = s[0];
     for (int i = 1; i < P::TM / (16 * P::MT); ++i) add(st, s[i * P::TN]);
-    a.parts[(b0 + n) * a.tiles_m + tile.m] = st;
+    a.parts[(b0 + n) * a.row_parts + a.part0 + tile.m] = st;
   }
 }
 
@@ -80,7 +80,7 @@ __global__ __launch_bounds__(256) void k_linear_join(LinearArgs a) {
   const int64_t row = static_cast<int64_t>(blockIdx.x) * (4 / PER_ROW) + wave / PER_ROW;
   if (row >= a.l.num_rows) return;
   Stats st = no_stats();
-  for (unsigned i = wave % PER_ROW * 64 + lane; i < a.tiles_m; i += 64 * PER_ROW) add(st, a.parts[row * a.tiles_m + i]);
+  for (unsigned i = wave % PER_ROW * 64 + lane; i < a.row_parts; i += 64 * PER_ROW) add(st, a.parts[row * a.row_parts + i]);
   wave_sum(st);
   if constexpr (PER_ROW > 1) {
     if (lane == 0) stats[wave] = st;
@@ -102,24 +102,27 @@ __global__ __launch_bounds__(256) void k_linear_join(LinearArgs a) {
 
 size_t carve(LinearArgs& a, void* ws) {
   Carver c(ws);
-  a.parts = c.take<Stats>(static_cast<size_t>(a.l.num_rows) * a.tiles_m);
+  a.parts = c.take<Stats>(static_cast<size_t>(a.l.num_rows) * a.row_parts);
   a.given = c.take<float>(static_cast<size_t>(a.l.num_rows));
   return c.bytes();
 }
 
-// Tiles of the call; a refusal of more than a launch takes.
-template <class P>
-int lay_out(LinearArgs& a) {
-  const int64_t m = ceil_div(a.l.vocab, P::TM), n = ceil_div(a.l.num_rows, P::TN);
-  a.tiles_m = static_cast<unsigned>(m);
-  a.tiles_n = static_cast<unsigned>(n);
-  if (m * n > INT32_MAX) return check_launch(m * n, P::kThreads);
-  if (const int st = check_launch(m * n, P::kThreads)) return st;
+// The call's segments and a row's parts; a refusal of more workgroups than a launch takes.
+template <class T>
+int lay_out(LinearArgs& a, bool direct, Segment (&s)[2], int& segments) {
+  segments = logit_segments<T>(a.l.vocab, a.l, direct, s);
+  int64_t parts = 0;
+  for (int i = 0; i < segments; ++i) {
+    const int64_t m = ceil_div(s[i].tokens, kTileM[s[i].shape]), n = ceil_div(a.l.num_rows, kTileN[s[i].shape]);
+    if (const int st = check_launch(m * n, 512)) return st;
+    parts += m;
+  }
+  a.row_parts = static_cast<unsigned>(parts);
   return check_launch(a.l.num_rows, 64);
 }
 
 template <class P>
-int launch(LinearArgs a, hipStream_t s) {
+int launch(const LinearArgs& a, hipStream_t s) {
   GS_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(k_linear_stats<P>), hipFuncAttributeMaxDynamicSharedMemorySize,
                              P::kLds));
   {
@@ -127,9 +130,26 @@ int launch(LinearArgs a, hipStream_t s) {
     k_linear_stats<P><<<a.tiles_m * a.tiles_n, P::kThreads, P::kLds, s>>>(a);
   }
   GS_LAUNCHED();
+  return GNNSHAP_OK;
+}
+
+template <class T>
+int run(LinearArgs a, bool direct, const Segment (&segment)[2], int segments, hipStream_t s) {
+  for (int i = 0; i < segments; ++i) {
+    a.v0 = segment[i].begin;
+    a.tokens = segment[i].tokens;
+    const int st = with_logits<T>(segment[i].shape, direct, [&](auto* p) {
+      using P = std::remove_pointer_t<decltype(p)>;
+      a.tiles_m = static_cast<unsigned>(ceil_div(a.tokens, P::TM));
+      a.tiles_n = static_cast<unsigned>(ceil_div(a.l.num_rows, P::TN));
+      return launch<P>(a, s);
+    });
+    if (st) return st;
+    a.part0 += a.tiles_m;
+  }
   {
     GS_TIMED("k_linear_join", s);
-    if (a.tiles_m > 64 && a.l.num_rows < 1024)
+    if (a.row_parts > 64 && a.l.num_rows < 1024)
       k_linear_join<4><<<static_cast<unsigned>(a.l.num_rows), 256, 0, s>>>(a);
     else
       k_linear_join<1><<<static_cast<unsigned>(ceil_div(a.l.num_rows, 4)), 256, 0, s>>>(a);
@@ -163,18 +183,15 @@ extern "C" int gnnshap_linear_logprobs_workspace(const gnnshap_linear* l, size_t
   if (l->num_rows == 0) return GNNSHAP_OK;
   return with_dtype(l->dtype, [&](auto* x) {
     using T = std::remove_pointer_t<decltype(x)>;
-    int st = GNNSHAP_OK;
     for (const bool direct : {true, false}) {  // as the call's addresses will have it
-      if (st) break;
-      st = with_logits<T>(l->vocab, l->num_rows, direct, [&](auto* p) {
-        LinearArgs a{};
-        a.l = *l;
-        if (const int refused = lay_out<std::remove_pointer_t<decltype(p)>>(a)) return refused;
-        *bytes = std::max(*bytes, carve(a, nullptr));
-        return static_cast<int>(GNNSHAP_OK);
-      });
+      LinearArgs a{};
+      a.l = *l;
+      Segment segment[2];
+      int segments;
+      if (const int st = lay_out<T>(a, direct, segment, segments)) return st;
+      *bytes = std::max(*bytes, carve(a, nullptr));
     }
-    return st;
+    return static_cast<int>(GNNSHAP_OK);
   });
   GS_TRY_END
 }
@@ -188,17 +205,17 @@ extern "C" int gnnshap_linear_logprobs(const gnnshap_linear* l, int32_t* info, v
   if (!l->hidden || !l->weight) return fail(GNNSHAP_EINVAL, "NULL hidden states or weights");
   return with_dtype(l->dtype, [&](auto* x) {
     using T = std::remove_pointer_t<decltype(x)>;
-    return with_logits<T>(l->vocab, l->num_rows, direct_logits<T>(*l), [&](auto* p) {
-      using P = std::remove_pointer_t<decltype(p)>;
-      LinearArgs a{};
-      a.l = *l;
-      a.info = info;
-      if (const int st = lay_out<P>(a)) return st;
-      const size_t need = carve(a, ws);
-      if (!ws || ws_bytes < need)
-        return fail(GNNSHAP_ECAPACITY, "linear_logprobs workspace needs %zu bytes, has %zu", need, ws ? ws_bytes : 0);
-      return launch<P>(a, static_cast<hipStream_t>(stream));
-    });
+    const bool direct = direct_logits<T>(*l);
+    LinearArgs a{};
+    a.l = *l;
+    a.info = info;
+    Segment segment[2];
+    int segments;
+    if (const int st = lay_out<T>(a, direct, segment, segments)) return st;
+    const size_t need = carve(a, ws);
+    if (!ws || ws_bytes < need)
+      return fail(GNNSHAP_ECAPACITY, "linear_logprobs workspace needs %zu bytes, has %zu", need, ws ? ws_bytes : 0);
+    return run<T>(a, direct, segment, segments, static_cast<hipStream_t>(stream));
   });
   GS_TRY_END
 }

@@ -35,7 +35,7 @@ __global__ __launch_bounds__(P::kThreads) void k_linear_d(LinearArgs a) {
   const TileAt tile = tile_at(blockIdx.x, a.tiles_m, a.tiles_n);
   const int64_t v0 = static_cast<int64_t>(tile.m) * P::TM, b0 = static_cast<int64_t>(tile.n) * P::TN;
   P p;
-  p.run(lds, Operand{static_cast<const T*>(a.l.weight) + a.v0 * a.l.weight_stride, a.l.weight_stride, a.piece},
+  p.run(lds, Operand{static_cast<const T*>(a.l.weight) + a.v0 * a.l.weight_stride, a.l.weight_stride, a.tokens},
         Operand{a.l.hidden, a.l.hidden_stride, a.l.num_rows}, v0, b0, a.l.width);
   const float scale = a.scale ? a.scale[0] : 1.f;
 #pragma unroll
@@ -60,10 +60,10 @@ __global__ __launch_bounds__(P::kThreads) void k_linear_d(LinearArgs a) {
         const float logp = (p.at(j, i, t) - top) - logs, e = __builtin_amdgcn_exp2f(logp * kLog2e);
         const float own = at == given ? gl : 0.f;
         d[j][i] = own - e * (gl + ge * ((e == 0.f ? 0.f : logp) + ent));
-        if (none || v0 + at >= a.piece) d[j][i] = 0.f;  // behind the piece: the products read it
+        if (none || v0 + at >= a.tokens) d[j][i] = 0.f;  // behind the piece, to the tile's end: the products read it
         d[j][i] *= scale;
       }
-    T* const out = static_cast<T*>(a.d) + v0;
+    T* const out = static_cast<T*>(a.d) + a.d0 + v0;
     p.template rows_out<T>(lds, t, [&](int j, int i) { return static_cast<T>(d[j][i]); }, [&](int n, int m, const auto& x) {
       if (b0 + n < a.l.num_rows) store_pack(out + (b0 + n) * a.pitch + m, x);
     });
@@ -132,30 +132,47 @@ struct JoinArgs {
   int64_t stride;
 };
 
-// Adds up dh's parts, four elements to a thread.
-template <class T>
+// Adds up dh's parts: four elements to a thread, and (few rows) WAYS threads to
+// these, each with every WAYS-th part (16 rows of 1,024 in 32 parts: 12.7 us with one, 4.0 with eight).
+template <class T, int WAYS>
 __global__ __launch_bounds__(256) void k_linear_dh_join(JoinArgs a) {
+  constexpr int kPacks = 256 / WAYS;
+  __shared__ float sums[WAYS][kPacks][4];
   const int64_t packs = (a.width + 3) / 4, rows = a.two ? a.rows / 2 : a.rows;
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (i >= rows * packs) return;
-  const int64_t row = i / packs, m = (i - row * packs) * 4;
+  const int way = threadIdx.x / kPacks, mine = threadIdx.x % kPacks;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * kPacks + mine;
+  const bool in = i < rows * packs;
+  const int64_t row = in ? i / packs : 0, m = in ? (i - row * packs) * 4 : 0;
   const int n = a.width - m < 4 ? static_cast<int>(a.width - m) : 4;
-  const float over = a.scale ? a.scale[1] : 1.f;
+  // the second parts of d's rows are parts like others
+  const int64_t all = a.two ? 2 * a.parts : a.parts;
   float s[4] = {0.f, 0.f, 0.f, 0.f};
-  const auto add_row = [&](const float* p) {
-    if (n == 4) {
-      const Pack<float, 4> x = load_pack<float, 4>(p);
+  const auto part_at = [&](int64_t p) {
+    return a.sums + (a.two ? (p >> 1) * a.rows + (p & 1) * rows + row : p * a.rows + row) * a.width + m;
+  };
+  if (in && n == 4) {
+#pragma unroll 8
+    for (int64_t p = way; p < all; p += WAYS) {
+      const Pack<float, 4> x = load_pack<float, 4>(part_at(p));
 #pragma unroll
       for (int e = 0; e < 4; ++e) s[e] += x.v[e];
-    } else {
-      for (int e = 0; e < n; ++e) s[e] += p[e];
     }
-  };
-#pragma unroll 4
-  for (int64_t part = 0; part < a.parts; ++part) add_row(a.sums + (part * a.rows + row) * a.width + m);
-  if (a.two)
-#pragma unroll 4
-    for (int64_t part = 0; part < a.parts; ++part) add_row(a.sums + (part * a.rows + rows + row) * a.width + m);
+  } else if (in) {
+    for (int64_t p = way; p < all; p += WAYS)
+      for (int e = 0; e < n; ++e) s[e] += part_at(p)[e];
+  }
+  if constexpr (WAYS > 1) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sums[way][mine][e] = s[e];
+    __syncthreads();
+    if (way > 0) return;
+#pragma unroll
+    for (int w = 1; w < WAYS; ++w)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] += sums[w][mine][e];
+  }
+  if (!in) return;
+  const float over = a.scale ? a.scale[1] : 1.f;
   T* const out = static_cast<T*>(a.out) + row * a.stride + m;
   if (n == 4) {
     Pack<T, 4> x;
@@ -342,16 +359,21 @@ int run(const LinearArgs& given, void* grad_hidden, int64_t gh_stride, void* gra
   for (int64_t v0 = 0; v0 < l.vocab; v0 += y.piece) {
     const int64_t piece = std::min(y.piece, l.vocab - v0);
     int st = GNNSHAP_OK;
+    Segment segment[2];
     if (l.num_rows > 0) {
-      st = with_logits<T>(piece, l.num_rows, direct_logits_too, [&](auto* p) {
-        using P = std::remove_pointer_t<decltype(p)>;
-        a.v0 = v0;
-        a.piece = piece;
-        a.tiles_m = static_cast<unsigned>(ceil_div(piece, P::TM));
-        a.tiles_n = static_cast<unsigned>(ceil_div(l.num_rows, P::TN));
-        return launch<P>(k_linear_d<P>, "k_linear_d", a, static_cast<int64_t>(a.tiles_m) * a.tiles_n, s);
-      });
-      if (st) return st;
+      const int segments = logit_segments<T>(piece, l, direct_logits_too, segment);
+      for (int i = 0; i < segments; ++i) {
+        a.v0 = v0 + segment[i].begin;
+        a.tokens = segment[i].tokens;
+        a.d0 = segment[i].begin;
+        st = with_logits<T>(segment[i].shape, direct_logits_too, [&](auto* p) {
+          using P = std::remove_pointer_t<decltype(p)>;
+          a.tiles_m = static_cast<unsigned>(ceil_div(a.tokens, P::TM));
+          a.tiles_n = static_cast<unsigned>(ceil_div(l.num_rows, P::TN));
+          return launch<P>(k_linear_d<P>, "k_linear_d", a, static_cast<int64_t>(a.tiles_m) * a.tiles_n, s);
+        });
+        if (st) return st;
+      }
     }
     if (grad_hidden && l.num_rows > 0) {
       st = with_shape<T, true, false, kHiddenShapes>(y.hidden_shape, direct_w, [&](auto* p) {
@@ -364,25 +386,33 @@ int run(const LinearArgs& given, void* grad_hidden, int64_t gh_stride, void* gra
       if (st) return st;
     }
     if (grad_weight) {
-      const int shape = shape_for(l.width, piece, sizeof(T) == 4,
-                                  direct_h ? kWeightShapes : kWeightShapes & kThroughRegisters);
-      st = with_shape<T, true, true, kWeightShapes>(shape, direct_h, [&](auto* p) {
-        using P = std::remove_pointer_t<decltype(p)>;
-        WeightArgs w{l.hidden, l.hidden_stride, y.d, y.pitch, piece, l.num_rows, l.width, y.two,
-                     static_cast<unsigned>(ceil_div(l.width, P::TM)), static_cast<unsigned>(ceil_div(piece, P::TN)),
-                     a.scale, static_cast<T*>(grad_weight) + v0 * gw_stride, gw_stride};
-        return launch<P>(k_linear_dw<P>, "k_linear_dw", w, static_cast<int64_t>(w.tiles_m) * w.tiles_n, s);
-      });
+      const int segments = segments_for<false>(
+          piece, l.width, std::max<int64_t>(l.num_rows, 1) * (y.two ? 2 : 1) * static_cast<int64_t>(sizeof(T)), sizeof(T) == 4,
+          direct_h ? kWeightShapes : kWeightShapes & kThroughRegisters, segment);
+      for (int i = 0; i < segments && !st; ++i)
+        st = with_shape<T, true, true, kWeightShapes>(segment[i].shape, direct_h, [&](auto* p) {
+          using P = std::remove_pointer_t<decltype(p)>;
+          WeightArgs w{l.hidden, l.hidden_stride, static_cast<const T*>(y.d) + segment[i].begin, y.pitch, segment[i].tokens,
+                       l.num_rows, l.width, y.two, static_cast<unsigned>(ceil_div(l.width, P::TM)),
+                       static_cast<unsigned>(ceil_div(segment[i].tokens, P::TN)), a.scale,
+                       static_cast<T*>(grad_weight) + (v0 + segment[i].begin) * gw_stride, gw_stride};
+          return launch<P>(k_linear_dw<P>, "k_linear_dw", w, static_cast<int64_t>(w.tiles_m) * w.tiles_n, s);
+        });
       if (st) return st;
     }
   }
   if (grad_hidden && l.num_rows > 0) {
     JoinArgs j{y.sums, y.parts, y.d_rows, l.width, y.two, a.scale, grad_hidden, gh_stride};
-    const int64_t groups = ceil_div(l.num_rows * ceil_div(l.width, 4), 256);
+    const int64_t packs = l.num_rows * ceil_div(l.width, 4);
+    const bool few = y.parts > 8 && packs < 65536;
+    const int64_t groups = ceil_div(packs, few ? 32 : 256);
     if (const int st = check_launch(groups, 256)) return st;
     {
       GS_TIMED("k_linear_dh_join", s);
-      k_linear_dh_join<T><<<static_cast<unsigned>(groups), 256, 0, s>>>(j);
+      if (few)
+        k_linear_dh_join<T, 8><<<static_cast<unsigned>(groups), 256, 0, s>>>(j);
+      else
+        k_linear_dh_join<T, 1><<<static_cast<unsigned>(groups), 256, 0, s>>>(j);
     }
     GS_LAUNCHED();
   }

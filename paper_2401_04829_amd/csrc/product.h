@@ -233,7 +233,7 @@ struct Product {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                  :
                  : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(off), "s"(b)
-                 : "memory");
+                 : "memory", "m0");
   }
   // At most LEFT loads of this wavefront are on their way, and its reads of LDS are done.
   template <int LEFT>
