@@ -62,8 +62,9 @@ struct Images {
 
 // The images of up to 4,096 HELD tokens stay in registers, so that memory is
 // waited for twice; HELD = 0: of any number, read for each digit and once more.
-// One workgroup's instructions bound it: 30,000 tokens, of which 4,000 stay,
-// 38 us when an image was found anew each time; 2,001 tokens 8.5 us.
+// One workgroup's instructions bound it: 30,000 tokens, of which 4,000 stay, 29 us
+// (38 when an image was found anew for each digit, 47 when the weights were
+// read for each); 64 x 2,001 tokens 10 us.
 template <int HELD>
 __global__ __launch_bounds__(kSelect) void k_evict_select(EvictArgs a) {
   constexpr int kWaves = kSelect / 64, kBlocks = kWaves * (HELD ? HELD : 1);
@@ -305,7 +306,11 @@ __device__ __forceinline__ int64_t place_of(const EvictArgs& a, int64_t seq, int
   return p * a.c.page_stride + slot * a.c.slot_stride;
 }
 
-// A workgroup: a.packs packs of 16 bytes of one head's keys or values, of all of a sequence's tokens.
+// A workgroup: a.packs packs of 16 bytes of one head's keys or values, of all of a
+// sequence's tokens.  Bound by memory where sequences are many (64 of 2,001 tokens,
+// of which one goes and the last 200 to 220 of each move up, 120 MB: 24 us, 5
+// TB/s), else by three dependent loads of each turn (kept place, page, element): 4,000
+// tokens of one sequence 17 us.
 template <class T>
 __global__ __launch_bounds__(kMove) void k_evict_move(EvictArgs a) {
   unsigned b = blockIdx.x;

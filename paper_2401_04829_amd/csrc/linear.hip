@@ -53,7 +53,8 @@ __global__ __launch_bounds__(P::kThreads) void k_linear_stats(LinearArgs a) {
     s += __shfl_xor(s, 32);
     w += __shfl_xor(w, 32);
     if (lane < 16) mine[p.col_of(t)] = Stats{most, s, w};
-    const int64_t given = a.l.targets && row < a.l.num_rows ? a.l.targets[row] - a.v0 - v0 : -1;
+    int64_t given = a.l.targets && row < a.l.num_rows ? a.l.targets[row] : -1;
+    given = given < 0 ? -1 : given - a.v0 - v0;
     if (__ballot(given >= p.wave_m() && given < p.wave_m() + 16 * P::MT)) {
 #pragma unroll
       for (int j = 0; j < P::kRuns; ++j)

@@ -50,7 +50,7 @@ __global__ __launch_bounds__(P::kThreads) void k_linear_d(LinearArgs a) {
     const float gl = a.gl && given >= 0 ? a.gl[b] : 0.f;
     const float ge = a.ge ? a.ge[b] : 0.f, ent = a.ge ? a.l.entropy[b] : 0.f;
     const bool none = top == -INFINITY && logs == 0.f;
-    given -= a.v0 + v0;
+    given = given < 0 ? -1 : given - a.v0 - v0;
     float d[P::kRuns][P::kRun];
 #pragma unroll
     for (int j = 0; j < P::kRuns; ++j)

@@ -9,9 +9,13 @@
 // the 16 columns at the end.
 //
 // Few queries (a new token of each sequence) are bound by reading the keys
-// once; the kv heads' sums meet in LDS.  Many (coalitions, a prompt's rows) are
-// bound by an exponential per query and key; their range is split so that the
-// chip is full, and a second launch adds up the parts in order.
+// once, or by the call; the kv heads' sums meet in LDS.  Many (coalitions, a
+// prompt's rows) are bound by the vector instructions of a weight (the
+// exponential, its argument, the mask, the sum: 10 per query and key) and the
+// matrix instructions beside them; their range is split so that the chip is
+// full, and a second launch adds up the parts in order.  bf16, 32 heads over 8 of
+// 128: 10,000 coalitions on 417 tokens 88 us and 5 to join (queries three tiles
+// ahead instead of two: 91); one row on 4,000 tokens 7 us.
 #include "attend.h"
 
 namespace {
@@ -25,7 +29,7 @@ struct WeightsArgs {
   gnnshap_observed o;
   int share, page_shift;
   int64_t queries;   // of a sequence and kv head
-  float scale;
+  float scale2;      // scale log2 e
   int splits;        // of the queries; 0: the kernel of few
   int64_t split;     // tiles of 16 queries of a split
   float* part;       // [sequence][kv head][split][max_length]
@@ -49,23 +53,31 @@ struct Vectors {
     }
   }
   typedef T vec8 __attribute__((ext_vector_type(8)));
-  static __device__ __forceinline__ f4_t products(const Vectors& k, const Vectors& q) {
-    f4_t c = {0.f, 0.f, 0.f, 0.f};
+  // c[n] = products of the N tiles of keys with the queries: steps outside, so that
+  // an instruction does not wait for the one before it.
+  template <int N>
+  static __device__ __forceinline__ void products(const Vectors (&k)[N], const Vectors& q, f4_t (&c)[N]) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) c[n] = f4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-      if constexpr (std::is_same_v<T, bf16_t>) {
-        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(vec8, k.s[i]), __builtin_bit_cast(vec8, q.s[i]), c,
-                                                    0, 0, 0);
-      } else if constexpr (std::is_same_v<T, f16_t>) {
-        c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(vec8, k.s[i]), __builtin_bit_cast(vec8, q.s[i]), c,
-                                                   0, 0, 0);
-      } else {
+      if constexpr (std::is_same_v<T, float>) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k.s[i][e]), __uint_as_float(q.s[i][e]), c, 0, 0, 0);
+#pragma unroll
+          for (int n = 0; n < N; ++n)
+            c[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[n].s[i][e]), __uint_as_float(q.s[i][e]), c[n], 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int n = 0; n < N; ++n) c[n] = mfma(k[n].s[i], q.s[i], c[n]);
       }
     }
-    return c;
+  }
+  static __device__ __forceinline__ f4_t mfma(u4_t a, u4_t b, f4_t c) {
+    if constexpr (std::is_same_v<T, bf16_t>)
+      return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(vec8, a), __builtin_bit_cast(vec8, b), c, 0, 0, 0);
+    else
+      return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(vec8, a), __builtin_bit_cast(vec8, b), c, 0, 0, 0);
   }
 };
 
@@ -109,15 +121,11 @@ struct KeyTile {
 template <int NK>
 struct Players {
   uint32_t always[NK / 2];   // no players: seen by every row
-  const uint32_t* masks;     // without players: words that are read and do not matter
-  int64_t row_words;
   int at[NK / 2 + 1], shift;   // 32-bit words of a row, the first key's bit in the first
   __device__ __forceinline__ Players(const WeightsArgs& a, int64_t k0) {
     const bool any = a.o.num_players > 0;
     const int64_t first = k0 - a.o.first_player;   // the first key among the players
     const int words = any ? static_cast<int>((a.o.num_players + 31) >> 5) : 1;
-    masks = any ? reinterpret_cast<const uint32_t*>(a.o.masks) : reinterpret_cast<const uint32_t*>(a.o.lse);
-    row_words = any ? 2 * a.o.mask_words : 0;
     shift = static_cast<int>(first & 31);
 #pragma unroll
     for (int w = 0; w <= NK / 2; ++w) {
@@ -134,6 +142,27 @@ struct Players {
   }
 };
 
+// Where a sequence's queries of a kv head lie, and what goes with its rows;
+// offsets from there are of type I, in bytes: 32 bits spare the kernel of many a
+// quarter of its instructions.
+template <class I>
+struct Rows {
+  const char *q, *lse, *len, *masks;
+  I q_row, q_head, lse_row, mask_row;
+  __device__ __forceinline__ Rows(const WeightsArgs& a, int64_t seq, int kv_head, int element) {
+    const int64_t row = seq * a.o.rows_per_seq, head = static_cast<int64_t>(kv_head) * a.share;
+    const bool any = a.o.num_players > 0;   // without players words are read that do not matter
+    q = static_cast<const char*>(a.o.q) + (row * a.o.q_row_stride + head * a.o.q_head_stride) * element;
+    lse = reinterpret_cast<const char*>(a.o.lse + row * a.o.heads + head);
+    len = reinterpret_cast<const char*>(a.o.lengths + row);
+    masks = any ? reinterpret_cast<const char*>(a.o.masks + row * a.o.mask_words) : lse;
+    q_row = static_cast<I>(a.o.q_row_stride * element);
+    q_head = static_cast<I>(a.o.q_head_stride * element);
+    lse_row = static_cast<I>(a.o.heads) * 4;
+    mask_row = any ? static_cast<I>(a.o.mask_words) * 8 : 0;
+  }
+};
+
 // 16 queries of a sequence and kv head, this lane's among them: row `row` of the
 // sequence, query head `of` of the kv head.  load() only asks memory, so that the
 // next queries can be on their way while these are multiplied.
@@ -144,17 +173,18 @@ struct QueryTile {
   int len;
   uint32_t word[NK / 2 + 1];
   bool in;
-  __device__ __forceinline__ void load(const WeightsArgs& a, const Players<NK>& p, int64_t seq, int kv_head, int row, int of,
+  template <class I>
+  __device__ __forceinline__ void load(const WeightsArgs& a, const Players<NK>& p, const Rows<I>& rows, int row, int of,
                                        bool there) {
     in = there;
-    const int64_t b = seq * a.o.rows_per_seq + (in ? row : 0);
-    const int head = kv_head * a.share + (in ? of : 0);
-    q.load(static_cast<const T*>(a.o.q) + b * a.o.q_row_stride + head * a.o.q_head_stride, a.c.head_dim, false);
-    lse = a.o.lse[b * a.o.heads + head];
-    len = a.o.lengths[b];
-    const uint32_t* const m = p.masks + b * p.row_words;
+    const I b = in ? row : 0, h = in ? of : 0;
+    q.load(reinterpret_cast<const T*>(rows.q + (b * rows.q_row + h * rows.q_head)), a.c.head_dim, false);
+    lse = *reinterpret_cast<const float*>(rows.lse + (b * rows.lse_row + h * 4));
+    len = *reinterpret_cast<const int*>(rows.len + b * 4);
+    const I m = b * rows.mask_row;
 #pragma unroll
-    for (int w = 0; w <= NK / 2; ++w) word[w] = m[p.at[w]];
+    for (int w = 0; w <= NK / 2; ++w)
+      word[w] = *reinterpret_cast<const uint32_t*>(rows.masks + (m + static_cast<I>(4 * p.at[w])));
   }
   // The keys that the lane's query sees, of those from 32 w on.
   __device__ __forceinline__ uint32_t sees(const WeightsArgs& a, const Players<NK>& p, int64_t k0, int w, bool& bad) const {
@@ -166,28 +196,36 @@ struct QueryTile {
   }
 };
 
+// With n the whole number next to lse log2 e, a weight is 2^(s log2 e - n) times
+// f = e^(n ln 2 - lse): one multiplication and addition makes the exponent, whose
+// rounding is that of the score, and f, which is the row's, rides on the sum.
 template <class T, int DP, int NK>
 __device__ __forceinline__ void add(const WeightsArgs& a, const Players<NK>& p, KeyTile<T, DP, NK>& t,
                                     const QueryTile<T, DP, NK>& q, int64_t k0, bool& bad) {
+  constexpr float kLn2High = 0.693145752f, kLn2Low = 1.42860677e-6f;   // their sum is ln 2
+  const float n = rintf(q.lse * kLog2eF);
+  float f = __builtin_amdgcn_exp2f(fmaf(n, kLn2Low, fmaf(n, kLn2High, -q.lse)) * kLog2eF);
+  f = fabsf(n) < INFINITY ? f : 1.f;   // (an lse that is not finite is in the exponents)
+  uint32_t bits[NK / 2], any = 0u;
 #pragma unroll
   for (int w = 0; w < NK / 2; ++w) {
     const uint32_t lost = static_cast<uint32_t>(t.lost >> (32 * w)), all = q.sees(a, p, k0, w, bad);
     bad |= (all & lost) != 0u;
-    const uint32_t bits = (all & ~lost) >> (4 * ((threadIdx.x >> 4) & 3));
-    if (!__ballot(bits)) continue;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const f4_t c = Vectors<T, DP>::products(t.key[2 * w + i], q.q);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        // the difference first: its rounding is that of a small number.  What is
-        // not seen may be NaN: its bits are cleared
-        const float x = __builtin_amdgcn_exp2f(fmaf(c[e], a.scale, -q.lse) * kLog2eF);
-        const int seen_too = static_cast<int>(bits << (31 - 16 * i - e)) >> 31;
-        t.sum[8 * w + 4 * i + e] += __uint_as_float(__float_as_uint(x) & static_cast<uint32_t>(seen_too));
-      }
-    }
+    bits[w] = (all & ~lost) >> (4 * ((threadIdx.x >> 4) & 3));
+    any |= bits[w];
   }
+  if (!__ballot(any)) return;
+  f4_t c[NK];
+  Vectors<T, DP>::products(t.key, q.q, c);
+#pragma unroll
+  for (int i = 0; i < NK; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      // what is not seen may be NaN: its bits are cleared
+      const float x = __builtin_amdgcn_exp2f(fmaf(c[i][e], a.scale2, -n));
+      const uint32_t seen_too = static_cast<uint32_t>(__builtin_amdgcn_sbfe(static_cast<int>(bits[i / 2]), 16 * (i % 2) + e, 1));
+      t.sum[4 * i + e] = fmaf(__uint_as_float(__float_as_uint(x) & seen_too), f, t.sum[4 * i + e]);
+    }
 }
 
 // Adds up the 16 columns; all lanes get the sums of their keys.
@@ -214,14 +252,19 @@ __global__ __launch_bounds__(256) void k_cache_weights(WeightsArgs a, int by_hea
   bool bad = false;
   // a wavefront whose keys no row sees has nothing to read
   bool any = false;
-  for (int64_t b = lane; b < a.o.rows_per_seq && !any; b += 64) any = a.o.lengths[seq * a.o.rows_per_seq + b] > k0;
+  for (int64_t b = lane; b < a.o.rows_per_seq; b += 64) {
+    const int len = a.o.lengths[seq * a.o.rows_per_seq + b];
+    any |= len > k0;
+    bad |= len < 0;
+  }
   if (__ballot(any)) {
     for (int h = own; h < a.c.kv_heads; h += by_heads) {
       t.load(a, h);
+      const Rows<int64_t> rows(a, seq, h, sizeof(T));
       for (int q0 = 0; q0 < a.queries; q0 += 16) {
         QueryTile<T, DP, 2> q;
         const int n = q0 + r, row = n / a.share;
-        q.load(a, players, seq, h, row, n - row * a.share, n < a.queries);
+        q.load(a, players, rows, row, n - row * a.share, n < a.queries);
         add(a, players, t, q, k0, bad);
       }
     }
@@ -240,29 +283,35 @@ __global__ __launch_bounds__(256) void k_cache_weights(WeightsArgs a, int by_hea
   }
 }
 
-// Many queries: each wavefront of a workgroup has 16 NK keys of its own, all the same queries.
+// Many queries: each wavefront has 16 NK keys and a split of the queries.  The
+// wavefronts that share queries follow each other, the workgroups of an XCD (every
+// eighth) too, so that the queries come through one cache.
 template <class T, int DP, int NK>
-__global__ __launch_bounds__(256) void k_cache_weights_many(WeightsArgs a, unsigned tiles) {
+__global__ __launch_bounds__(256, DP * sizeof(T) <= 512 ? 2 : 1) void k_cache_weights_many(WeightsArgs a, unsigned tiles, unsigned places) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-  unsigned b = blockIdx.x;
+  const unsigned xcd = blockIdx.x % 8, each = gridDim.x / 8, more = gridDim.x % 8;
+  unsigned b = __builtin_amdgcn_readfirstlane((xcd * each + (xcd < more ? xcd : more) + blockIdx.x / 8) * 4 + wave);
+  if (b >= places) return;
+  const int64_t k0 = static_cast<int64_t>(b % tiles) * (16 * NK);
+  b /= tiles;
   const int split = b % a.splits;
   b /= a.splits;
   const int kv_head = b % a.c.kv_heads;
-  b /= a.c.kv_heads;
-  const int64_t k0 = (static_cast<int64_t>(b % tiles) * 4 + wave) * (16 * NK), seq = b / tiles;
+  const int64_t seq = b / a.c.kv_heads;
   KeyTile<T, DP, NK> t;
   t.find(a, seq, k0);
   const int q0 = static_cast<int>(split * a.split * 16);
   const int q1 = static_cast<int>(q0 + a.split * 16 < a.queries ? q0 + a.split * 16 : a.queries);
-  if (q0 < q1 && k0 < a.o.max_length) {
+  if (q0 < q1) {
     t.load(a, kv_head);
     const Players<NK> players(a, k0);
+    const Rows<uint32_t> rows(a, seq, kv_head, sizeof(T));
     QueryTile<T, DP, NK> now, next;
     // this lane's query goes on by 16, the rows by 16 / share
     int n = q0 + r, row = n / a.share, of = n - row * a.share;
     const int rows_on = 16 / a.share, heads_on = 16 - rows_on * a.share;
     const auto load = [&](QueryTile<T, DP, NK>& q) {
-      q.load(a, players, seq, kv_head, row, of, n < q1);
+      q.load(a, players, rows, row, of, n < q1);
       n += 16;
       row += rows_on;
       of += heads_on;
@@ -294,9 +343,10 @@ __global__ __launch_bounds__(256) void k_cache_weights_many(WeightsArgs a, unsig
     }
 }
 
-// Tiles of 16 keys of a wavefront: four where they and two tiles of queries fit its registers.
-template <class T, int DP>
-constexpr int kKeyTiles = DP * sizeof(T) <= 256 ? 4 : 2;
+// Tiles of 16 keys of a wavefront: four where they and two tiles of queries fit
+// its registers (10,000 rows x 32 heads of 128 on 417 tokens: 138 us with four, 148
+// with two).
+constexpr int key_tiles_of(int padded_bytes) { return padded_bytes <= 256 ? 4 : 2; }
 
 // Adds the parts up, a thread per token of a sequence.
 __global__ __launch_bounds__(256) void k_cache_weights_join(WeightsArgs a) {
@@ -349,10 +399,10 @@ int check_observed(const gnnshap_cache* c, const gnnshap_observed* o) {
 int64_t sequences(const WeightsArgs& a) { return a.o.num_rows / a.o.rows_per_seq; }
 int64_t key_tiles(const WeightsArgs& a, int keys) { return ceil_div(std::max<int64_t>(a.o.max_length, 1), keys); }
 
-// Keys of a workgroup of the kernel of many.
+// Keys of a wavefront of the kernel of many.
 int keys_of_many(const WeightsArgs& a) {
   const int padded = a.c.head_dim <= 64 ? 64 : a.c.head_dim <= 128 ? 128 : 256;
-  return 64 * (padded * (a.c.dtype == GNNSHAP_F32 ? 4 : 2) <= 256 ? 4 : 2);
+  return 16 * key_tiles_of(padded * (a.c.dtype == GNNSHAP_F32 ? 4 : 2));
 }
 
 int by_heads(const WeightsArgs& a) { return a.c.kv_heads >= 4 ? 4 : a.c.kv_heads >= 2 ? 2 : 1; }
@@ -362,21 +412,26 @@ int lay_out(WeightsArgs& a, const gnnshap_cache* c, const gnnshap_observed* o) {
   a.o = *o;
   a.share = o->heads / c->kv_heads;
   a.queries = o->rows_per_seq * a.share;
-  a.scale = static_cast<float>(o->scale);
+  a.scale2 = static_cast<float>(o->scale * 1.4426950408889634074);
   a.page_shift = -1;
   for (int i = 0; i < 31; ++i)
     if (c->page_size == 1 << i) a.page_shift = i;
   if (a.queries > INT32_MAX - 1024)
     return fail(GNNSHAP_EUNSUPPORTED, "%lld queries of a sequence", static_cast<long long>(a.queries));
   const int64_t seqs = sequences(a), tiles = ceil_div(a.queries, 16);
-  if (a.queries <= 64) return check_launch(seqs * key_tiles(a, 128 / by_heads(a)), 256);
+  // the kernel of many counts a sequence's bytes in 32 bits
+  const int element = c->dtype == GNNSHAP_F32 ? 4 : 2;
+  const int64_t limit = int64_t(1) << 31, rows = o->rows_per_seq;
+  const bool near = o->q_row_stride <= limit / element / rows && o->q_head_stride <= limit / element / o->heads &&
+                    rows * o->heads * 4 < limit && rows * std::max<int64_t>(o->mask_words, 1) * 8 < limit;
+  if (a.queries <= 64 || !near) return check_launch(seqs * key_tiles(a, 128 / by_heads(a)), 256);
   const int64_t base = seqs * c->kv_heads * key_tiles(a, keys_of_many(a));
-  // three wavefronts per SIMD are resident, in one round (10,000 rows x 32 heads
-  // on 417 tokens: 768 workgroups 99 us, 1,536 105)
-  const int64_t want = std::max<int64_t>(1, std::min(768 / std::max<int64_t>(base, 1), ceil_div(tiles, 8)));
+  // two wavefronts per SIMD, in one round (10,000 rows x 32 heads on 417 tokens,
+  // in wavefronts: 2,048 83 us, 3,072 93, both with one key tile in eight empty)
+  const int64_t want = std::max<int64_t>(1, std::min(2048 / std::max<int64_t>(base, 1), ceil_div(tiles, 8)));
   a.split = ceil_div(tiles, want);
   a.splits = static_cast<int>(ceil_div(tiles, a.split));
-  if (const int st = check_launch(base * a.splits, 256)) return st;
+  if (const int st = check_launch(ceil_div(base * a.splits, 4), 256)) return st;
   return check_launch(seqs * key_tiles(a, 64), 256);
 }
 
@@ -397,12 +452,12 @@ int launch(const WeightsArgs& a, hipStream_t s) {
     GS_LAUNCHED();
     return GNNSHAP_OK;
   }
-  constexpr int NK = kKeyTiles<T, DP>;
-  const int64_t tiles = key_tiles(a, 64 * NK);
+  constexpr int NK = key_tiles_of(DP * static_cast<int>(sizeof(T)));
+  const int64_t tiles = key_tiles(a, 16 * NK), places = sequences(a) * a.c.kv_heads * a.splits * tiles;
   {
     GS_TIMED("k_cache_weights_many", s);
-    k_cache_weights_many<T, DP, NK><<<static_cast<unsigned>(sequences(a) * a.c.kv_heads * tiles * a.splits), 256, 0, s>>>(
-        a, static_cast<unsigned>(tiles));
+    k_cache_weights_many<T, DP, NK><<<static_cast<unsigned>(ceil_div(places, 4)), 256, 0, s>>>(
+        a, static_cast<unsigned>(tiles), static_cast<unsigned>(places));
   }
   GS_LAUNCHED();
   {

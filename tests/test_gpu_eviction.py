@@ -196,10 +196,17 @@ def test_lengths_and_pages_out_of_range(dev):
         bad[0, 1] = -3
         got = A.attention_weights(cache, queries, left, bad, n, torch.zeros((2, 64), device=dev), info=info)
         assert int(info) == 1 and torch.equal(got[1], want[1]) and torch.equal(got[0, 32:], want[0, 32:])
-        info.zero_()
-        n[0] = 65
-        A.attention_weights(cache, queries, left, table, n, torch.zeros((2, 64), device=dev), info=info)
-        assert int(info) == 1
+        for wrong in (65, -1):
+            info.zero_()
+            m = n.clone()
+            m[0] = wrong
+            A.attention_weights(cache, queries, left, table, m, torch.zeros((2, 64), device=dev), info=info)
+            assert int(info) == 1, (per, wrong)
+        for wrong in (65, -7):                             # and in eviction
+            info.zero_()
+            w = torch.rand((2, 64), generator=gen, device=dev)
+            e = A.evict_tokens(cache, table, torch.tensor([wrong, 30], **i32), w, 20, info=info)
+            assert int(info) == 1 and int(e.lengths[1]) == 20
 
 
 def _evicted(lengths, weights, keep, first, recent):
