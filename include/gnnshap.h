@@ -520,7 +520,8 @@ int gnnshap_gat_explain_batch(const gnnshap_subgraph* sgs, const gnnshap_sample_
  * its tokens alone: every coalition's new token attends over ONE cached
  * prompt, seeing the positions whose mask bit is set, and over tokens of its
  * own.  The calls below are the steps of such a model that touch the cache
- * or the answer; the products with its weights stay with the caller.
+ * or the answer; of the products with its weights only the
+ * vocabulary's is here, the others stay with the caller.
  *
  * Strides are in elements and need no alignment; the innermost axis
  * (head_dim elements, or the vocabulary) is contiguous.  `info` [dev, one

@@ -5,11 +5,15 @@ The players are tokens of a prompt.  Their keys and values are cached once
 attends over the cached prompt, seeing the positions its mask keeps, and over
 tokens of its own (`attend`); the answer's log probability is the coalition's
 value (`token_logprobs`), from which `AnswerExplainer` takes the Shapley
-values with the library's sampler and least squares.
+values with the library's sampler and least squares.  Around these: norms of
+heads with the rotation (`norm_rotate`, and on the way into the cache), the
+weights that attention gave cached tokens (`attention_weights`) and eviction of
+those that got least (`evict_tokens`), log probabilities straight from hidden
+states (`linear_logprobs`).
 
 Torch provides device memory and streams; the work runs in libgnnshap.so on
 the current stream.  Every tensor must be on the cache's (the logits') device.
-Of these calls only `differentiable_logprobs` has a derivative: the others
+Of these calls only those named `differentiable_` have a derivative: the others
 refuse tensors that require a gradient (unless under torch.no_grad()) or carry
 a tangent.
 """

@@ -6,10 +6,12 @@
 
 namespace gnnshap {
 
-// Of up to this many rows the gradient by the logits is given in two parts,
-// rounded and what that left: a few rows' gradients hang on few of its
+// Of up to this many rows the gradient by the logits is given in two 16-bit
+// parts, rounded and what that left: a few rows' gradients hang on few of its
 // elements, so that one rounding would show (up to 2^-8 in bf16, where the
-// result's own is 2^-9 on average), and cost nothing beside the weights.
+// result's own is 2^-9 on average; over many rows both come to 1.4 times the
+// result's own).  Of few rows it costs nothing beside the weights; of 200 it
+// would cost a third of the backward pass (50,021 x 2,048: 406 us against 303).
 constexpr int64_t kTwoParts = 128;
 
 struct LinearArgs {
