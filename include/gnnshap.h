@@ -703,7 +703,7 @@ typedef struct {
   const uint64_t* masks;         /* [dev] num_rows x mask_words, or NULL (num_players is then 0) */
   int64_t mask_words, num_players, first_player;
   double scale;                  /* scores are scale q.k, as for gnnshap_cache_attend */
-  float* weights;                /* [dev] sequence s's at weights + s weights_stride, max_length of them */
+  float* weights;                /* [dev] sequence s's at weights + s weights_stride, max_length of them, apart */
   int64_t weights_stride;
 } gnnshap_observed;
 
@@ -734,7 +734,7 @@ typedef struct {
   int64_t first, recent;         /* of these, its first and its last ones; first + recent <= keep */
   int32_t* kept;                 /* [dev] num_seqs x keep: the former places of the kept tokens, rising; then -1 */
   int32_t* new_lengths;          /* [dev] num_seqs; may be lengths */
-  float* new_weights;            /* [dev] likewise; may be weights, with their stride: the kept tokens', then 0 */
+  float* new_weights;            /* [dev] likewise, apart; may be weights, with their stride: the kept tokens', then 0 */
   int64_t new_weights_stride;
 } gnnshap_eviction;
 

@@ -15,7 +15,9 @@ Torch provides device memory and streams; the work runs in libgnnshap.so on
 the current stream.  Every tensor must be on the cache's (the logits') device.
 Of these calls only those named `differentiable_` have a derivative: the others
 refuse tensors that require a gradient (unless under torch.no_grad()) or carry
-a tangent.
+a tangent.  A backward pass is captured into a graph as any of torch's is: only
+while no other graph of the same leaves lives that was built outside of the
+capture (torch would wait for its stream, which ends the capture).
 """
 import math
 from functools import partial
@@ -126,6 +128,7 @@ def append_tokens(cache, k, v, table, index, rows=None, positions=None, q=None, 
     vp = _heads(v, "v", cache.kv_heads, dim, dtype, dev)
     _need(v.shape[0] == n, "as many values as keys are needed")
     _need(table.dim() == 2, "table: [rows, pages of a row]")
+    _need(q is not None or q_norm is None, "q_norm without queries")
     heads, qp, op = 0, (None, 0, 0), (None, 0, 0)
     if q is not None:
         heads = q.shape[1]

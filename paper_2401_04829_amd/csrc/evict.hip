@@ -368,6 +368,8 @@ int check_eviction(const gnnshap_cache* c, const gnnshap_eviction* e) {
     return fail(GNNSHAP_EINVAL, "the first %lld and the last %lld of %lld kept tokens", static_cast<long long>(e->first),
                 static_cast<long long>(e->recent), static_cast<long long>(e->keep));
   if (e->weights_stride < 0 || e->new_weights_stride < 0) return fail(GNNSHAP_EINVAL, "negative stride of the weights");
+  if (e->new_weights_stride < e->max_length && e->num_seqs > 1)
+    return fail(GNNSHAP_EINVAL, "the new weights' rows, %lld apart, overlap", static_cast<long long>(e->new_weights_stride));
   if (e->weights && e->weights == e->new_weights && e->weights_stride != e->new_weights_stride)
     return fail(GNNSHAP_EINVAL, "new_weights are weights with another stride");
   return GNNSHAP_OK;

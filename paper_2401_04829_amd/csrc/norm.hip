@@ -257,13 +257,13 @@ extern "C" int gnnshap_norm_rotate_backward(const gnnshap_normed* n, const gnnsh
   const gnnshap_heads* kinds[2] = {&n->q, &n->k};
   for (int i = 0; i < 2; ++i) {
     const char* const name = i ? "keys" : "queries";
+    a.dw[i] = i ? dk_norm : dq_norm;
     if (kinds[i]->heads == 0) continue;
     if (!grads[i] || grads[i]->heads != kinds[i]->heads)
       return fail(GNNSHAP_EINVAL, "%s: no gradient, or one of other heads", name);
     if (n->num_tokens > 0 && !kinds[i]->x) return fail(GNNSHAP_EINVAL, "%s: NULL x", name);
     if (const int st = check_heads(*grads[i], name, n->num_tokens)) return st;
     a.grad[i] = *grads[i];
-    a.dw[i] = i ? dk_norm : dq_norm;
   }
   const int lanes = lay_out(a);
   const size_t need = carve(a, ws);
@@ -284,7 +284,7 @@ extern "C" int gnnshap_norm_rotate_backward(const gnnshap_normed* n, const gnnsh
       });
       if (st) return st;
     }
-    if (weights) {  // of no tokens too: they are 0
+    if (weights) {  // of no tokens or heads too: they are 0
       GS_TIMED("k_norm_weights_join", s);
       k_norm_weights_join<T><<<dim3(n->head_dim / kColumns, 2), 256, 0, s>>>(a);
       GS_LAUNCHED();

@@ -392,7 +392,8 @@ int check_observed(const gnnshap_cache* c, const gnnshap_observed* o) {
   if (o->num_players > 0 && (!o->masks || o->mask_words < ceil_div(o->num_players, 64)))
     return fail(GNNSHAP_EINVAL, "%lld players without masks, or with %lld words", static_cast<long long>(o->num_players),
                 static_cast<long long>(o->mask_words));
-  if (o->weights_stride < 0) return fail(GNNSHAP_EINVAL, "negative stride of the weights");
+  if (o->weights_stride < 0 || (o->weights_stride < o->max_length && o->num_rows > o->rows_per_seq))
+    return fail(GNNSHAP_EINVAL, "the weights' rows, %lld apart, overlap", static_cast<long long>(o->weights_stride));
   return GNNSHAP_OK;
 }
 
@@ -422,7 +423,7 @@ int lay_out(WeightsArgs& a, const gnnshap_cache* c, const gnnshap_observed* o) {
   // the kernel of many counts a sequence's bytes in 32 bits
   const int element = c->dtype == GNNSHAP_F32 ? 4 : 2;
   const int64_t limit = int64_t(1) << 31, rows = o->rows_per_seq;
-  const bool near = o->q_row_stride <= limit / element / rows && o->q_head_stride <= limit / element / o->heads &&
+  const bool near = o->q_row_stride >= 0 && o->q_head_stride >= 0 && o->q_row_stride <= limit / element / rows && o->q_head_stride <= limit / element / o->heads &&
                     rows * o->heads * 4 < limit && rows * std::max<int64_t>(o->mask_words, 1) * 8 < limit;
   if (a.queries <= 64 || !near) return check_launch(seqs * key_tiles(a, 128 / by_heads(a)), 256);
   const int64_t base = seqs * c->kv_heads * key_tiles(a, keys_of_many(a));

@@ -48,7 +48,8 @@ def test_caches_that_are_refused(change, status):
     (dict(max_length=65), L.EINVAL), (dict(max_length=-1), L.EINVAL), (dict(table_width=-1), L.EINVAL),
     (dict(max_length=2 ** 31, table_width=2 ** 31), L.EUNSUPPORTED), (dict(num_players=5), L.EINVAL),
     (dict(num_players=65, masks=P, mask_words=1), L.EINVAL), (dict(num_players=-1), L.EINVAL),
-    (dict(first_player=-1), L.EINVAL), (dict(weights_stride=-1), L.EINVAL)])
+    (dict(first_player=-1), L.EINVAL), (dict(weights_stride=-1), L.EINVAL), (dict(weights_stride=0), L.EINVAL),
+    (dict(weights_stride=63), L.EINVAL)])
 def test_queries_that_are_refused(change, status):
     lib, n = L.load(), ctypes.c_size_t()
     assert lib.gnnshap_cache_weights_workspace(_cache(), _observed(**change), n) == status
@@ -76,7 +77,9 @@ def test_weights_null_arrays_and_workspace():
     (dict(max_length=2 ** 31, table_width=2 ** 31), L.EUNSUPPORTED), (dict(keep=2 ** 31), L.EUNSUPPORTED),
     (dict(keep=0), L.EINVAL), (dict(first=-1), L.EINVAL), (dict(recent=-1), L.EINVAL), (dict(first=25), L.EINVAL),
     (dict(recent=29), L.EINVAL), (dict(first=33, recent=0), L.EINVAL), (dict(recent=2 ** 63 - 1), L.EINVAL),
-    (dict(weights_stride=-1), L.EINVAL), (dict(new_weights_stride=-1), L.EINVAL), (dict(new_weights_stride=65), L.EINVAL)])
+    (dict(weights_stride=-1), L.EINVAL), (dict(new_weights_stride=-1), L.EINVAL), (dict(new_weights_stride=65), L.EINVAL),
+    (dict(weights_stride=0, new_weights=2 * P, new_weights_stride=0), L.EINVAL),
+    (dict(weights_stride=63, new_weights_stride=63), L.EINVAL)])
 def test_evictions_that_are_refused(change, status):
     lib, n = L.load(), ctypes.c_size_t()
     assert lib.gnnshap_cache_evict_workspace(_cache(), _eviction(**change), n) == status

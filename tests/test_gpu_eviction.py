@@ -369,3 +369,23 @@ def test_graph_and_stream(dev):
             if seed == 0:
                 assert all(torch.equal(a, b) for a, b in zip(first, want))
             q.normal_(generator=_gen(dev, seed))
+
+
+@pytest.mark.parametrize("per", [1, 40])
+def test_a_cache_of_more_than_2_31_elements(dev, per):
+    """Its last pages give what the first ones do, bit for bit."""
+    gen = _gen(dev, 11)
+    n = 2 ** 31 // (64 * 4 * 128) + 8
+    far = A.PagedCache.empty(n, 64, 4, 128, device=dev)
+    near = _cache(gen, dev, torch.bfloat16, 6, 64, 4, 128)
+    for a, b in ((far.k, near.k), (far.v, near.v)):
+        a[-6:] = b
+    table = _pages(gen, dev, 2, 3)
+    lengths = torch.full((2,), 190, dtype=torch.int32, device=dev)
+    q = torch.randn((2 * per, 8, 128), generator=gen, device=dev).bfloat16()
+    lse = torch.full((2 * per, 8), 8.0, device=dev)
+    got = []
+    for cache, t in ((near, table), (far, table + (n - 6))):
+        w = A.attention_weights(cache, q, lse, t, lengths.repeat_interleave(per), torch.zeros((2, 192), device=dev))
+        got.append([w, *A.evict_tokens(cache, t, lengths, w, 100, 4, 20), cache.k[-6:], cache.v[-6:]])
+    assert all(torch.equal(a, b) for a, b in zip(*got)) and bool((got[0][0][:, :190] > 0).all())

@@ -335,3 +335,40 @@ def test_nothing_behind_the_outputs_is_written(dev):
             assert torch.equal(got[1:-1, 2:-3], x)
             got[1:-1, 2:-3] = 9.0
             assert bool((got == 9).all())
+
+
+@pytest.mark.parametrize("rows", [3, 300])
+def test_weights_of_more_than_2_31_elements_apart(dev, rows):
+    """The rows of a wide tensor's columns give what the same rows side by side do."""
+    h, w, t, gl, ge = _inputs(dev, torch.bfloat16, rows, 70000, 64)
+    wide = torch.empty((70000, 32768), dtype=torch.bfloat16, device=dev)
+    wide[:, 64:128] = w
+    got = []
+    for x in (w, wide[:, 64:128]):
+        r = A.linear_logprobs(h, x, t)
+        got.append([*r, *A.linear_logprobs_backward(h, x, t, r.maximum, r.log_sum, r.entropy, gl, ge)])
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+def test_captured_autograd(dev):
+    """Forward and backward by autograd, captured, replayed on other values."""
+    h, w, t, gl, ge = _inputs(dev, torch.bfloat16, 40, 1500, 128)
+    h.requires_grad_()
+    w.requires_grad_()
+
+    def step():
+        return torch.autograd.grad(A.differentiable_linear_logprobs(h, w, t), (h, w), (gl, ge))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for seed in range(3):
+        with torch.no_grad():
+            h.copy_(torch.randn(h.shape, generator=torch.Generator(dev).manual_seed(seed), device=dev))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, step()))

@@ -257,3 +257,39 @@ def test_graph_and_stream(dev):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(held, step()))
+
+
+def test_gradients_of_weights_without_heads(dev):
+    """No heads and no tokens: the weights' gradients are 0, not what memory held."""
+    w = torch.ones(64, device=dev)
+    for n, heads in ((5, 0), (0, 4)):
+        q, k = torch.zeros((n, heads, 64), device=dev), torch.zeros((n, 2, 64), device=dev)
+        torch.full((4096,), math.nan, device=dev)   # what the next allocations find
+        got = A.norm_rotate_backward(q, torch.ones_like(k), q, k, w, w)
+        assert int(got[2].count_nonzero()) == 0 and int(got[3].count_nonzero()) == 0
+
+
+def test_captured_autograd(dev):
+    """Forward and backward by autograd, captured, replayed on other values."""
+    gen = _gen(dev, 6)
+    q, k, gq, gk = (torch.randn((33, h, 128), generator=gen, device=dev).bfloat16() for h in (8, 2, 8, 2))
+    leaves = [x.requires_grad_() for x in (q, k, *(torch.ones(128, device=dev, dtype=torch.bfloat16) for _ in range(2)))]
+    cos, sin = _angles(dev, 33, 128)
+
+    def step():
+        out = A.differentiable_norm_rotate(*leaves, cos, sin)
+        return torch.autograd.grad(out, leaves, (gq, gk))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for seed in range(3):
+        with torch.no_grad():
+            q.copy_(torch.randn(q.shape, generator=_gen(dev, seed), device=dev))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, step()))

@@ -74,3 +74,12 @@ def test_tensors_that_are_refused():
         A.norm_rotate(x.requires_grad_())
     with pytest.raises(ValueError, match="has no derivative"):
         A.norm_rotate_backward(x.detach(), None, x)
+
+
+def test_a_norm_of_queries_needs_queries():
+    c = A.PagedCache.__new__(A.PagedCache)
+    c.k = c.v = torch.zeros((4, 16, 2, 64))
+    c.kv_heads, c.head_dim, c.page_size, c.dtype, c.device, c._c = 2, 64, 16, torch.float32, torch.device("cpu"), None
+    x, at = torch.zeros((3, 2, 64)), torch.zeros(3, dtype=torch.int32)
+    with pytest.raises(ValueError, match="q_norm without queries"):
+        A.append_tokens(c, x, x, at[None], at, q_norm=torch.ones(64))
