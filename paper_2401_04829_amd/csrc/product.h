@@ -87,10 +87,7 @@ struct Product {
   // which A and B start as many bytes further on.
   __device__ __forceinline__ void run(char* lds, const Operand& A, const Operand& B, int64_t m0, int64_t n0, int64_t K,
                                       int segments = 1, int64_t a_segment = 0, int64_t b_segment = 0) {
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-      for (int j = 0; j < NT; ++j) acc[i][j] = f4_t{0.f, 0.f, 0.f, 0.f};
+    clear_sums();
     const int per = static_cast<int>((K + KE - 1) / KE), chunks = per * segments;
     if (chunks == 0) return;
     const char* const a0 =
@@ -173,6 +170,7 @@ struct Product {
       wait<0>();
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
+      join_sums();
     } else {
       u4_t held[kLoads];
       const auto fetch = [&] {
@@ -227,6 +225,7 @@ struct Product {
         if (c + 1 < chunks) put(c + 1);
       }
       __syncthreads();
+      join_sums();
     }
   }
 
@@ -249,16 +248,46 @@ struct Product {
 
   typedef T vec8 __attribute__((ext_vector_type(8)));
   static __device__ __forceinline__ f4_t mfma(u4_t a, u4_t b, f4_t c) {
-    if constexpr (std::is_same_v<T, bf16_t>) {
+    if constexpr (std::is_same_v<T, bf16_t>)
       return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(vec8, a), __builtin_bit_cast(vec8, b), c, 0, 0, 0);
-    } else if constexpr (std::is_same_v<T, f16_t>) {
+    else
       return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(vec8, a), __builtin_bit_cast(vec8, b), c, 0, 0, 0);
+  }
+  // fp32, small tiles: a sum is kept in kParts parts, which take the fours of K in
+  // turn and are added at the end, so that fewer roundings meet a large sum: dw
+  // of 6,151 rows 5.0e-7 off instead of 1.4e-6, dh of 712 tokens 1.3e-7 instead of
+  // 3.4e-7, for 2 to 9 % of the time.  (Of large tiles two parts cost 5 to 8 %.)
+  static constexpr int kParts = sizeof(T) == 2 || MT * NT > 4 ? 1 : 8;
+  f4_t more[kParts > 1 ? kParts - 1 : 1][MT][NT];
+  __device__ __forceinline__ void add_product(int step, int i, int j, u4_t a, u4_t b) {
+    if constexpr (sizeof(T) == 2) {
+      acc[i][j] = mfma(a, b, acc[i][j]);
     } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
+      for (int e = 0; e < 4; ++e) {
+        const int part = (4 * step + e) % kParts;
+        f4_t& c = part == 0 ? acc[i][j] : more[part > 0 ? part - 1 : 0][i][j];
         c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[e]), __uint_as_float(b[e]), c, 0, 0, 0);
-      return c;
+      }
     }
+  }
+  __device__ __forceinline__ void clear_sums() {
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        acc[i][j] = f4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int p = 1; p < kParts; ++p) more[p - 1][i][j] = f4_t{0.f, 0.f, 0.f, 0.f};
+      }
+  }
+  __device__ __forceinline__ void join_sums() {
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int p = 1; p < kParts; ++p) acc[i][j] += more[p - 1][i][j];
   }
 
   // A wavefront's operands of one step: 64 bytes of K, of which the lane's
@@ -321,7 +350,7 @@ struct Product {
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = mfma(a[i], b[j], acc[i][j]);
+        for (int j = 0; j < NT; ++j) add_product(step, i, j, a[i], b[j]);
       __builtin_amdgcn_s_setprio(0);
     }
   }
