@@ -15,7 +15,9 @@
 //
 // dh sums over the vocabulary, of which several workgroups take parts where the
 // tiles are few: each keeps its part of the sum in fp32 over all pieces, and a
-// last launch adds the parts up in order.
+// last launch adds the parts up in order.  So do dw's workgroups with the rows,
+// where a small vocabulary leaves few tiles (100,000 rows x 41 tokens x 256
+// in bf16: 50 us instead of 880).
 //
 // In fp16 d is carried 2^k larger, k from the largest incoming gradient, so that
 // its largest elements are below 2^15 and those down to 2^-28 of them keep 11
@@ -27,6 +29,7 @@ namespace {
 using namespace gnnshap;
 
 constexpr int64_t kPieceBytes = int64_t(192) << 20;  // of d
+constexpr float kJoinTime = 6.f;                     // us, of a launch that adds up few parts
 
 template <class P>
 __global__ __launch_bounds__(P::kThreads) void k_linear_d(LinearArgs a) {
@@ -76,30 +79,32 @@ __global__ __launch_bounds__(P::kThreads) void k_linear_d(LinearArgs a) {
   }
 }
 
-struct HiddenArgs {
-  const void* weight;   // of the piece
-  int64_t weight_stride;
+// A product whose K is split: dh's always, dw's of few tiles and many rows.
+struct SplitArgs {
+  const void* a;        // turned over
+  int64_t a_stride;
   const void* d;
   int64_t pitch;
-  int64_t piece, rows, width;  // rows of d
+  int64_t K, rows, width;  // rows of the result, elements of a row
   unsigned tiles_m, tiles_n;
-  int64_t split;        // of the vocabulary, a workgroup
+  int64_t split;        // of K, a workgroup
   float* sums;          // [split][row][width]
-  bool first;           // piece
+  bool first;           // or: add to what is there
 };
 
-// dh's parts: a tile's rows are elements of the width, its columns rows of d.
+// The parts of dh (d by rows) or dw (d turned over): a tile's rows are elements
+// of the width, its columns rows of the result.
 template <class P>
-__global__ __launch_bounds__(P::kThreads) void k_linear_dh(HiddenArgs a) {
+__global__ __launch_bounds__(P::kThreads) void k_linear_parts(SplitArgs a) {
   using T = typename P::T;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const unsigned tiles = a.tiles_m * a.tiles_n, part = blockIdx.x / tiles;
   const TileAt tile = tile_at(blockIdx.x - part * tiles, a.tiles_m, a.tiles_n);
   const int64_t m0 = static_cast<int64_t>(tile.m) * P::TM, n0 = static_cast<int64_t>(tile.n) * P::TN;
-  const int64_t k0 = part * a.split, K = a.piece - k0 < a.split ? a.piece - k0 : a.split;
+  const int64_t k0 = part * a.split, K = a.K - k0 < a.split ? a.K - k0 : a.split;
   P p;
-  p.run(lds, Operand{static_cast<const T*>(a.weight) + k0 * a.weight_stride, a.weight_stride, a.width},
-        Operand{static_cast<const T*>(a.d) + k0, a.pitch, a.rows}, m0, n0, K > 0 ? K : 0);
+  p.run(lds, Operand{static_cast<const T*>(a.a) + k0 * a.a_stride, a.a_stride, a.width},
+        Operand{static_cast<const T*>(a.d) + (P::kTurnedB ? k0 * a.pitch : k0), a.pitch, a.rows}, m0, n0, K > 0 ? K : 0);
 #pragma unroll
   for (int t = 0; t < P::NT; ++t)
     p.template rows_out<float>(lds, t, [&](int j, int i) { return p.at(j, i, t); }, [&](int n, int m, const auto& x) {
@@ -132,10 +137,10 @@ struct JoinArgs {
   int64_t stride;
 };
 
-// Adds up dh's parts: four elements to a thread, and (few rows) WAYS threads to
+// Adds up the parts: four elements to a thread, and (few rows) WAYS threads to
 // these, each with every WAYS-th part (16 rows of 1,024 in 32 parts: 12.7 us with one, 4.0 with eight).
 template <class T, int WAYS>
-__global__ __launch_bounds__(256) void k_linear_dh_join(JoinArgs a) {
+__global__ __launch_bounds__(256) void k_linear_parts_join(JoinArgs a) {
   constexpr int kPacks = 256 / WAYS;
   __shared__ float sums[WAYS][kPacks][4];
   const int64_t packs = (a.width + 3) / 4, rows = a.two ? a.rows / 2 : a.rows;
@@ -254,52 +259,72 @@ constexpr unsigned kHiddenShapes = 0x1B;   // all but 128 x 64 and those whose A
 // dw's: the width by tokens.
 constexpr unsigned kWeightShapes = 0x0F;
 
-// How dh's product is laid out: its shape and how many workgroups take parts of
-// the vocabulary.  Each part is a sum more to write and to read.
+// A chunk by way of registers takes about so many times as long (1,000 rows x
+// 100 tokens x 100 in bf16, dw in 128 x 128: 2.2 us instead of 0.7).
+constexpr float kSlow = 3.f;
+
+// How a product whose K is split is laid out: its shape and how many workgroups
+// take parts of K.  Each part is a sum more to write and to read.
 struct Split {
   int shape;
   int64_t parts;
+  float time;   // us
 };
-Split hidden_split(const gnnshap_linear& l, int64_t rows, int64_t piece, unsigned shapes) {
-  const bool wide = l.dtype == GNNSHAP_F32;
-  Split best{-1, 1};
-  float least = 0.f;
+Split split_of(int64_t M, int64_t N, int64_t K, bool wide, unsigned shapes, float slow, int64_t least_parts) {
+  Split best{-1, 1, 0.f};
   for (int i = 0; i < kShapes; ++i) {
     if (!(shapes >> i & 1u)) continue;
-    const int64_t tiles = ceil_div(l.width, kTileM[i]) * ceil_div(rows, kTileN[i]);
-    for (int64_t parts = 1; parts <= 64; parts *= 2) {
-      if (parts > 1 && piece / parts < 256) break;
-      const int64_t chunks = ceil_div(ceil_div(piece, parts), wide ? 32 : 64);
+    const int64_t tiles = ceil_div(M, kTileM[i]) * ceil_div(N, kTileN[i]);
+    for (int64_t parts = least_parts; parts <= 64; parts *= 2) {
+      if (parts > 1 && K / parts < 256) break;
+      const int64_t chunks = ceil_div(ceil_div(K, parts), wide ? 32 : 64);
       // a part's sum: written and read, 8 bytes an element, at 3 TB/s
-      const float t = pace(i, wide, tiles * parts, l.width * parts) * static_cast<float>(chunks) +
-                      static_cast<float>(parts * rows * l.width) * 8.f / 3e6f;
-      if (best.shape < 0 || t < least) {
-        best = Split{i, parts};
-        least = t;
-      }
+      const float t = pace(i, wide, tiles * parts, M * parts) * slow * static_cast<float>(chunks) +
+                      static_cast<float>(parts * M * N) * 8.f / 3e6f;
+      if (best.shape < 0 || t < best.time) best = Split{i, parts, t};
     }
   }
   return best;
 }
 
-// The weights turned over: their packs lie along the width.
+// dw's parts, 1 where its tiles are enough: then it is written at once.
+Split weight_split(const gnnshap_linear& l, int64_t tokens, bool two, bool direct) {
+  const bool wide = l.dtype == GNNSHAP_F32;
+  const unsigned shapes = direct ? kWeightShapes : kWeightShapes & kThroughRegisters;
+  const float slow = direct ? 1.f : kSlow;
+  const Split none{-1, 1, 0.f};
+  if (two) return none;
+  const int shape = shape_for(l.width, tokens, wide, shapes);
+  const float whole = pace(shape, wide, ceil_div(l.width, kTileM[shape]) * ceil_div(tokens, kTileN[shape]), l.width) *
+                      slow * static_cast<float>(ceil_div(l.num_rows, wide ? 32 : 64));
+  const Split s = split_of(l.width, tokens, l.num_rows, wide, shapes, slow, 2);
+  return s.shape >= 0 && s.time + kJoinTime < whole ? s : none;
+}
+
+// The weights and the hidden states turned over: their packs lie along the width.
 template <class T>
 bool direct_weight(const gnnshap_linear& l) {
   return direct_operand<T>(l.weight, l.weight_stride, l.width, 256);
+}
+template <class T>
+bool direct_hidden(const gnnshap_linear& l) {
+  return direct_operand<T>(l.hidden, l.hidden_stride, l.width, 256);
 }
 
 // How the backward pass is laid out.
 struct Layout {
   bool two;
-  int hidden_shape;
-  int64_t d_rows, piece, pitch, split, parts;
+  int hidden_shape, weight_shape;
+  int64_t d_rows, piece, pitch;
+  int64_t split, parts;                  // of dh
+  int64_t weight_split, weight_parts;    // of dw; one part: written at once
   float* scale;
   void* d;
-  float* sums;
+  float *sums, *weight_sums;
 };
 
 template <class T>
-Layout lay_out(const gnnshap_linear& l, bool direct) {
+Layout lay_out(const gnnshap_linear& l, bool direct_w, bool direct_h) {
   Layout y{};
   y.two = sizeof(T) == 2 && l.num_rows <= kTwoParts;
   y.d_rows = y.two ? 2 * l.num_rows : l.num_rows;
@@ -308,11 +333,16 @@ Layout lay_out(const gnnshap_linear& l, bool direct) {
   const int64_t pieces = ceil_div(l.vocab, most);
   y.piece = ceil_div(ceil_div(l.vocab, pieces), 256) * 256;
   y.pitch = y.piece;
-  const Split h = hidden_split(l, std::max<int64_t>(y.d_rows, 1), std::min(y.piece, l.vocab),
-                               direct ? kHiddenShapes : kHiddenShapes & kThroughRegisters);
+  const int64_t tokens = std::min(y.piece, l.vocab);
+  const Split h = split_of(l.width, std::max<int64_t>(y.d_rows, 1), tokens, sizeof(T) == 4,
+                           direct_w ? kHiddenShapes : kHiddenShapes & kThroughRegisters, direct_w ? 1.f : kSlow, 1);
   y.hidden_shape = h.shape;
   y.split = ceil_div(ceil_div(y.piece, h.parts), 64) * 64;
   y.parts = ceil_div(y.piece, y.split);
+  const Split w = weight_split(l, tokens, y.two, direct_h);
+  y.weight_shape = w.shape;
+  y.weight_split = ceil_div(ceil_div(std::max<int64_t>(l.num_rows, 1), w.parts), 64) * 64;
+  y.weight_parts = ceil_div(std::max<int64_t>(l.num_rows, 1), y.weight_split);
   return y;
 }
 
@@ -321,6 +351,8 @@ size_t carve(Layout& y, const gnnshap_linear& l, void* ws) {
   y.scale = c.take<float>(2);
   y.d = c.take<char>(static_cast<size_t>(y.d_rows) * y.pitch * (l.dtype == GNNSHAP_F32 ? 4 : 2));
   y.sums = c.take<float>(static_cast<size_t>(y.parts) * y.d_rows * l.width);
+  if (y.weight_parts > 1)
+    y.weight_sums = c.take<float>(static_cast<size_t>(y.weight_parts) * std::min(y.piece, l.vocab) * l.width);
   return c.bytes();
 }
 
@@ -331,6 +363,23 @@ int launch(void (*kernel)(A), const char* name, const A& a, int64_t workgroups, 
   {
     GS_TIMED(name, s);
     kernel<<<static_cast<unsigned>(workgroups), P::kThreads, P::kLds, s>>>(a);
+  }
+  GS_LAUNCHED();
+  return GNNSHAP_OK;
+}
+
+template <class T>
+int join(const JoinArgs& j, hipStream_t s) {
+  const int64_t packs = (j.two ? j.rows / 2 : j.rows) * ceil_div(j.width, 4);
+  const bool few = j.parts > 8 && packs < 65536;
+  const int64_t groups = ceil_div(packs, few ? 32 : 256);
+  if (const int st = check_launch(groups, 256)) return st;
+  {
+    GS_TIMED("k_linear_parts_join", s);
+    if (few)
+      k_linear_parts_join<T, 8><<<static_cast<unsigned>(groups), 256, 0, s>>>(j);
+    else
+      k_linear_parts_join<T, 1><<<static_cast<unsigned>(groups), 256, 0, s>>>(j);
   }
   GS_LAUNCHED();
   return GNNSHAP_OK;
@@ -353,9 +402,7 @@ int run(const LinearArgs& given, void* grad_hidden, int64_t gh_stride, void* gra
   a.pitch = y.pitch;
   a.two = y.two;
   const bool direct_logits_too = direct_logits<T>(l);
-  // turned over, packs lie along the width
-  const bool direct_w = direct_weight<T>(l);
-  const bool direct_h = direct_operand<T>(l.hidden, l.hidden_stride, l.width, 256);
+  const bool direct_w = direct_weight<T>(l), direct_h = direct_hidden<T>(l);
   for (int64_t v0 = 0; v0 < l.vocab; v0 += y.piece) {
     const int64_t piece = std::min(y.piece, l.vocab - v0);
     int st = GNNSHAP_OK;
@@ -378,14 +425,26 @@ int run(const LinearArgs& given, void* grad_hidden, int64_t gh_stride, void* gra
     if (grad_hidden && l.num_rows > 0) {
       st = with_shape<T, true, false, kHiddenShapes>(y.hidden_shape, direct_w, [&](auto* p) {
         using P = std::remove_pointer_t<decltype(p)>;
-        HiddenArgs h{static_cast<const T*>(l.weight) + v0 * l.weight_stride, l.weight_stride, y.d, y.pitch, piece, y.d_rows,
-                     l.width, static_cast<unsigned>(ceil_div(l.width, P::TM)),
-                     static_cast<unsigned>(ceil_div(y.d_rows, P::TN)), y.split, y.sums, v0 == 0};
-        return launch<P>(k_linear_dh<P>, "k_linear_dh", h, y.parts * h.tiles_m * h.tiles_n, s);
+        SplitArgs h{static_cast<const T*>(l.weight) + v0 * l.weight_stride, l.weight_stride, y.d, y.pitch, piece, y.d_rows,
+                    l.width, static_cast<unsigned>(ceil_div(l.width, P::TM)),
+                    static_cast<unsigned>(ceil_div(y.d_rows, P::TN)), y.split, y.sums, v0 == 0};
+        return launch<P>(k_linear_parts<P>, "k_linear_dh", h, y.parts * h.tiles_m * h.tiles_n, s);
       });
       if (st) return st;
     }
-    if (grad_weight) {
+    if (grad_weight && y.weight_parts > 1) {
+      st = with_shape<T, true, true, kWeightShapes>(y.weight_shape, direct_h, [&](auto* p) {
+        using P = std::remove_pointer_t<decltype(p)>;
+        SplitArgs w{l.hidden, l.hidden_stride, y.d, y.pitch, l.num_rows, piece, l.width,
+                    static_cast<unsigned>(ceil_div(l.width, P::TM)), static_cast<unsigned>(ceil_div(piece, P::TN)),
+                    y.weight_split, y.weight_sums, true};
+        return launch<P>(k_linear_parts<P>, "k_linear_dw", w, y.weight_parts * w.tiles_m * w.tiles_n, s);
+      });
+      if (!st)
+        st = join<T>(JoinArgs{y.weight_sums, y.weight_parts, piece, l.width, false, a.scale,
+                              static_cast<T*>(grad_weight) + v0 * gw_stride, gw_stride}, s);
+      if (st) return st;
+    } else if (grad_weight) {
       const int segments = segments_for<false>(
           piece, l.width, std::max<int64_t>(l.num_rows, 1) * (y.two ? 2 : 1) * static_cast<int64_t>(sizeof(T)), sizeof(T) == 4,
           direct_h ? kWeightShapes : kWeightShapes & kThroughRegisters, segment);
@@ -401,21 +460,8 @@ int run(const LinearArgs& given, void* grad_hidden, int64_t gh_stride, void* gra
       if (st) return st;
     }
   }
-  if (grad_hidden && l.num_rows > 0) {
-    JoinArgs j{y.sums, y.parts, y.d_rows, l.width, y.two, a.scale, grad_hidden, gh_stride};
-    const int64_t packs = l.num_rows * ceil_div(l.width, 4);
-    const bool few = y.parts > 8 && packs < 65536;
-    const int64_t groups = ceil_div(packs, few ? 32 : 256);
-    if (const int st = check_launch(groups, 256)) return st;
-    {
-      GS_TIMED("k_linear_dh_join", s);
-      if (few)
-        k_linear_dh_join<T, 8><<<static_cast<unsigned>(groups), 256, 0, s>>>(j);
-      else
-        k_linear_dh_join<T, 1><<<static_cast<unsigned>(groups), 256, 0, s>>>(j);
-    }
-    GS_LAUNCHED();
-  }
+  if (grad_hidden && l.num_rows > 0)
+    return join<T>(JoinArgs{y.sums, y.parts, y.d_rows, l.width, y.two, a.scale, grad_hidden, gh_stride}, s);
   return GNNSHAP_OK;
 }
 
@@ -428,8 +474,8 @@ extern "C" int gnnshap_linear_logprobs_backward_workspace(const gnnshap_linear* 
   if (const int st = check_linear(l)) return st;
   return with_dtype(l->dtype, [&](auto* x) {
     *bytes = 0;
-    for (const bool direct : {true, false}) {  // as the call's addresses will have it
-      Layout y = lay_out<std::remove_pointer_t<decltype(x)>>(*l, direct);
+    for (const int direct : {0, 1, 2, 3}) {  // as the call's addresses will have it
+      Layout y = lay_out<std::remove_pointer_t<decltype(x)>>(*l, direct & 1, direct & 2);
       *bytes = std::max(*bytes, carve(y, *l, nullptr));
     }
     return static_cast<int>(GNNSHAP_OK);
@@ -456,7 +502,7 @@ extern "C" int gnnshap_linear_logprobs_backward(const gnnshap_linear* l, const f
   a.info = info;
   return with_dtype(l->dtype, [&](auto* x) {
     using T = std::remove_pointer_t<decltype(x)>;
-    Layout y = lay_out<T>(*l, direct_weight<T>(*l));
+    Layout y = lay_out<T>(*l, direct_weight<T>(*l), direct_hidden<T>(*l));
     const size_t need = carve(y, *l, ws);
     if (!ws || ws_bytes < need)
       return fail(GNNSHAP_ECAPACITY, "linear_logprobs_backward workspace needs %zu bytes, has %zu", need,

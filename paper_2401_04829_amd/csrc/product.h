@@ -40,7 +40,7 @@ template <class T_, int MT_, int NT_, int WAVES_M, int WAVES_N, int KB_, int STA
 struct Product {
   using T = T_;
   static constexpr int MT = MT_, NT = NT_, KB = KB_, STAGES = DIRECT_ ? STAGES_ : 2;
-  static constexpr bool DIRECT = DIRECT_;
+  static constexpr bool DIRECT = DIRECT_, kTurnedB = B_TURNED;
   static constexpr int TM = 16 * MT * WAVES_M, TN = 16 * NT * WAVES_N;
   static constexpr int kWaves = WAVES_M * WAVES_N, kThreads = 64 * kWaves;
   static constexpr int kOwnA = own_tiles<T>(MT), kOwnB = own_tiles<T>(NT);

@@ -96,6 +96,8 @@ class _Exact:
 SIZES = [  # rows, vocabulary, width: on all sides of the tiles (16, 64, 128, 256) and of the variants
     (1, 1, 8), (1, 5001, 264), (2, 2, 1), (16, 257, 64), (17, 255, 72), (40, 1000, 200), (128, 300, 136), (129, 513, 40),
     (257, 1025, 320), (300, 64, 96), (5, 700, 7), (150, 333, 77), (33, 256, 515),
+    # many rows of a small vocabulary, whose gradient is summed in parts
+    (5000, 41, 256), (1300, 17, 100), (2611, 5, 72), (9001, 2, 17),
 ]
 
 
