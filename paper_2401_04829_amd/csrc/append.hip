@@ -9,7 +9,7 @@
 // copy, or by the launch when there are few tokens.  20,000 bf16 tokens of
 // 32 query and 2 x 8 key and value heads of 128: 89 us in the kernel, 5.6 TB/s
 // (a large copy reaches 4.7 to 5.1); one token: 3 us.  The norm of a head is a sum
-// over the lanes that hold it (heads.h); with it 104 us and 4.
+// over the lanes that hold it (heads.h); with it 98 us and 4.
 #include "heads.h"
 
 namespace {

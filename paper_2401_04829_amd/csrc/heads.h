@@ -75,6 +75,8 @@ struct HeadUnits {
         for (int e = 0; e < N; ++e) v[j][h * N + e] = static_cast<float>(x.v[e]);
       }
   }
+  // (past the caches: 20,000 tokens into a cache 106 us by way of them, 98 past
+  // them; 16,384 tokens forward and backward 198 and 186)
   __device__ __forceinline__ void store(T* p) const {
 #pragma unroll
     for (int j = 0; j < kUnits; ++j)
@@ -84,7 +86,7 @@ struct HeadUnits {
         Pack<T, N> x;
 #pragma unroll
         for (int e = 0; e < N; ++e) x.v[e] = static_cast<T>(v[j][h * N + e]);
-        store_pack(p + at[j][h], x);
+        stream_pack(p + at[j][h], x);
       }
   }
   // 1 / sqrt(mean square + eps) of the head, in all of its lanes.

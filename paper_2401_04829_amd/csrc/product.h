@@ -48,6 +48,11 @@ struct Product {
   static constexpr int kVec = 16 / sizeof(T), kSteps = KB / 64;
   static constexpr int kBytesA = TM * KB, kBytesB = TN * KB, kStage = kBytesA + kBytesB;
   static constexpr int kLds = STAGES * kStage;
+  // Bytes of LDS of a launch: short sums need few buffers, and more workgroups fit a compute unit.
+  static int lds_for(int64_t K, int segments) {
+    const int64_t chunks = (K + KE - 1) / KE * segments;
+    return static_cast<int>(chunks < 1 ? 1 : chunks < STAGES ? chunks : STAGES) * kStage;
+  }
   // Moves of 1,024 bytes: each wavefront takes the same number of them (some of the last are made twice).
   static constexpr int kMoves = kStage / 1024, kLoads = (kMoves + kWaves - 1) / kWaves;
   static_assert(kBytesA % 1024 == 0 && kBytesB % 1024 == 0, "an operand's chunk is whole moves");
@@ -154,6 +159,13 @@ struct Product {
         if (c < chunks)
 #pragma unroll
           for (int step = 0; step < kSteps; ++step) issue(c, step);
+      if (chunks == 1 && K <= KE / kSteps) {  // a step is all there is
+        wait<0>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        multiply<1>(lds, [](int) {});
+      }
+      else
 #pragma unroll 1
       for (int c = 0; c < chunks; ++c) {
         // this chunk is there, and nobody reads the one before it any more
@@ -338,10 +350,10 @@ struct Product {
   // shares, and a wavefront that multiplies goes before one that reads (bf16,
   // 2,048 x 49,152 x 4,096 at 256 x 256: 725 us with all moves in front, 678 in
   // shares, 637 in shares and by priority; 10,000 x 32,768 x 2,048: 1,189, 1,129, 1,093).
-  template <class F>
+  template <int STEPS = kSteps, class F>
   __device__ __forceinline__ void multiply(const char* stage, F f) {
 #pragma unroll
-    for (int step = 0; step < kSteps; ++step) {
+    for (int step = 0; step < STEPS; ++step) {
       u4_t a[MT], b[NT];
       operands<B_TURNED, NT, kOwnB, TN>(b, stage + kBytesA, wave_n(), step);
       operands<A_TURNED, MT, kOwnA, TM>(a, stage, wave_m(), step);
@@ -375,7 +387,7 @@ struct Product {
   __device__ __forceinline__ void rows_out(char* lds, int t, V value, F store) const {
     constexpr int kPack = kRun * static_cast<int>(sizeof(O)) < 16 ? kRun : 16 / static_cast<int>(sizeof(O));
     constexpr int kPieces = 16 * MT / kPack, kBytes = kPack * static_cast<int>(sizeof(O));
-    static_assert(kWaves * 16 * 16 * MT * static_cast<int>(sizeof(O)) <= kLds, "a wavefront's rows fit");
+    static_assert(kWaves * 16 * 16 * MT * static_cast<int>(sizeof(O)) <= kStage, "a wavefront's rows fit");
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     char* const room = lds + wave * (16 * kPieces * kBytes);
     const auto at_piece = [&](int row, int piece) {

@@ -33,6 +33,18 @@ __device__ __forceinline__ void store_pack(T* p, const Pack<T, N>& r) {
   __builtin_memcpy(p, &r, sizeof(r));
 }
 
+// The same past the caches' usual order: for what is written once, in large, and
+// not read soon, so that it does not push out what is.
+template <class T, int N>
+__device__ __forceinline__ void stream_pack(T* p, const Pack<T, N>& r) {
+  if constexpr (sizeof(r) >= 4) {
+    typedef unsigned words __attribute__((ext_vector_type(sizeof(r) / 4), aligned(alignof(T))));
+    __builtin_nontemporal_store(__builtin_bit_cast(words, r), reinterpret_cast<words*>(p));
+  } else {
+    store_pack(p, r);
+  }
+}
+
 // Calls f with a null pointer of the element type that `dtype` names.
 template <class F>
 inline int with_dtype(int32_t dtype, F f) {
