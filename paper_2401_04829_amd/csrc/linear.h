@@ -11,7 +11,7 @@ namespace gnnshap {
 // elements, so that one rounding would show (up to 2^-8 in bf16, where the
 // result's own is 2^-9 on average; over many rows both come to 1.4 times the
 // result's own).  Of few rows it costs nothing beside the weights; of 200 it
-// would cost a third of the backward pass (50,021 x 2,048: 406 us against 303).
+// would cost nearly half the backward pass (50,021 x 2,048: 354 us against 245).
 constexpr int64_t kTwoParts = 128;
 
 struct LinearArgs {
@@ -65,8 +65,11 @@ constexpr Pace kPace[2][kShapes] = {{{1.7f, 1.8f}, {.71f, .53f}, {.53f, .42f}, {
 // Time of a chunk of `tiles` tiles that read `rows` rows of A.
 inline float pace(int shape, bool wide, int64_t tiles, int64_t rows) {
   const Pace& p = kPace[wide][shape];
-  // one workgroup of the largest shape fills a compute unit: rounds are whole
-  const float rounds = shape == 0 ? static_cast<float>(ceil_div(tiles, 256)) : static_cast<float>(tiles) / 256.f;
+  // one workgroup of the largest shape, and in fp32 of each, fills a compute unit:
+  // rounds are whole (87 rows x 17,374 tokens x 2,328, fp32: 182 us by parts of
+  // rounds, 132 by whole ones; of many rounds the last one matters less)
+  const bool whole = shape == 0 || (wide && tiles < 4 * 256);
+  const float rounds = whole ? static_cast<float>(ceil_div(tiles, 256)) : static_cast<float>(tiles) / 256.f;
   // A, the larger operand, comes from memory at 5.2 TB/s at most
   return std::max({p.alone, p.full * rounds, static_cast<float>(rows) * 128.f / 5.2e6f});
 }
