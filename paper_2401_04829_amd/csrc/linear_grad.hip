@@ -419,7 +419,8 @@ int run(const LinearArgs& given, void* grad_hidden, int64_t gh_stride, void* gra
           using P = std::remove_pointer_t<decltype(p)>;
           a.tiles_m = static_cast<unsigned>(ceil_div(a.tokens, P::TM));
           a.tiles_n = static_cast<unsigned>(ceil_div(l.num_rows, P::TN));
-          return launch<P>(k_linear_d<P>, "k_linear_d", a, static_cast<int64_t>(a.tiles_m) * a.tiles_n, P::lds_for(l.width, 1), s);
+          return launch<P>(k_linear_d<P>, "k_linear_d", a, static_cast<int64_t>(a.tiles_m) * a.tiles_n,
+                           P::lds_for(l.width, 1), s);
         });
         if (st) return st;
       }
@@ -430,7 +431,8 @@ int run(const LinearArgs& given, void* grad_hidden, int64_t gh_stride, void* gra
         SplitArgs h{static_cast<const T*>(l.weight) + v0 * l.weight_stride, l.weight_stride, y.d, y.pitch, piece, y.d_rows,
                     l.width, static_cast<unsigned>(ceil_div(l.width, P::TM)),
                     static_cast<unsigned>(ceil_div(y.d_rows, P::TN)), y.split, y.sums, v0 == 0};
-        return launch<P>(k_linear_parts<P>, "k_linear_dh", h, y.parts * h.tiles_m * h.tiles_n, P::lds_for(y.split, 1), s);
+        return launch<P>(k_linear_parts<P>, "k_linear_dh", h, y.parts * h.tiles_m * h.tiles_n,
+                         P::lds_for(y.split, 1), s);
       });
       if (st) return st;
     }
@@ -440,7 +442,8 @@ int run(const LinearArgs& given, void* grad_hidden, int64_t gh_stride, void* gra
         SplitArgs w{l.hidden, l.hidden_stride, y.d, y.pitch, l.num_rows, piece, l.width,
                     static_cast<unsigned>(ceil_div(l.width, P::TM)), static_cast<unsigned>(ceil_div(piece, P::TN)),
                     y.weight_split, y.weight_sums, true};
-        return launch<P>(k_linear_parts<P>, "k_linear_dw", w, y.weight_parts * w.tiles_m * w.tiles_n, P::lds_for(y.weight_split, 1), s);
+        return launch<P>(k_linear_parts<P>, "k_linear_dw", w, y.weight_parts * w.tiles_m * w.tiles_n,
+                         P::lds_for(y.weight_split, 1), s);
       });
       if (!st)
         st = join<T>(JoinArgs{y.weight_sums, y.weight_parts, piece, l.width, false, a.scale,

@@ -93,7 +93,8 @@ struct Product {
   __device__ __forceinline__ void run(char* lds, const Operand& A, const Operand& B, int64_t m0, int64_t n0, int64_t K,
                                       int segments = 1, int64_t a_segment = 0, int64_t b_segment = 0) {
     clear_sums();
-    const int per = static_cast<int>((K + KE - 1) / KE), chunks = per * segments;
+    const int per = static_cast<int>((K + KE - 1) / KE);
+    int chunks = per * segments;
     if (chunks == 0) return;
     const char* const a0 =
         static_cast<const char*>(A.p) + (A_TURNED ? m0 : m0 * A.stride) * static_cast<int64_t>(sizeof(T));
@@ -164,8 +165,8 @@ struct Product {
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         multiply<1>(lds, [](int) {});
+        chunks = 0;
       }
-      else
 #pragma unroll 1
       for (int c = 0; c < chunks; ++c) {
         // this chunk is there, and nobody reads the one before it any more
