@@ -836,10 +836,10 @@ int gnnshap_linear_logprobs_backward_workspace(const gnnshap_linear* linear, siz
  * piece of the vocabulary,
  *     grad_hidden = d weight,  grad_weight = d^T hidden,
  * summed in fp32 in a fixed order.  d enters these products in the elements'
- * type; of up to 128 rows in two parts, the second what the first's rounding
- * left.  Reads maximum, log_sum and entropy (with g_entropy) as
- * gnnshap_linear_logprobs wrote them.  grad_hidden, grad_weight, g_logprob and
- * g_entropy may be NULL.  With no rows grad_weight is 0. */
+ * type, of 16 bits in two parts, the second what the first's rounding left.
+ * Reads maximum, log_sum and entropy (with g_entropy) as gnnshap_linear_logprobs
+ * wrote them.  grad_hidden, grad_weight, g_logprob and g_entropy may be NULL.
+ * With no rows grad_weight is 0. */
 int gnnshap_linear_logprobs_backward(const gnnshap_linear* linear, const float* g_logprob, const float* g_entropy,
                                      void* grad_hidden, int64_t grad_hidden_stride, void* grad_weight,
                                      int64_t grad_weight_stride, int32_t* info, void* ws, size_t ws_bytes,

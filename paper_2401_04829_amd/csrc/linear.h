@@ -6,13 +6,19 @@
 
 namespace gnnshap {
 
-// Of up to this many rows the gradient by the logits is given in two 16-bit
-// parts, rounded and what that left: a few rows' gradients hang on few of its
-// elements, so that one rounding would show (up to 2^-8 in bf16, where the
-// result's own is 2^-9 on average; over many rows both come to 1.4 times the
-// result's own).  Of few rows it costs nothing beside the weights; of 200 it
-// would cost nearly half the backward pass (50,021 x 2,048: 354 us against 245).
-constexpr int64_t kTwoParts = 128;
+// The gradient by the logits, d, enters the products of 16-bit types in two parts,
+// rounded and what that left: rounded once, each of d's elements is off by up to u
+// of itself (2^-8 in bf16), which the sums over the vocabulary and the rows keep
+// even where the terms themselves cancel, as those of a vector that all weights
+// share do (sum_j d_j = 0): up to 10 times the result's own rounding instead of
+// none.  Two parts leave u^2, at the price of a product more for dh and for dw.
+// (2,000 rows x 50,021 tokens of 2,048 in bf16: 1,230 us with one part, 2,000 with
+// two; 200 rows: 258 and 355.)
+// Of up to this many rows dh takes the second parts as rows of their own, so that
+// the weights are read once; of more as a second sum over the vocabulary, so that
+// no more results are written and added up (50,021 x 2,048, bf16, rows of their
+// own and second sums: 200 rows 355 and 376 us, 256 rows 374 and 394, 400 rows 577 and 566).
+constexpr int64_t kBeside = 256;
 
 struct LinearArgs {
   gnnshap_linear l;
@@ -25,7 +31,7 @@ struct LinearArgs {
   const float* gl;
   const float* ge;
   const float* scale;         // of d in fp16, and one over it; NULL: 1
-  void* d;                    // [row, then what rounding left of row][pitch]
+  void* d;                    // [row, then (two parts) what rounding left of row][pitch]
   int64_t pitch;
   bool two;                   // d in two parts
   int64_t v0, tokens;         // the segment: its first token and how many

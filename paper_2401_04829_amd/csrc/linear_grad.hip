@@ -5,13 +5,13 @@
 // incoming gradients of a row,
 //     d_j = g (1[j = t] - p_j) - g_H p_j (log p_j + H),
 //     dh = d w,  dw = d^T h.
-// The logits are not kept by the forward pass: they are computed again (the
-// same product, bit for bit), for a piece of the vocabulary at a time, whose d
-// is written in the elements' type and read by the two other products; w and h
+// The logits are not kept by the forward pass: they are computed again, for a
+// piece of the vocabulary at a time, whose d is written in the elements' type
+// (of 16 bits in two parts, linear.h) and read by the two other products; w and h
 // are turned over on the way from LDS to the matrix instructions.  So are three
-// products of 2 rows vocabulary width operations each, where many rows make
-// them bound by the matrix instructions; few rows are bound by reading the
-// weights twice and writing their gradient once.
+// products of 2 rows vocabulary width operations each, in 16 bits five, where many
+// rows make them bound by the matrix instructions; few rows are bound by reading
+// the weights twice and writing their gradient once.
 //
 // dh sums over the vocabulary, of which several workgroups take parts where the
 // tiles are few: each keeps its part of the sum in fp32 over all pieces, and a
@@ -28,7 +28,11 @@ namespace {
 
 using namespace gnnshap;
 
-constexpr int64_t kPieceBytes = int64_t(192) << 20;  // of d
+// Of d, all of it: each piece is another round of launches, whose last workgroups
+// leave compute units without work, and another reading and writing of dh's sums
+// (10,000 rows x 32,768 tokens of 2,048 in bf16: 9,220 us with 192 MB, 7,080 with 384,
+// 6,260 with 768, 6,150 with 1,536).
+constexpr int64_t kPieceBytes = int64_t(768) << 20;
 constexpr float kJoinTime = 6.f;                     // us, of a launch that adds up few parts
 
 template <class P>
@@ -86,6 +90,8 @@ struct SplitArgs {
   const void* d;
   int64_t pitch;
   int64_t K, rows, width;  // rows of the result, elements of a row
+  int segments;            // d's parts, of which each starts `d_part` bytes behind the one before
+  int64_t d_part;
   unsigned tiles_m, tiles_n;
   int64_t split;        // of K, a workgroup
   float* sums;          // [split][row][width]
@@ -104,7 +110,8 @@ __global__ __launch_bounds__(P::kThreads) void k_linear_parts(SplitArgs a) {
   const int64_t k0 = part * a.split, K = a.K - k0 < a.split ? a.K - k0 : a.split;
   P p;
   p.run(lds, Operand{static_cast<const T*>(a.a) + k0 * a.a_stride, a.a_stride, a.width},
-        Operand{static_cast<const T*>(a.d) + (P::kTurnedB ? k0 * a.pitch : k0), a.pitch, a.rows}, m0, n0, K > 0 ? K : 0);
+        Operand{static_cast<const T*>(a.d) + (P::kTurnedB ? k0 * a.pitch : k0), a.pitch, a.rows}, m0, n0, K > 0 ? K : 0,
+        a.segments, 0, a.d_part);
 #pragma unroll
   for (int t = 0; t < P::NT; ++t)
     p.template rows_out<float>(lds, t, [&](int j, int i) { return p.at(j, i, t); }, [&](int n, int m, const auto& x) {
@@ -195,7 +202,8 @@ struct WeightArgs {
   const void* d;
   int64_t pitch;
   int64_t piece, rows, width;  // rows of the hidden states
-  bool two;
+  int segments;                // as in SplitArgs
+  int64_t d_part;
   unsigned tiles_m, tiles_n;
   const float* scale;
   void* out;            // of the piece
@@ -212,8 +220,8 @@ __global__ __launch_bounds__(P::kThreads) void k_linear_dw(WeightArgs a) {
   const TileAt tile = tile_at(blockIdx.x, a.tiles_m, a.tiles_n);
   const int64_t m0 = static_cast<int64_t>(tile.m) * P::TM, n0 = static_cast<int64_t>(tile.n) * P::TN;
   P p;
-  p.run(lds, Operand{a.hidden, a.hidden_stride, a.width}, Operand{a.d, a.pitch, a.piece}, m0, n0, a.rows, a.two ? 2 : 1,
-        0, a.rows * a.pitch * static_cast<int64_t>(sizeof(T)));
+  p.run(lds, Operand{a.hidden, a.hidden_stride, a.width}, Operand{a.d, a.pitch, a.piece}, m0, n0, a.rows, a.segments,
+        0, a.d_part);
   const float over = a.scale ? a.scale[1] : 1.f;
   constexpr int kPack = 16 / sizeof(T);
   static_assert(P::kRun >= kPack, "a lane's run is whole packs");
@@ -272,14 +280,14 @@ struct Split {
   int64_t parts;
   float time;   // us
 };
-Split split_of(int64_t M, int64_t N, int64_t K, bool wide, unsigned shapes, float slow, int64_t least_parts) {
+Split split_of(int64_t M, int64_t N, int64_t K, int segments, bool wide, unsigned shapes, float slow, int64_t least_parts) {
   Split best{-1, 1, 0.f};
   for (int i = 0; i < kShapes; ++i) {
     if (!(shapes >> i & 1u)) continue;
     const int64_t tiles = ceil_div(M, kTileM[i]) * ceil_div(N, kTileN[i]);
     for (int64_t parts = least_parts; parts <= 64; parts *= 2) {
       if (parts > 1 && K / parts < 256) break;
-      const int64_t chunks = ceil_div(ceil_div(K, parts), wide ? 32 : 64);
+      const int64_t chunks = ceil_div(ceil_div(K, parts), wide ? 32 : 64) * segments;
       // a part's sum: written and read, 8 bytes an element, at 3 TB/s
       const float t = pace(i, wide, tiles * parts, M * parts) * slow * static_cast<float>(chunks) +
                       static_cast<float>(parts * M * N) * 8.f / 3e6f;
@@ -290,17 +298,15 @@ Split split_of(int64_t M, int64_t N, int64_t K, bool wide, unsigned shapes, floa
 }
 
 // dw's parts, 1 where its tiles are enough: then it is written at once.
-Split weight_split(const gnnshap_linear& l, int64_t tokens, bool two, bool direct) {
+Split weight_split(const gnnshap_linear& l, int64_t tokens, int segments, bool direct) {
   const bool wide = l.dtype == GNNSHAP_F32;
   const unsigned shapes = direct ? kWeightShapes : kWeightShapes & kThroughRegisters;
   const float slow = direct ? 1.f : kSlow;
-  const Split none{-1, 1, 0.f};
-  if (two) return none;
   const int shape = shape_for(l.width, tokens, wide, shapes);
   const float whole = pace(shape, wide, ceil_div(l.width, kTileM[shape]) * ceil_div(tokens, kTileN[shape]), l.width) *
-                      slow * static_cast<float>(ceil_div(l.num_rows, wide ? 32 : 64));
-  const Split s = split_of(l.width, tokens, l.num_rows, wide, shapes, slow, 2);
-  return s.shape >= 0 && s.time + kJoinTime < whole ? s : none;
+                      slow * static_cast<float>(ceil_div(l.num_rows, wide ? 32 : 64) * segments);
+  const Split s = split_of(l.width, tokens, l.num_rows, segments, wide, shapes, slow, 2);
+  return s.shape >= 0 && s.time + kJoinTime < whole ? s : Split{-1, 1, 0.f};
 }
 
 // The weights and the hidden states turned over: their packs lie along the width.
@@ -315,9 +321,9 @@ bool direct_hidden(const gnnshap_linear& l) {
 
 // How the backward pass is laid out.
 struct Layout {
-  bool two;
+  bool two, beside;                      // d in two parts, dh with these as rows beside each other
   int hidden_shape, weight_shape;
-  int64_t d_rows, piece, pitch;
+  int64_t d_rows, hidden_rows, piece, pitch;   // rows of d and of dh's product
   int64_t split, parts;                  // of dh
   int64_t weight_split, weight_parts;    // of dw; one part: written at once
   float* scale;
@@ -328,20 +334,22 @@ struct Layout {
 template <class T>
 Layout lay_out(const gnnshap_linear& l, bool direct_w, bool direct_h) {
   Layout y{};
-  y.two = sizeof(T) == 2 && l.num_rows <= kTwoParts;
+  y.two = sizeof(T) == 2;
+  y.beside = y.two && l.num_rows <= kBeside;
   y.d_rows = y.two ? 2 * l.num_rows : l.num_rows;
+  y.hidden_rows = y.beside ? 2 * l.num_rows : l.num_rows;
   // pieces of like size, whole tiles of 256
   const int64_t most = std::max<int64_t>(kPieceBytes / (std::max<int64_t>(y.d_rows, 1) * sizeof(T)) / 256 * 256, 256);
   const int64_t pieces = ceil_div(l.vocab, most);
   y.piece = ceil_div(ceil_div(l.vocab, pieces), 256) * 256;
   y.pitch = y.piece;
   const int64_t tokens = std::min(y.piece, l.vocab);
-  const Split h = split_of(l.width, std::max<int64_t>(y.d_rows, 1), tokens, sizeof(T) == 4,
+  const Split h = split_of(l.width, std::max<int64_t>(y.hidden_rows, 1), tokens, y.two && !y.beside ? 2 : 1, sizeof(T) == 4,
                            direct_w ? kHiddenShapes : kHiddenShapes & kThroughRegisters, direct_w ? 1.f : kSlow, 1);
   y.hidden_shape = h.shape;
   y.split = ceil_div(ceil_div(y.piece, h.parts), 64) * 64;
   y.parts = ceil_div(y.piece, y.split);
-  const Split w = weight_split(l, tokens, y.two, direct_h);
+  const Split w = weight_split(l, tokens, y.two ? 2 : 1, direct_h);
   y.weight_shape = w.shape;
   y.weight_split = ceil_div(ceil_div(std::max<int64_t>(l.num_rows, 1), w.parts), 64) * 64;
   y.weight_parts = ceil_div(std::max<int64_t>(l.num_rows, 1), y.weight_split);
@@ -352,7 +360,7 @@ size_t carve(Layout& y, const gnnshap_linear& l, void* ws) {
   Carver c(ws);
   y.scale = c.take<float>(2);
   y.d = c.take<char>(static_cast<size_t>(y.d_rows) * y.pitch * (l.dtype == GNNSHAP_F32 ? 4 : 2));
-  y.sums = c.take<float>(static_cast<size_t>(y.parts) * y.d_rows * l.width);
+  y.sums = c.take<float>(static_cast<size_t>(y.parts) * y.hidden_rows * l.width);
   if (y.weight_parts > 1)
     y.weight_sums = c.take<float>(static_cast<size_t>(y.weight_parts) * std::min(y.piece, l.vocab) * l.width);
   return c.bytes();
@@ -405,6 +413,8 @@ int run(const LinearArgs& given, void* grad_hidden, int64_t gh_stride, void* gra
   a.two = y.two;
   const bool direct_logits_too = direct_logits<T>(l);
   const bool direct_w = direct_weight<T>(l), direct_h = direct_hidden<T>(l);
+  const int64_t d_part = l.num_rows * y.pitch * static_cast<int64_t>(sizeof(T));
+  const int hidden_segments = y.two && !y.beside ? 2 : 1, weight_segments = y.two ? 2 : 1;
   for (int64_t v0 = 0; v0 < l.vocab; v0 += y.piece) {
     const int64_t piece = std::min(y.piece, l.vocab - v0);
     int st = GNNSHAP_OK;
@@ -428,22 +438,22 @@ int run(const LinearArgs& given, void* grad_hidden, int64_t gh_stride, void* gra
     if (grad_hidden && l.num_rows > 0) {
       st = with_shape<T, true, false, kHiddenShapes>(y.hidden_shape, direct_w, [&](auto* p) {
         using P = std::remove_pointer_t<decltype(p)>;
-        SplitArgs h{static_cast<const T*>(l.weight) + v0 * l.weight_stride, l.weight_stride, y.d, y.pitch, piece, y.d_rows,
-                    l.width, static_cast<unsigned>(ceil_div(l.width, P::TM)),
-                    static_cast<unsigned>(ceil_div(y.d_rows, P::TN)), y.split, y.sums, v0 == 0};
+        SplitArgs h{static_cast<const T*>(l.weight) + v0 * l.weight_stride, l.weight_stride, y.d, y.pitch, piece, y.hidden_rows,
+                    l.width, hidden_segments, d_part, static_cast<unsigned>(ceil_div(l.width, P::TM)),
+                    static_cast<unsigned>(ceil_div(y.hidden_rows, P::TN)), y.split, y.sums, v0 == 0};
         return launch<P>(k_linear_parts<P>, "k_linear_dh", h, y.parts * h.tiles_m * h.tiles_n,
-                         P::lds_for(y.split, 1), s);
+                         P::lds_for(y.split, hidden_segments), s);
       });
       if (st) return st;
     }
     if (grad_weight && y.weight_parts > 1) {
       st = with_shape<T, true, true, kWeightShapes>(y.weight_shape, direct_h, [&](auto* p) {
         using P = std::remove_pointer_t<decltype(p)>;
-        SplitArgs w{l.hidden, l.hidden_stride, y.d, y.pitch, l.num_rows, piece, l.width,
+        SplitArgs w{l.hidden, l.hidden_stride, y.d, y.pitch, l.num_rows, piece, l.width, weight_segments, d_part,
                     static_cast<unsigned>(ceil_div(l.width, P::TM)), static_cast<unsigned>(ceil_div(piece, P::TN)),
                     y.weight_split, y.weight_sums, true};
         return launch<P>(k_linear_parts<P>, "k_linear_dw", w, y.weight_parts * w.tiles_m * w.tiles_n,
-                         P::lds_for(y.weight_split, 1), s);
+                         P::lds_for(y.weight_split, weight_segments), s);
       });
       if (!st)
         st = join<T>(JoinArgs{y.weight_sums, y.weight_parts, piece, l.width, false, a.scale,
@@ -451,23 +461,23 @@ int run(const LinearArgs& given, void* grad_hidden, int64_t gh_stride, void* gra
       if (st) return st;
     } else if (grad_weight) {
       const int segments = segments_for<false>(
-          piece, l.width, std::max<int64_t>(l.num_rows, 1) * (y.two ? 2 : 1) * static_cast<int64_t>(sizeof(T)), sizeof(T) == 4,
+          piece, l.width, std::max<int64_t>(l.num_rows, 1) * weight_segments * static_cast<int64_t>(sizeof(T)), sizeof(T) == 4,
           direct_h ? kWeightShapes : kWeightShapes & kThroughRegisters, segment);
       for (int i = 0; i < segments && !st; ++i)
         st = with_shape<T, true, true, kWeightShapes>(segment[i].shape, direct_h, [&](auto* p) {
           using P = std::remove_pointer_t<decltype(p)>;
           WeightArgs w{l.hidden, l.hidden_stride, static_cast<const T*>(y.d) + segment[i].begin, y.pitch, segment[i].tokens,
-                       l.num_rows, l.width, y.two, static_cast<unsigned>(ceil_div(l.width, P::TM)),
+                       l.num_rows, l.width, weight_segments, d_part, static_cast<unsigned>(ceil_div(l.width, P::TM)),
                        static_cast<unsigned>(ceil_div(segment[i].tokens, P::TN)), a.scale,
                        static_cast<T*>(grad_weight) + (v0 + segment[i].begin) * gw_stride, gw_stride};
           return launch<P>(k_linear_dw<P>, "k_linear_dw", w, static_cast<int64_t>(w.tiles_m) * w.tiles_n,
-                           P::lds_for(l.num_rows, y.two ? 2 : 1), s);
+                           P::lds_for(l.num_rows, weight_segments), s);
         });
       if (st) return st;
     }
   }
   if (grad_hidden && l.num_rows > 0)
-    return join<T>(JoinArgs{y.sums, y.parts, y.d_rows, l.width, y.two, a.scale, grad_hidden, gh_stride}, s);
+    return join<T>(JoinArgs{y.sums, y.parts, y.hidden_rows, l.width, y.beside, a.scale, grad_hidden, gh_stride}, s);
   return GNNSHAP_OK;
 }
 
