@@ -55,15 +55,6 @@ struct HeadUnits {
       if (u >= D / (2 * N)) at[j][0] = at[j][1] = -1;
     }
   }
-  // f(float&, element) of each element that the lane has.
-  template <class F>
-  __device__ __forceinline__ void each(F f) {
-#pragma unroll
-    for (int j = 0; j < kUnits; ++j)
-#pragma unroll
-      for (int e = 0; e < 2 * N; ++e)
-        if (at[j][0] >= 0) f(v[j][e], at[j][e / N] + e % N);
-  }
   __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
     for (int j = 0; j < kUnits; ++j)

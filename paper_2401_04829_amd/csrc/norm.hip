@@ -9,7 +9,9 @@
 // sums over a head are moves between these lanes.  Everything is read once
 // and written once.  The weights' gradient stays in the lanes' registers over
 // all of a workgroup's heads, is added up in LDS, then by a second launch over
-// the workgroups, always in the same order.  Bound by memory: 16,384 bf16 tokens
+// the workgroups, always in the same order; of fp32 heads in 64 bits, as every
+// chain of 32 additions in 32 bits would leave about 1.4e-7 (500 tokens of 8 heads of 64:
+// 2.2e-7 off with all three chains in 32 bits).  Bound by memory: 16,384 bf16 tokens
 // of 32 + 8 heads of 128: 61 us forward (336 MB, 5.5 TB/s), 109 us backward (503 MB,
 // 4.6 TB/s) and 4 to add up.
 #include "heads.h"
@@ -18,10 +20,14 @@ namespace {
 
 using namespace gnnshap;
 
+// What the weights' gradients are summed in.
+template <class T>
+using Sum = std::conditional_t<std::is_same_v<T, float>, double, float>;
+
 struct NormArgs {
   gnnshap_normed n;
   gnnshap_heads grad[2];  // of queries and keys
-  float* part[2];         // [workgroup][head_dim] of the weights' gradients
+  void* part[2];          // [workgroup][head_dim] of the weights' gradients, of type Sum<T>
   int groups[2];          // workgroups that take the queries, the keys
   void* dw[2];
   int32_t* info;
@@ -59,22 +65,23 @@ __global__ __launch_bounds__(256) void k_norm_rotate(NormArgs a) {
 // The first groups[0] workgroups take the queries' heads, the others the keys'.
 template <class T, int N>
 __global__ __launch_bounds__(256) void k_norm_rotate_grad(NormArgs a) {
-  __shared__ float sums[256 * HeadUnits<T, N>::kUnits * 2 * N];
+  using Units = HeadUnits<T, N>;
+  __shared__ Sum<T> sums[256 * Units::kUnits * 2 * N];
   const bool is_k = static_cast<int>(blockIdx.x) >= a.groups[0];
   const int group = is_k ? blockIdx.x - a.groups[0] : blockIdx.x, groups = a.groups[is_k];
   const gnnshap_heads& h = is_k ? a.n.k : a.n.q;
   const gnnshap_heads& g = a.grad[is_k];
   const T* const weight = static_cast<const T*>(is_k ? a.n.k_norm : a.n.q_norm);
   const int D = a.n.head_dim, rot = a.n.cos ? a.n.rot_dim : 0;
-  using Units = HeadUnits<T, N>;
-  Units w(D, rot, a.n.interleaved), dw = w;
+  Units w(D, rot, a.n.interleaved);
+  Sum<T> dw[Units::kUnits][2 * N];
   if (weight) w.load(weight);
 #pragma unroll
   for (int j = 0; j < Units::kUnits; ++j)
 #pragma unroll
     for (int e = 0; e < 2 * N; ++e) {
       if (!weight) w.v[j][e] = 1.f;
-      dw.v[j][e] = 0.f;
+      dw[j][e] = 0;
     }
   // the workgroups' heads in turn; from one to the next `on` tokens and `heads_on` heads further
   const int64_t first = static_cast<int64_t>(group) * blockDim.y + threadIdx.y;
@@ -99,7 +106,7 @@ __global__ __launch_bounds__(256) void k_norm_rotate_grad(NormArgs a) {
 #pragma unroll
       for (int e = 0; e < 2 * N; ++e) {
         x.v[j][e] *= r;
-        dw.v[j][e] += z.v[j][e] * x.v[j][e];
+        dw[j][e] += static_cast<Sum<T>>(z.v[j][e]) * x.v[j][e];
         z.v[j][e] *= w.v[j][e];
         along += z.v[j][e] * x.v[j][e];
       }
@@ -111,12 +118,16 @@ __global__ __launch_bounds__(256) void k_norm_rotate_grad(NormArgs a) {
     z.store(static_cast<T*>(g.out) + t * g.out_token_stride + head * g.out_head_stride);
   }
   if (!a.dw[is_k]) return;
-  dw.each([&](float& s, int d) { sums[threadIdx.y * D + d] = s; });
+#pragma unroll
+  for (int j = 0; j < Units::kUnits; ++j)
+#pragma unroll
+    for (int e = 0; e < 2 * N; ++e)
+      if (w.at[j][0] >= 0) sums[threadIdx.y * D + w.at[j][e / N] + e % N] = dw[j][e];
   __syncthreads();
   for (int d = threadIdx.y * blockDim.x + threadIdx.x; d < D; d += blockDim.x * blockDim.y) {
-    float s = 0.f;
+    Sum<T> s = 0;
     for (unsigned y = 0; y < blockDim.y; ++y) s += sums[y * D + d];
-    a.part[is_k][static_cast<int64_t>(group) * D + d] = s;
+    static_cast<Sum<T>*>(a.part[is_k])[static_cast<int64_t>(group) * D + d] = s;
   }
 }
 
@@ -125,17 +136,18 @@ constexpr int kColumns = 8;  // of a workgroup that adds up parts
 // Adds up the workgroups' parts of the weights' gradients.
 template <class T>
 __global__ __launch_bounds__(256) void k_norm_weights_join(NormArgs a) {
-  __shared__ float sums[256 / kColumns][kColumns];
+  __shared__ Sum<T> sums[256 / kColumns][kColumns];
   const int is_k = blockIdx.y, c = threadIdx.x % kColumns, y = threadIdx.x / kColumns, D = a.n.head_dim;
   const int d = blockIdx.x * kColumns + c;
   if (!a.dw[is_k]) return;
-  float s = 0.f;
+  Sum<T> s = 0;
+  const Sum<T>* const part = static_cast<const Sum<T>*>(a.part[is_k]);
 #pragma unroll 8
-  for (int i = y; i < a.groups[is_k]; i += 256 / kColumns) s += a.part[is_k][static_cast<int64_t>(i) * D + d];
+  for (int i = y; i < a.groups[is_k]; i += 256 / kColumns) s += part[static_cast<int64_t>(i) * D + d];
   sums[y][c] = s;
   __syncthreads();
   if (y > 0) return;
-  s = 0.f;
+  s = 0;
   for (int i = 0; i < 256 / kColumns; ++i) s += sums[i][c];
   static_cast<T*>(a.dw[is_k])[d] = static_cast<T>(s);
 }
@@ -195,7 +207,8 @@ int lay_out(NormArgs& a) {
 
 size_t carve(NormArgs& a, void* ws) {
   Carver c(ws);
-  for (int i = 0; i < 2; ++i) a.part[i] = c.take<float>(static_cast<size_t>(a.groups[i]) * a.n.head_dim);
+  const size_t sum = a.n.dtype == GNNSHAP_F32 ? sizeof(Sum<float>) : sizeof(Sum<bf16_t>);
+  for (int i = 0; i < 2; ++i) a.part[i] = c.take<char>(static_cast<size_t>(a.groups[i]) * a.n.head_dim * sum);
   return c.bytes();
 }
 
