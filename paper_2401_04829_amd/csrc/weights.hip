@@ -198,14 +198,19 @@ struct QueryTile {
 
 // With n the whole number next to lse log2 e, a weight is 2^(s log2 e - n) times
 // f = e^(n ln 2 - lse): one multiplication and addition makes the exponent, whose
-// rounding is that of the score, and f, which is the row's, rides on the sum.
+// rounding is that of the score, and f, which is the row's, rides on the sum.  f's
+// argument is reduced by ln 2 in two parts (the method of Cody and Waite): the
+// first has 15 bits, so that n times it less lse is exact up to n = 2^9 and rounded
+// once beyond (fused), the second is what is left of ln 2.  n itself has 24 bits:
+// below 2^30 it is 65 off at most and f finite, so that what a row does not see, 0
+// times f, adds nothing; from there on lse has no bits to make up for, and f is 1.
 template <class T, int DP, int NK>
 __device__ __forceinline__ void add(const WeightsArgs& a, const Players<NK>& p, KeyTile<T, DP, NK>& t,
                                     const QueryTile<T, DP, NK>& q, int64_t k0, bool& bad) {
   constexpr float kLn2High = 0.693145752f, kLn2Low = 1.42860677e-6f;   // their sum is ln 2
   const float n = rintf(q.lse * kLog2eF);
   float f = __builtin_amdgcn_exp2f(fmaf(n, kLn2Low, fmaf(n, kLn2High, -q.lse)) * kLog2eF);
-  f = fabsf(n) < INFINITY ? f : 1.f;   // (an lse that is not finite is in the exponents)
+  f = fabsf(n) < 0x1p30f ? f : 1.f;
   uint32_t bits[NK / 2], any = 0u;
 #pragma unroll
   for (int w = 0; w < NK / 2; ++w) {
