@@ -474,8 +474,9 @@ class _Logprob(torch.autograd.Function):
     def forward(ctx, logits, targets):
         maximum, log_sum = torch.empty((2, logits.shape[0]), dtype=torch.float32, device=logits.device).unbind(0)
         r = token_logprobs(logits, targets, maximum=maximum, log_sum=log_sum)
-        ctx.save_for_backward(logits, targets, r.lse, r.entropy, maximum, log_sum)
-        return r.logprob, r.entropy
+        logprob, entropy = r.logprob.data, r.entropy.data   # (autograd refuses to change views in place)
+        ctx.save_for_backward(logits, targets, r.lse, entropy, maximum, log_sum)
+        return logprob, entropy
 
     @staticmethod
     def backward(ctx, grad_logprob, grad_entropy):
@@ -573,8 +574,9 @@ class _LinearLogprob(torch.autograd.Function):
     @staticmethod
     def forward(ctx, hidden, weight, targets):
         r = linear_logprobs(hidden, weight, targets)
-        ctx.save_for_backward(hidden, weight, targets, r.maximum, r.log_sum, r.entropy)
-        return r.logprob, r.entropy
+        logprob, entropy = r.logprob.data, r.entropy.data   # (autograd refuses to change views in place)
+        ctx.save_for_backward(hidden, weight, targets, r.maximum, r.log_sum, entropy)
+        return logprob, entropy
 
     @staticmethod
     def backward(ctx, grad_logprob, grad_entropy):
