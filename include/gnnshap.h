@@ -71,7 +71,12 @@ enum gnnshap_status {
 
 const char* gnnshap_status_str(int status);
 const char* gnnshap_last_error(void);
-int gnnshap_version(void); /* major*10000 + minor*100 + patch */
+/* major*10000 + minor*100 + patch.  Structs grow at their ends with the minor
+ * number: a program makes no other call into a library whose gnnshap_version() / 100
+ * is not the GNNSHAP_VERSION / 100 that it was compiled with, since a longer struct's
+ * end would be read behind its own.  200: gnnshap_new_tokens has norms. */
+#define GNNSHAP_VERSION 200
+int gnnshap_version(void);
 
 /* ------------------------------------------------------------------------ */
 /* Graph: in-CSR of a simple directed graph (row = destination).            */

@@ -11,6 +11,7 @@ LIB_PATH = os.path.join(_HERE, "libgnnshap.so")
 HEADER = os.path.join(os.path.dirname(_HERE), "include", "gnnshap.h")
 
 OK, EINVAL, ECAPACITY, EHIP, ESINGULAR, EUNSUPPORTED = range(6)
+VERSION = 200      # GNNSHAP_VERSION, that of the structs below
 MAX_HOPS = 8
 MAX_LAYERS = 8
 
@@ -214,6 +215,9 @@ def load():
             fn = getattr(lib, name)
             fn.restype = res
             fn.argtypes = args
+        if lib.gnnshap_version() // 100 != VERSION // 100:
+            raise RuntimeError(f"{LIB_PATH} is of version {lib.gnnshap_version()}, not {VERSION}; run "
+                               "`python -m paper_2401_04829_amd.build`")
         _lib = lib
     return _lib
 

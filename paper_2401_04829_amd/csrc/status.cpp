@@ -36,6 +36,6 @@ const char* gnnshap_status_str(int status) {
 
 const char* gnnshap_last_error(void) { return gnnshap::g_msg; }
 
-int gnnshap_version(void) { return 100; /* 0.1.0 */ }
+int gnnshap_version(void) { return GNNSHAP_VERSION; }
 
 }  // extern "C"
