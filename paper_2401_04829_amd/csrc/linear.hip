@@ -111,7 +111,7 @@ size_t carve(LinearArgs& a, void* ws) {
 // The call's segments and a row's parts; a refusal of more workgroups than a launch takes.
 template <class T>
 int lay_out(LinearArgs& a, bool direct, Segment (&s)[2], int& segments) {
-  segments = logit_segments<T>(a.l.vocab, a.l, direct, s);
+  segments = logit_segments(a.l.vocab, a.l, sizeof(T), direct, s);
   int64_t parts = 0;
   for (int i = 0; i < segments; ++i) {
     const int64_t m = ceil_div(s[i].tokens, kTileM[s[i].shape]), n = ceil_div(a.l.num_rows, kTileN[s[i].shape]);

@@ -5,8 +5,10 @@
 // incoming gradients of a row,
 //     d_j = g (1[j = t] - p_j) - g_H p_j (log p_j + H),
 //     dh = d w,  dw = d^T h.
-// The logits are not kept by the forward pass: they are computed again, for a
-// piece of the vocabulary at a time, whose d is written in the elements' type
+// The logits are not kept by the forward pass: they are computed again (of 16-bit
+// elements the same sums; in fp32 a piece's tiles may sum in another order than
+// the forward's, by whose rounding their logits then differ), for a piece of the
+// vocabulary at a time, whose d is written in the elements' type
 // (of 16 bits in two parts, linear.h) and read by the two other products; w and h
 // are turned over on the way from LDS to the matrix instructions.  So are three
 // products of 2 rows vocabulary width operations each, in 16 bits five, where many
@@ -27,13 +29,6 @@
 namespace {
 
 using namespace gnnshap;
-
-// Of d, all of it: each piece is another round of launches, whose last workgroups
-// leave compute units without work, and another reading and writing of dh's sums
-// (10,000 rows x 32,768 tokens of 2,048 in bf16: 9,220 us with 192 MB, 7,080 with 384,
-// 6,260 with 768, 6,150 with 1,536).
-constexpr int64_t kPieceBytes = int64_t(768) << 20;
-constexpr float kJoinTime = 6.f;                     // us, of a launch that adds up few parts
 
 template <class P>
 __global__ __launch_bounds__(P::kThreads) void k_linear_d(LinearArgs a) {
@@ -264,51 +259,6 @@ __global__ __launch_bounds__(1024) void k_linear_scale(LinearArgs a, float* scal
   scale[1] = ldexpf(1.f, -k);
 }
 
-// dh's product: a tile's rows are elements of the width, its columns rows of d.
-constexpr unsigned kHiddenShapes = 0x1B;   // all but 128 x 64 and those whose A would be read element by element
-// dw's: the width by tokens.
-constexpr unsigned kWeightShapes = 0x0F;
-
-// A chunk by way of registers takes about so many times as long (1,000 rows x
-// 100 tokens x 100 in bf16, dw in 128 x 128: 2.2 us instead of 0.7).
-constexpr float kSlow = 3.f;
-
-// How a product whose K is split is laid out: its shape and how many workgroups
-// take parts of K.  Each part is a sum more to write and to read.
-struct Split {
-  int shape;
-  int64_t parts;
-  float time;   // us
-};
-Split split_of(int64_t M, int64_t N, int64_t K, int segments, bool wide, unsigned shapes, float slow, int64_t least_parts) {
-  Split best{-1, 1, 0.f};
-  for (int i = 0; i < kShapes; ++i) {
-    if (!(shapes >> i & 1u)) continue;
-    const int64_t tiles = ceil_div(M, kTileM[i]) * ceil_div(N, kTileN[i]);
-    for (int64_t parts = least_parts; parts <= 64; parts *= 2) {
-      if (parts > 1 && K / parts < 256) break;
-      const int64_t chunks = ceil_div(ceil_div(K, parts), wide ? 32 : 64) * segments;
-      // a part's sum: written and read, 8 bytes an element, at 3 TB/s
-      const float t = pace(i, wide, tiles * parts, M * parts) * slow * static_cast<float>(chunks) +
-                      static_cast<float>(parts * M * N) * 8.f / 3e6f;
-      if (best.shape < 0 || t < best.time) best = Split{i, parts, t};
-    }
-  }
-  return best;
-}
-
-// dw's parts, 1 where its tiles are enough: then it is written at once.
-Split weight_split(const gnnshap_linear& l, int64_t tokens, int segments, bool direct) {
-  const bool wide = l.dtype == GNNSHAP_F32;
-  const unsigned shapes = direct ? kWeightShapes : kWeightShapes & kThroughRegisters;
-  const float slow = direct ? 1.f : kSlow;
-  const int shape = shape_for(l.width, tokens, wide, shapes);
-  const float whole = pace(shape, wide, ceil_div(l.width, kTileM[shape]) * ceil_div(tokens, kTileN[shape]), l.width) *
-                      slow * static_cast<float>(ceil_div(l.num_rows, wide ? 32 : 64) * segments);
-  const Split s = split_of(l.width, tokens, l.num_rows, segments, wide, shapes, slow, 2);
-  return s.shape >= 0 && s.time + kJoinTime < whole ? s : Split{-1, 1, 0.f};
-}
-
 // The weights and the hidden states turned over: their packs lie along the width.
 template <class T>
 bool direct_weight(const gnnshap_linear& l) {
@@ -317,43 +267,6 @@ bool direct_weight(const gnnshap_linear& l) {
 template <class T>
 bool direct_hidden(const gnnshap_linear& l) {
   return direct_operand<T>(l.hidden, l.hidden_stride, l.width, 256);
-}
-
-// How the backward pass is laid out.
-struct Layout {
-  bool two, beside;                      // d in two parts, dh with these as rows beside each other
-  int hidden_shape, weight_shape;
-  int64_t d_rows, hidden_rows, piece, pitch;   // rows of d and of dh's product
-  int64_t split, parts;                  // of dh
-  int64_t weight_split, weight_parts;    // of dw; one part: written at once
-  float* scale;
-  void* d;
-  float *sums, *weight_sums;
-};
-
-template <class T>
-Layout lay_out(const gnnshap_linear& l, bool direct_w, bool direct_h) {
-  Layout y{};
-  y.two = sizeof(T) == 2;
-  y.beside = y.two && l.num_rows <= kBeside;
-  y.d_rows = y.two ? 2 * l.num_rows : l.num_rows;
-  y.hidden_rows = y.beside ? 2 * l.num_rows : l.num_rows;
-  // pieces of like size, whole tiles of 256
-  const int64_t most = std::max<int64_t>(kPieceBytes / (std::max<int64_t>(y.d_rows, 1) * sizeof(T)) / 256 * 256, 256);
-  const int64_t pieces = ceil_div(l.vocab, most);
-  y.piece = ceil_div(ceil_div(l.vocab, pieces), 256) * 256;
-  y.pitch = y.piece;
-  const int64_t tokens = std::min(y.piece, l.vocab);
-  const Split h = split_of(l.width, std::max<int64_t>(y.hidden_rows, 1), tokens, y.two && !y.beside ? 2 : 1, sizeof(T) == 4,
-                           direct_w ? kHiddenShapes : kHiddenShapes & kThroughRegisters, direct_w ? 1.f : kSlow, 1);
-  y.hidden_shape = h.shape;
-  y.split = ceil_div(ceil_div(y.piece, h.parts), 64) * 64;
-  y.parts = ceil_div(y.piece, y.split);
-  const Split w = weight_split(l, tokens, y.two ? 2 : 1, direct_h);
-  y.weight_shape = w.shape;
-  y.weight_split = ceil_div(ceil_div(std::max<int64_t>(l.num_rows, 1), w.parts), 64) * 64;
-  y.weight_parts = ceil_div(std::max<int64_t>(l.num_rows, 1), y.weight_split);
-  return y;
 }
 
 size_t carve(Layout& y, const gnnshap_linear& l, void* ws) {
@@ -414,13 +327,12 @@ int run(const LinearArgs& given, void* grad_hidden, int64_t gh_stride, void* gra
   const bool direct_logits_too = direct_logits<T>(l);
   const bool direct_w = direct_weight<T>(l), direct_h = direct_hidden<T>(l);
   const int64_t d_part = l.num_rows * y.pitch * static_cast<int64_t>(sizeof(T));
-  const int hidden_segments = y.two && !y.beside ? 2 : 1, weight_segments = y.two ? 2 : 1;
   for (int64_t v0 = 0; v0 < l.vocab; v0 += y.piece) {
     const int64_t piece = std::min(y.piece, l.vocab - v0);
     int st = GNNSHAP_OK;
     Segment segment[2];
     if (l.num_rows > 0) {
-      const int segments = logit_segments<T>(piece, l, direct_logits_too, segment);
+      const int segments = logit_segments(piece, l, sizeof(T), direct_logits_too, segment);
       for (int i = 0; i < segments; ++i) {
         a.v0 = v0 + segment[i].begin;
         a.tokens = segment[i].tokens;
@@ -439,39 +351,37 @@ int run(const LinearArgs& given, void* grad_hidden, int64_t gh_stride, void* gra
       st = with_shape<T, true, false, kHiddenShapes>(y.hidden_shape, direct_w, [&](auto* p) {
         using P = std::remove_pointer_t<decltype(p)>;
         SplitArgs h{static_cast<const T*>(l.weight) + v0 * l.weight_stride, l.weight_stride, y.d, y.pitch, piece, y.hidden_rows,
-                    l.width, hidden_segments, d_part, static_cast<unsigned>(ceil_div(l.width, P::TM)),
+                    l.width, y.hidden_segments, d_part, static_cast<unsigned>(ceil_div(l.width, P::TM)),
                     static_cast<unsigned>(ceil_div(y.hidden_rows, P::TN)), y.split, y.sums, v0 == 0};
         return launch<P>(k_linear_parts<P>, "k_linear_dh", h, y.parts * h.tiles_m * h.tiles_n,
-                         P::lds_for(y.split, hidden_segments), s);
+                         P::lds_for(y.split, y.hidden_segments), s);
       });
       if (st) return st;
     }
     if (grad_weight && y.weight_parts > 1) {
       st = with_shape<T, true, true, kWeightShapes>(y.weight_shape, direct_h, [&](auto* p) {
         using P = std::remove_pointer_t<decltype(p)>;
-        SplitArgs w{l.hidden, l.hidden_stride, y.d, y.pitch, l.num_rows, piece, l.width, weight_segments, d_part,
+        SplitArgs w{l.hidden, l.hidden_stride, y.d, y.pitch, l.num_rows, piece, l.width, y.weight_segments, d_part,
                     static_cast<unsigned>(ceil_div(l.width, P::TM)), static_cast<unsigned>(ceil_div(piece, P::TN)),
                     y.weight_split, y.weight_sums, true};
         return launch<P>(k_linear_parts<P>, "k_linear_dw", w, y.weight_parts * w.tiles_m * w.tiles_n,
-                         P::lds_for(y.weight_split, weight_segments), s);
+                         P::lds_for(y.weight_split, y.weight_segments), s);
       });
       if (!st)
         st = join<T>(JoinArgs{y.weight_sums, y.weight_parts, piece, l.width, false, a.scale,
                               static_cast<T*>(grad_weight) + v0 * gw_stride, gw_stride}, s);
       if (st) return st;
     } else if (grad_weight) {
-      const int segments = segments_for<false>(
-          piece, l.width, std::max<int64_t>(l.num_rows, 1) * weight_segments * static_cast<int64_t>(sizeof(T)), sizeof(T) == 4,
-          direct_h ? kWeightShapes : kWeightShapes & kThroughRegisters, segment);
+      const int segments = weight_segments_for(piece, l, sizeof(T), y.weight_segments, direct_h, segment);
       for (int i = 0; i < segments && !st; ++i)
         st = with_shape<T, true, true, kWeightShapes>(segment[i].shape, direct_h, [&](auto* p) {
           using P = std::remove_pointer_t<decltype(p)>;
           WeightArgs w{l.hidden, l.hidden_stride, static_cast<const T*>(y.d) + segment[i].begin, y.pitch, segment[i].tokens,
-                       l.num_rows, l.width, weight_segments, d_part, static_cast<unsigned>(ceil_div(l.width, P::TM)),
+                       l.num_rows, l.width, y.weight_segments, d_part, static_cast<unsigned>(ceil_div(l.width, P::TM)),
                        static_cast<unsigned>(ceil_div(segment[i].tokens, P::TN)), a.scale,
                        static_cast<T*>(grad_weight) + (v0 + segment[i].begin) * gw_stride, gw_stride};
           return launch<P>(k_linear_dw<P>, "k_linear_dw", w, static_cast<int64_t>(w.tiles_m) * w.tiles_n,
-                           P::lds_for(l.num_rows, weight_segments), s);
+                           P::lds_for(l.num_rows, y.weight_segments), s);
         });
       if (st) return st;
     }
@@ -491,7 +401,7 @@ extern "C" int gnnshap_linear_logprobs_backward_workspace(const gnnshap_linear* 
   return with_dtype(l->dtype, [&](auto* x) {
     *bytes = 0;
     for (const int direct : {0, 1, 2, 3}) {  // as the call's addresses will have it
-      Layout y = lay_out<std::remove_pointer_t<decltype(x)>>(*l, direct & 1, direct & 2);
+      Layout y = lay_out(*l, sizeof(std::remove_pointer_t<decltype(x)>), direct & 1, direct & 2);
       *bytes = std::max(*bytes, carve(y, *l, nullptr));
     }
     return static_cast<int>(GNNSHAP_OK);
@@ -518,7 +428,7 @@ extern "C" int gnnshap_linear_logprobs_backward(const gnnshap_linear* l, const f
   a.info = info;
   return with_dtype(l->dtype, [&](auto* x) {
     using T = std::remove_pointer_t<decltype(x)>;
-    Layout y = lay_out<T>(*l, direct_weight<T>(*l), direct_hidden<T>(*l));
+    Layout y = lay_out(*l, sizeof(T), direct_weight<T>(*l), direct_hidden<T>(*l));
     const size_t need = carve(y, *l, ws);
     if (!ws || ws_bytes < need)
       return fail(GNNSHAP_ECAPACITY, "linear_logprobs_backward workspace needs %zu bytes, has %zu", need,

@@ -4,7 +4,9 @@ room only for what fp32 sums leave.
 
 The root mean square of a row's errors is at most 1.3 times that of rounding
 the exact row (256 elements and more: their mean square is off by a tenth at
-most) and, beside that, of `rest` times the terms' sizes |d| |w| (|d|^T |h|).
+most) and, beside that, of `rest` times the terms' sizes s |w| (s^T |h|), s_j =
+|g| (1[j = t] + p_j) + |g_H| p_j (|log p_j| + H) (not |d_j|: a relative error of
+p_j is one of these parts of d_j, however much 1 - p_j or log p_j + H cancel).
 rest, with u the type's half unit, D the width and n the terms of a sum:
   - d in two parts of a 16-bit type: u^2;
   - a logit's sum of D products: 2^-24 sqrt(D) of the products' root sum of
@@ -51,11 +53,13 @@ def exact(h, w, t, gl, ge, part=512):
         d = -p * (gl[rows, None] + ge[rows, None].double() * (logp + ent))
         at = torch.arange(x.shape[0], device=h.device)
         d[at, t[rows].clamp(min=0)] += gl[rows]
+        s = p * (gl[rows, None].abs() + ge[rows, None].abs().double() * (logp.abs() + ent))
+        s[at, t[rows].clamp(min=0)] += gl[rows].abs()
         root = max(root, float((x.square() @ w2.t()).max().sqrt()))
         dh.append(d @ w64)
-        dh_size.append(d.abs() @ w64.abs())
+        dh_size.append(s @ w64.abs())
         dw = dw + d.t() @ x
-        dw_size = dw_size + d.abs().t() @ x.abs()
+        dw_size = dw_size + s.t() @ x.abs()
     return torch.cat(dh), torch.cat(dh_size), dw, dw_size, root
 
 
