@@ -43,8 +43,8 @@
  *     a call reports.  gnnshap_last_error() gives a thread-local message about
  *     the last failure.
  *   - All floating-point device data is fp32, row-major, except the token
- *     operators' (gnnshap_cache_*, gnnshap_token_*), which name their element
- *     type and strides.
+ *     operators' (gnnshap_cache_*, gnnshap_norm_*, gnnshap_token_*,
+ *     gnnshap_linear_*), which name their element type and strides.
  */
 #ifndef GNNSHAP_H
 #define GNNSHAP_H

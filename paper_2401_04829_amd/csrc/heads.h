@@ -66,8 +66,9 @@ struct HeadUnits {
         for (int e = 0; e < N; ++e) v[j][h * N + e] = static_cast<float>(x.v[e]);
       }
   }
-  // (past the caches: 20,000 tokens into a cache 106 us by way of them, 98 past
-  // them; 16,384 tokens forward and backward 198 and 186)
+  // (past the caches, few heads or many: 20,000 tokens into a cache 106 us by way of
+  // them, 98 past them; 16,384 tokens forward and backward 198 and 186; without
+  // what reads them next)
   __device__ __forceinline__ void store(T* p) const {
 #pragma unroll
     for (int j = 0; j < kUnits; ++j)

@@ -19,7 +19,7 @@
 // tiles are few: each keeps its part of the sum in fp32 over all pieces, and a
 // last launch adds the parts up in order.  So do dw's workgroups with the rows,
 // where a small vocabulary leaves few tiles (100,000 rows x 41 tokens x 256
-// in bf16: 50 us instead of 880).
+// in bf16: 35 us before the join; written at once, with d in one part, 880).
 //
 // In fp16 d is carried 2^k larger, k from the largest incoming gradient, so that
 // its largest elements are below 2^15 and those down to 2^-28 of them keep 11

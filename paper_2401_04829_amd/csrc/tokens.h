@@ -33,8 +33,8 @@ __device__ __forceinline__ void store_pack(T* p, const Pack<T, N>& r) {
   __builtin_memcpy(p, &r, sizeof(r));
 }
 
-// The same past the caches' usual order: for what is written once, in large, and
-// not read soon, so that it does not push out what is.
+// The same past the caches' usual order, so that what is written once does not push
+// out what is read: for results of a pass over memory.
 template <class T, int N>
 __device__ __forceinline__ void stream_pack(T* p, const Pack<T, N>& r) {
   if constexpr (sizeof(r) >= 4) {
