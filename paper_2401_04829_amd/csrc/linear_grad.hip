@@ -71,7 +71,11 @@ __global__ __launch_bounds__(P::kThreads) void k_linear_d(LinearArgs a) {
     });
     if (a.two)
       p.template rows_out<T>(
-          lds, t, [&](int j, int i) { return static_cast<T>(d[j][i] - static_cast<float>(static_cast<T>(d[j][i]))); },
+          lds, t,
+          [&](int j, int i) {
+            const float rest = d[j][i] - static_cast<float>(static_cast<T>(d[j][i]));
+            return static_cast<T>(rest == rest ? rest : 0.f);  // an infinite d stays one
+          },
           [&](int n, int m, const auto& x) {
             if (b0 + n < a.l.num_rows) store_pack(out + (a.l.num_rows + b0 + n) * a.pitch + m, x);
           });
